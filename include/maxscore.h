@@ -259,6 +259,89 @@ maxscore_status maxscore_combine_bwd(maxscore_ctx* ctx, const void* dY, const vo
 maxscore_status maxscore_gate_bwd(maxscore_ctx* ctx, const void* hidden, const void* w_gate,
                                   const float* dlogits, float* dw_gate, void* dH, void* cuda_stream);
 
+/* ---- the experts between dispatch and combine ----------------------------------------------------- */
+
+/* Products of the expert buffers with one weight matrix per expert.  A buffer is [E, C, width] in io_dtype; expert e
+ * owns its first min(expert_load[e], C) rows (a negative load counts as 0) and only those take part: what lies behind
+ * them is never used, whatever it holds, and the rows behind them in an output buffer become zero, as in dispatch.
+ *   w_layout 0: weights are [E, d_in, d_out] as w_gate in Eq. 2;  1: [E, d_out, d_in].
+ *   Widths (d_in, d_out, d_ff) need not be d_model; a multiple of 8 for bf16 I/O and of 4 for fp32, as d_model.
+ * Products are accumulated in fp32 and rounded once.  Outputs must not overlap inputs.  Reproducible bit for bit.
+ * After the bf16 calls maxscore_check_internal tells whether a bounded wait gave up, as for maxscore_gate.
+ * Errors: NULL (unless said otherwise) or misaligned pointers, an output that is an input's own buffer, non-positive
+ * widths, w_layout not 0 or 1 -> MAXSCORE_ERR_INVALID_ARG; widths that are no such multiple -> MAXSCORE_ERR_UNSUPPORTED. */
+
+/* y[e, s, :] = x[e, s, :] . W_e.   x [E, C, d_in], y [E, C, d_out].
+ * The gradient with respect to x is the same call on dy with d_in and d_out exchanged and the other w_layout. */
+maxscore_status maxscore_expert_gemm(maxscore_ctx* ctx, const void* x, const void* w, const int32_t* expert_load, void* y,
+                                     int32_t d_in, int32_t d_out, int32_t w_layout, void* cuda_stream);
+
+/* Gradient with respect to the weights: dw_e = sum over the rows s in use of x[e, s, :]^T dy[e, s, :], always fp32, in the
+ * layout of the weights ([E, d_in, d_out] or [E, d_out, d_in]).  accumulate != 0 adds to dw; an expert without rows
+ * gets (adds) zero. */
+maxscore_status maxscore_expert_gemm_dw(maxscore_ctx* ctx, const void* x, const void* dy, const int32_t* expert_load, float* dw,
+                                        int32_t d_in, int32_t d_out, int32_t w_layout, int accumulate, void* cuda_stream);
+
+/* First product of a gated expert with its activation: [g | u] = x . W_up, h = silu(g) * u, silu(g) = g / (1 + e^-g).
+ *   w_up [E, d_in, 2 d_ff] (w_layout 1: [E, 2 d_ff, d_in]), gate columns first
+ *   pre  [E, C, 2 d_ff] out, [g | u] rounded to io_dtype for maxscore_expert_glu_bwd, or NULL
+ *   h    [E, C, d_ff]   out, from the unrounded g and u */
+maxscore_status maxscore_expert_glu(maxscore_ctx* ctx, const void* x, const void* w_up, const int32_t* expert_load, void* pre,
+                                    void* h, int32_t d_in, int32_t d_ff, int32_t w_layout, void* cuda_stream);
+
+/* Backward of the activation through the second product y = h . W_down: dh = dy . W_down^T is not stored;
+ *   dpre[e, s, :] = [dh * u * s * (1 + g (1 - s)) | dh * g * s],  s = 1 / (1 + e^-g).
+ *   dy [E, C, d_out], w_down [E, d_ff, d_out] (w_layout 1: [E, d_out, d_ff]), pre as maxscore_expert_glu left it,
+ *   dpre [E, C, 2 d_ff] out.
+ * The other gradients: dx = expert_gemm(dpre) with d_in = 2 d_ff and the other layout of w_up, dw_up = expert_gemm_dw(x,
+ * dpre), dw_down = expert_gemm_dw(h, dy). */
+maxscore_status maxscore_expert_glu_bwd(maxscore_ctx* ctx, const void* dy, const void* w_down, const void* pre,
+                                        const int32_t* expert_load, void* dpre, int32_t d_out, int32_t d_ff, int32_t w_layout,
+                                        void* cuda_stream);
+
+/* ---- the norms before and after the block ---------------------------------------------------------- */
+
+/* After-norm, gate, scaled residual and before-norm around a block, all steps in one pass over the rows:
+ *   n_i  = y_i / rms(y_i) * (w_offset + w_post)                 w_post NULL: n = y
+ *   r'_i = res_scale * residual_i + gate[i / rows_per_gate] * n_i    gate NULL: n is added as it is
+ *   h_i  = r'_i / rms(r'_i) * (w_offset + w_pre)                w_pre NULL: no h
+ * with rms(v)^2 = mean(v^2) + eps.  y and r' are rounded to io_dtype and each norm takes the rounded row, so that the
+ * backward call, which is handed those rows, works from the same numbers.  Sums are fp32.
+ *   w_post, w_pre [d_model], gate [ceil(T / rows_per_gate), d_model]: DEVICE memory, io_dtype, 16-byte aligned.
+ * Limits: d_model <= 16384 for bf16 I/O, 8192 for fp32 (MAXSCORE_ERR_UNSUPPORTED). */
+typedef struct {
+  const void* w_post;    /* after-norm weight or NULL                                              */
+  const void* gate;      /* gate rows or NULL                                                      */
+  const void* w_pre;     /* weight of the norm before the next block, or NULL                      */
+  int32_t rows_per_gate; /* consecutive tokens that share a gate row, > 0 when gate is given       */
+  float eps;             /* > 0, finite                                                            */
+  float w_offset;        /* added to both norm weights (0, or 1 for weights stored around zero)    */
+  float res_scale;       /* finite                                                                 */
+} maxscore_norm;
+
+/* maxscore_combine followed by the steps above, without the round trip of y through memory.
+ *   src, expert_idx, slot_idx, gate_w as in maxscore_combine (gate_w NULL = unit weights)
+ *   residual [T, d_model] in; y [T, d_model] out or NULL (what maxscore_combine would have written, bit for bit; the
+ *   backward call needs it); r_out [T, d_model] out (may be residual's buffer); h [T, d_model] out, NULL iff w_pre is. */
+maxscore_status maxscore_combine_norm(maxscore_ctx* ctx, const void* src, const int32_t* expert_idx, const int32_t* slot_idx,
+                                      const float* gate_w, const void* residual, const maxscore_norm* norm, void* y,
+                                      void* r_out, void* h, void* cuda_stream);
+
+/* The same with the block's output y given.  y NULL: r' = res_scale * residual, w_post and gate must be NULL (the norm in
+ * front of a first block).  r_out may be NULL if h is wanted alone, or residual's buffer. */
+maxscore_status maxscore_block_norm(maxscore_ctx* ctx, const void* y, const void* residual, const maxscore_norm* norm,
+                                    void* r_out, void* h, void* cuda_stream);
+
+/* Backward of either call from the rows it returned.
+ *   dr_out [T, d_model] gradient of r_out, or NULL = zero; dh [T, d_model] gradient of h, NULL iff w_pre is
+ *   y, r_out as returned (y NULL as in the forward call; r_out may be NULL without w_pre)
+ *   dy [T, d_model] out (NULL iff y is); dr [T, d_model] out, gradient of residual (may be dr_out's buffer)
+ *   dw_post [d_model], dgate [gate rows, d_model], dw_pre [d_model]: fp32 out, each NULL iff its weight is.
+ * Column sums are formed in a fixed order: results repeat bit for bit.  Uses the context's workspace. */
+maxscore_status maxscore_block_norm_bwd(maxscore_ctx* ctx, const void* dr_out, const void* dh, const void* y, const void* r_out,
+                                        const maxscore_norm* norm, void* dy, void* dr, float* dw_post, float* dgate,
+                                        float* dw_pre, void* cuda_stream);
+
 /* ---- housekeeping (no counterpart in the paper) --------------------------------------------------- */
 
 /* Reads and clears the context's internal-error flag: *flag_out != 0 means that a bounded wait inside one of

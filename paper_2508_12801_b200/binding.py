@@ -41,6 +41,11 @@ class DeviceBuffers(C.Structure):
                                            "slot_idx", "gate_w", "slot_token", "expert_load", "stats", "xdisp")]
 
 
+class Norm(C.Structure):
+    _fields_ = [("w_post", C.c_void_p), ("gate", C.c_void_p), ("w_pre", C.c_void_p), ("rows_per_gate", C.c_int32),
+                ("eps", C.c_float), ("w_offset", C.c_float), ("res_scale", C.c_float)]
+
+
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmaxscore.so")
 EXPORTS = ["maxscore_capacity", "maxscore_workspace_bytes", "maxscore_create", "maxscore_destroy",
            "maxscore_last_cuda_error", "maxscore_route_fwd", "maxscore_dispatch", "maxscore_combine",
@@ -48,7 +53,9 @@ EXPORTS = ["maxscore_capacity", "maxscore_workspace_bytes", "maxscore_create", "
            "maxscore_assign", "maxscore_index_build", "maxscore_combine_bwd", "maxscore_gate_bwd",
            "maxscore_route_dispatch_host", "maxscore_index_build_noalloc", "maxscore_aux_loss",
            "maxscore_softtopk_bwd_aux", "maxscore_check_internal", "maxscore_launch_count",
-           "maxscore_test_raise_internal", "maxscore_assign_iterative", "maxscore_assign_top2_sinkhorn"]
+           "maxscore_test_raise_internal", "maxscore_assign_iterative", "maxscore_assign_top2_sinkhorn",
+           "maxscore_expert_gemm", "maxscore_expert_gemm_dw", "maxscore_expert_glu", "maxscore_expert_glu_bwd",
+           "maxscore_combine_norm", "maxscore_block_norm", "maxscore_block_norm_bwd"]
 
 
 def _load():
@@ -68,6 +75,14 @@ def _load():
 
 
 _lib = _load()
+_vp, _i32 = C.c_void_p, C.c_int32
+_lib.maxscore_expert_gemm.argtypes = [_vp] * 5 + [_i32] * 3 + [_vp]
+_lib.maxscore_expert_gemm_dw.argtypes = [_vp] * 5 + [_i32] * 4 + [_vp]
+_lib.maxscore_expert_glu.argtypes = [_vp] * 6 + [_i32] * 3 + [_vp]
+_lib.maxscore_expert_glu_bwd.argtypes = [_vp] * 6 + [_i32] * 3 + [_vp]
+_lib.maxscore_combine_norm.argtypes = [_vp] * 11
+_lib.maxscore_block_norm.argtypes = [_vp] * 7
+_lib.maxscore_block_norm_bwd.argtypes = [_vp] * 12
 
 
 class MaxScoreError(RuntimeError):
@@ -121,12 +136,14 @@ class Context:
         self.params = params
         nbytes = workspace_bytes(params)
         self.device = torch.device(device)
+        self.io_torch = torch.bfloat16 if params.io_dtype == BF16 else torch.float32
         with torch.cuda.device(self.device):
             self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
             base = (self.workspace.data_ptr() + 255) // 256 * 256
             self.handle = C.c_void_p()
             _check(_lib.maxscore_create(C.byref(self.handle), C.byref(params), C.c_void_p(base), C.c_size_t(nbytes)),
                    "maxscore_create")
+            self.device_index = torch.cuda.current_device()
         self.capacity = capacity(params)
 
     def close(self):
@@ -232,6 +249,118 @@ def combine_bwd(ctx, dY, yexp, expert_idx, slot_idx, gate_w, slot_token, dyexp, 
 def gate_bwd(ctx, hidden, w_gate, dlogits, dw_gate, dH, stream=None):
     _check(_lib.maxscore_gate_bwd(ctx.handle, _ptr(hidden), _ptr(w_gate), _ptr(dlogits), _ptr(dw_gate), _ptr(dH),
                                   _stream(stream)), "maxscore_gate_bwd")
+
+
+# ---- the experts between dispatch and combine, and the norms around them --------------------------------
+def _need(ctx, name, t, dtype, numel, optional=False):
+    """The tensor's address, after checks of what the C entry cannot see: type, size, device, contiguity."""
+    if t is None:
+        if optional:
+            return None
+        raise ValueError(f"{name}: a tensor is needed")
+    if t.dtype is not dtype or t.numel() != numel or not t.is_contiguous() or t.get_device() != ctx.device_index:
+        raise ValueError(f"{name}: a contiguous {dtype} tensor of {numel} elements on {ctx.device} is needed, got "
+                         f"{tuple(t.shape)} {t.dtype} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
+    return t.data_ptr()
+
+
+def _call(ctx, where, fn, *args, stream=None):
+    """One C call on the context's device: on `stream`, or on that device's current stream."""
+    if torch.cuda.current_device() != ctx.device_index:
+        with torch.cuda.device(ctx.device_index):
+            return _call(ctx, where, fn, *args, stream=stream)
+    if stream is None:
+        stream = torch.cuda.current_stream(ctx.device_index)
+    status = fn(ctx.handle, *args, stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
+    if status:
+        _check(status, where)
+
+
+def expert_gemm(ctx, x, w, expert_load, y, d_in, d_out, w_layout=0, stream=None):
+    """y[e, s] = x[e, s] W_e for the rows in use, zero rows behind them; with d_in and d_out exchanged and the other
+    w_layout, the gradient with respect to x."""
+    io, rows = ctx.io_torch, ctx.params.E * ctx.capacity
+    _call(ctx, "maxscore_expert_gemm", _lib.maxscore_expert_gemm, _need(ctx, "x", x, io, rows * d_in),
+          _need(ctx, "w", w, io, ctx.params.E * d_in * d_out), _need(ctx, "expert_load", expert_load, torch.int32, ctx.params.E),
+          _need(ctx, "y", y, io, rows * d_out), d_in, d_out, w_layout, stream=stream)
+
+
+def expert_gemm_dw(ctx, x, dy, expert_load, dw, d_in, d_out, w_layout=0, accumulate=0, stream=None):
+    """dw_e = x_e^T dy_e over the rows in use, fp32, in the weights' layout."""
+    io, rows = ctx.io_torch, ctx.params.E * ctx.capacity
+    _call(ctx, "maxscore_expert_gemm_dw", _lib.maxscore_expert_gemm_dw, _need(ctx, "x", x, io, rows * d_in),
+          _need(ctx, "dy", dy, io, rows * d_out), _need(ctx, "expert_load", expert_load, torch.int32, ctx.params.E),
+          _need(ctx, "dw", dw, torch.float32, ctx.params.E * d_in * d_out), d_in, d_out, w_layout, accumulate, stream=stream)
+
+
+def expert_glu(ctx, x, w_up, expert_load, pre, h, d_in, d_ff, w_layout=0, stream=None):
+    """[g | u] = x W_up, h = silu(g) u; pre (may be None) receives [g | u]."""
+    io, rows = ctx.io_torch, ctx.params.E * ctx.capacity
+    _call(ctx, "maxscore_expert_glu", _lib.maxscore_expert_glu, _need(ctx, "x", x, io, rows * d_in),
+          _need(ctx, "w_up", w_up, io, ctx.params.E * d_in * 2 * d_ff), _need(ctx, "expert_load", expert_load, torch.int32, ctx.params.E),
+          _need(ctx, "pre", pre, io, rows * 2 * d_ff, optional=True), _need(ctx, "h", h, io, rows * d_ff), d_in, d_ff, w_layout,
+          stream=stream)
+
+
+def expert_glu_bwd(ctx, dy, w_down, pre, expert_load, dpre, d_out, d_ff, w_layout=0, stream=None):
+    """dpre = gradient of [g | u] for y = (silu(g) u) W_down."""
+    io, rows = ctx.io_torch, ctx.params.E * ctx.capacity
+    _call(ctx, "maxscore_expert_glu_bwd", _lib.maxscore_expert_glu_bwd, _need(ctx, "dy", dy, io, rows * d_out),
+          _need(ctx, "w_down", w_down, io, ctx.params.E * d_ff * d_out), _need(ctx, "pre", pre, io, rows * 2 * d_ff),
+          _need(ctx, "expert_load", expert_load, torch.int32, ctx.params.E), _need(ctx, "dpre", dpre, io, rows * 2 * d_ff), d_out, d_ff,
+          w_layout, stream=stream)
+
+
+def make_norm(w_post=None, gate=None, w_pre=None, rows_per_gate=0, eps=1e-5, w_offset=0.0, res_scale=1.0) -> Norm:
+    """maxscore_norm from tensors; it keeps them alive and is checked against the context at each call."""
+    n = Norm(*(t.data_ptr() if t is not None else None for t in (w_post, gate, w_pre)), rows_per_gate, eps, w_offset, res_scale)
+    n.tensors = (w_post, gate, w_pre)
+    return n
+
+
+def _gate_rows(ctx, norm):
+    return -(-ctx.params.T // norm.rows_per_gate) if norm.rows_per_gate > 0 else 0
+
+
+def _norm(ctx, norm):
+    d, io = ctx.params.d_model, ctx.io_torch
+    w_post, gate, w_pre = norm.tensors
+    _need(ctx, "w_post", w_post, io, d, optional=True)
+    _need(ctx, "w_pre", w_pre, io, d, optional=True)
+    if gate is not None and norm.rows_per_gate > 0:       # the C entry refuses a gate without rows_per_gate
+        _need(ctx, "gate", gate, io, _gate_rows(ctx, norm) * d)
+    return C.byref(norm)
+
+
+def combine_norm(ctx, src, expert_idx, slot_idx, gate_w, residual, norm, y, r_out, h, stream=None):
+    """combine, after-norm, gate, scaled residual and before-norm in one pass; y and (without w_pre) h may be None."""
+    p, io = ctx.params, ctx.io_torch
+    Td, Tk = p.T * p.d_model, p.T * p.k
+    _call(ctx, "maxscore_combine_norm", _lib.maxscore_combine_norm, _need(ctx, "src", src, io, p.E * ctx.capacity * p.d_model),
+          _need(ctx, "expert_idx", expert_idx, torch.int32, Tk), _need(ctx, "slot_idx", slot_idx, torch.int32, Tk),
+          _need(ctx, "gate_w", gate_w, torch.float32, Tk, optional=True), _need(ctx, "residual", residual, io, Td), _norm(ctx, norm),
+          _need(ctx, "y", y, io, Td, optional=True), _need(ctx, "r_out", r_out, io, Td), _need(ctx, "h", h, io, Td, optional=True),
+          stream=stream)
+
+
+def block_norm(ctx, y, residual, norm, r_out, h, stream=None):
+    """after-norm, gate, scaled residual and before-norm of a block's output y (None in front of a first block)."""
+    io, Td = ctx.io_torch, ctx.params.T * ctx.params.d_model
+    _call(ctx, "maxscore_block_norm", _lib.maxscore_block_norm, _need(ctx, "y", y, io, Td, optional=True),
+          _need(ctx, "residual", residual, io, Td), _norm(ctx, norm), _need(ctx, "r_out", r_out, io, Td, optional=True),
+          _need(ctx, "h", h, io, Td, optional=True), stream=stream)
+
+
+def block_norm_bwd(ctx, dr_out, dh, y, r_out, norm, dy, dr, dw_post, dgate, dw_pre, stream=None):
+    """Gradients of block_norm / combine_norm from the rows they returned."""
+    d, io, f32 = ctx.params.d_model, ctx.io_torch, torch.float32
+    Td = ctx.params.T * d
+    _call(ctx, "maxscore_block_norm_bwd", _lib.maxscore_block_norm_bwd, _need(ctx, "dr_out", dr_out, io, Td, optional=True),
+          _need(ctx, "dh", dh, io, Td, optional=True), _need(ctx, "y", y, io, Td, optional=True),
+          _need(ctx, "r_out", r_out, io, Td, optional=True), _norm(ctx, norm), _need(ctx, "dy", dy, io, Td, optional=True),
+          _need(ctx, "dr", dr, io, Td), _need(ctx, "dw_post", dw_post, f32, d, optional=True),
+          _need(ctx, "dgate", dgate, f32, _gate_rows(ctx, norm) * d, optional=True), _need(ctx, "dw_pre", dw_pre, f32, d, optional=True),
+          stream=stream)
 
 
 def check_internal(ctx, stream=None) -> int:

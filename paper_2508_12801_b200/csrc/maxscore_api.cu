@@ -8,6 +8,8 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
+#include <initializer_list>
 #include <new>
 
 #include "common.cuh"
@@ -17,6 +19,8 @@
 #include "softtopk.cuh"
 #include "reroute.cuh"
 #include "alg1.cuh"
+#include "expert.cuh"
+#include "norm.cuh"
 
 using namespace msr;
 
@@ -52,11 +56,13 @@ int32_t capacity_of(const maxscore_params& p) {
 }
 
 struct Layout {          // byte offsets inside the workspace
-  size_t state, aux, cand, rec_val, rec_meta, rec_pos, rec_bxc, rec_ndv, rec_off, rec_cnt, rec_aarg, rr_choice, rr_rank, rr_cnt, rr_base, rr_held, rr_dropped, rr_bc, rr_blk, rr_dtok, rr_order, rr_dnum, a1_v, a1_partial, a1_ticket, cache_x, cache_id, cache_bound, cache_raw, block_counts, wt, error_flag, dls, wk, dwpart, total;
+  size_t state, aux, cand, rec_val, rec_meta, rec_pos, rec_bxc, rec_ndv, rec_off, rec_cnt, rec_aarg, rr_choice, rr_rank, rr_cnt, rr_base, rr_held, rr_dropped, rr_bc, rr_blk, rr_dtok, rr_order, rr_dnum, a1_v, a1_partial, a1_ticket, cache_x, cache_id, cache_bound, cache_raw, block_counts, wt, error_flag, dls, wk, dwpart, normpart, total;
   int Npad, n_idx_blocks;
   int rec_cap;                                // entries of the exact phase's candidate records
   int Kpad, dw_splits, dw_tokens_per_split;   // tensor-core backward GEMMs (bf16 I/O)
 };
+
+constexpr int kNormParts = 592;          // partial column sums of the norm backward, at most (units, and CTAs)
 
 Layout layout_of(const maxscore_params& p) {
   Layout l{};
@@ -119,6 +125,7 @@ Layout layout_of(const maxscore_params& p) {
   l.dls = off; off = align_up(off + (bf ? sizeof(__nv_bfloat16) * (size_t)p.T * 2 * l.Kpad : 0), 1024);
   l.wk = off; off = align_up(off + (bf ? sizeof(__nv_bfloat16) * (size_t)p.d_model * l.Kpad : 0), 1024);
   l.dwpart = off; off = align_up(off + (bf ? sizeof(float) * (size_t)l.dw_splits * p.d_model * p.E : 0), 1024);
+  l.normpart = off; off = align_up(off + sizeof(float) * 3 * (size_t)(p.T < kNormParts ? p.T : kNormParts) * p.d_model, 1024);
   l.total = off;
   return l;
 }
@@ -961,3 +968,230 @@ extern "C" maxscore_status maxscore_index_build_noalloc(int32_t T, int32_t E, in
   MS_LAUNCH_CHECK("index_fill_kernel");
   return MAXSCORE_OK;
 }
+
+// ==================================================================================================
+// Experts and norms
+namespace {
+
+maxscore_status check_expert(const maxscore_ctx* c, std::initializer_list<const void*> ptrs, int32_t w0, int32_t w1, int32_t w_layout) {
+  if (!c) return MAXSCORE_ERR_INVALID_ARG;
+  for (const void* p : ptrs) if (!p || !aligned16(p)) return MAXSCORE_ERR_INVALID_ARG;
+  if (w0 <= 0 || w1 <= 0 || (w_layout != 0 && w_layout != 1)) return MAXSCORE_ERR_INVALID_ARG;
+  const int m = c->p.io_dtype == MAXSCORE_BF16 ? 8 : 4;
+  if (w0 % m || w1 % m || w0 > (1 << 24) || w1 > (1 << 24)) return MAXSCORE_ERR_UNSUPPORTED;
+  return MAXSCORE_OK;
+}
+
+template <typename T, int EPI, bool A_MN, bool B_MN>
+maxscore_status launch_fma(maxscore_ctx* c, const void* A, const void* B, const void* pre_in, void* out, void* pre_out,
+                           const ExpertArgs& a, cudaStream_t st) {
+  // 128 x 128 tiles once the batch could fill the SMs with them, 64 x 64 below
+  const long long rows = (long long)c->p.T * c->p.k;
+  const long long big = EPI == kEpiDw ? (long long)a.E * ((a.M + 127) / 128) * ((a.N + 127) / 128)
+                                      : (rows + 127) / 128 * ((a.N * (EPI == kEpiGlu ? 2 : 1) + 127) / 128);
+  if (big >= 2 * c->sm_count)
+    expert_fma_kernel<T, 128, 128, EPI, A_MN, B_MN><<<c->sm_count * 2, 256, 0, st>>>((const T*)A, (const T*)B, (const T*)pre_in, out, (T*)pre_out, a);
+  else
+    expert_fma_kernel<T, 64, 64, EPI, A_MN, B_MN><<<c->sm_count * 4, 256, 0, st>>>((const T*)A, (const T*)B, (const T*)pre_in, out, (T*)pre_out, a);
+  MS_LAUNCH_CHECK("expert_fma_kernel");
+  c->launches += 1;
+  return MAXSCORE_OK;
+}
+
+// b_mn: the weights' columns run along the product's N side in memory
+template <int EPI>
+maxscore_status launch_expert(maxscore_ctx* c, const void* A, const void* B, const void* pre_in, void* out, void* pre_out,
+                              const ExpertArgs& a, bool b_mn, cudaStream_t st) {
+  if (c->p.io_dtype == MAXSCORE_BF16) {
+    if constexpr (EPI == kEpiDw) return launch_fma<__nv_bfloat16, EPI, true, true>(c, A, B, pre_in, out, pre_out, a, st);
+    else return b_mn ? launch_fma<__nv_bfloat16, EPI, false, true>(c, A, B, pre_in, out, pre_out, a, st)
+                     : launch_fma<__nv_bfloat16, EPI, false, false>(c, A, B, pre_in, out, pre_out, a, st);
+  }
+  if constexpr (EPI == kEpiDw) return launch_fma<float, EPI, true, true>(c, A, B, pre_in, out, pre_out, a, st);
+  else return b_mn ? launch_fma<float, EPI, false, true>(c, A, B, pre_in, out, pre_out, a, st)
+                   : launch_fma<float, EPI, false, false>(c, A, B, pre_in, out, pre_out, a, st);
+}
+
+ExpertArgs expert_args(const maxscore_ctx* c, const int32_t* load, int M, int N, int K, int accumulate = 0) {
+  ExpertArgs a{};
+  a.load = load; a.E = c->p.E; a.C = c->C; a.M = M; a.N = N; a.K = K; a.accumulate = accumulate;
+  return a;
+}
+
+// `y`: whether the call has a block output
+maxscore_status check_norm(const maxscore_ctx* c, const maxscore_norm* n, bool y) {
+  if (!c || !n) return MAXSCORE_ERR_INVALID_ARG;
+  if (!aligned16(n->w_post) || !aligned16(n->gate) || !aligned16(n->w_pre)) return MAXSCORE_ERR_INVALID_ARG;
+  if (!(n->eps > 0.f) || !isfinite(n->eps) || !isfinite(n->w_offset) || !isfinite(n->res_scale)) return MAXSCORE_ERR_INVALID_ARG;
+  if (n->gate && n->rows_per_gate <= 0) return MAXSCORE_ERR_INVALID_ARG;
+  if (!y && (n->w_post || n->gate)) return MAXSCORE_ERR_INVALID_ARG;
+  if ((size_t)c->p.d_model * elem_bytes(c) > 32768) return MAXSCORE_ERR_UNSUPPORTED;
+  return MAXSCORE_OK;
+}
+
+NormArgs norm_args(const maxscore_ctx* c, const maxscore_norm* n) {
+  NormArgs a{};
+  a.T = c->p.T; a.d = c->p.d_model; a.nvec = (int)(c->p.d_model * elem_bytes(c) / 16);
+  a.rows_per_gate = n->gate && n->rows_per_gate < c->p.T ? n->rows_per_gate : c->p.T;
+  a.eps = n->eps; a.w_offset = n->w_offset; a.res_scale = n->res_scale;
+  a.w_post = n->w_post; a.gate = n->gate; a.w_pre = n->w_pre;
+  return a;
+}
+
+// Threads of a row: one 16-byte vector each up to 64 vectors, two beyond.
+int norm_vecs(int nvec) { return nvec <= 64 ? 1 : 2; }
+int norm_threads(int nvec) { const int v = norm_vecs(nvec); return ((nvec + v - 1) / v + 31) / 32 * 32; }
+
+template <typename T, int SRC>
+maxscore_status launch_norm_fwd(maxscore_ctx* c, const void* y_in, const void* src, const int32_t* expert_idx, const int32_t* slot_idx,
+                                const float* gate_w, const void* residual, const maxscore_norm* n, void* y_out, void* r_out, void* h,
+                                cudaStream_t st) {
+  const maxscore_params& p = c->p;
+  const NormArgs a = norm_args(c, n);
+  const int G = norm_threads(a.nvec);
+  const int grid = std::min(p.T, c->sm_count * std::max(1, 2048 / G));
+  auto go = [&](auto kernel) {
+    kernel<<<grid, G, 0, st>>>((const T*)y_in, (const T*)src, expert_idx, slot_idx, gate_w, p.E, p.k, c->C, (const T*)residual,
+                               (T*)y_out, (T*)r_out, (T*)h, a);
+  };
+  if (norm_vecs(a.nvec) == 1) go(norm_fwd_kernel<T, 1, SRC, 64>);
+  else if (G <= 256) go(norm_fwd_kernel<T, 2, SRC, 256>);
+  else go(norm_fwd_kernel<T, 2, SRC, 1024>);
+  MS_LAUNCH_CHECK("norm_fwd_kernel");
+  c->launches += 1;
+  return MAXSCORE_OK;
+}
+
+template <typename T>
+maxscore_status launch_norm_bwd(maxscore_ctx* c, const void* dr_out, const void* dh, const void* y, const void* r_out,
+                                const maxscore_norm* n, void* dy, void* dr, float* dw_post, float* dgate, float* dw_pre,
+                                cudaStream_t st) {
+  const maxscore_params& p = c->p;
+  const NormArgs a = norm_args(c, n);
+  const int G = norm_threads(a.nvec);
+  const int parts = std::min(p.T, kNormParts);                       // rows of each partial matrix in the workspace
+  const int ctas = std::min(parts, c->sm_count * std::max(1, std::min(4, 512 / G)));
+  const int gate_rows = (p.T + a.rows_per_gate - 1) / a.rows_per_gate;
+  NormUnits u{};
+  u.per_gate = std::max(1, std::min(a.rows_per_gate, ctas / gate_rows));
+  u.rows = (a.rows_per_gate + u.per_gate - 1) / u.per_gate;
+  u.n_units = gate_rows * u.per_gate;                                // at most `ctas` whenever per_gate > 1
+  const int grid = std::min(u.n_units, ctas);
+  float* part = reinterpret_cast<float*>(c->ws + c->lay.normpart);
+  const size_t one = (size_t)parts * p.d_model;
+  float* pp = n->w_post ? part : nullptr;
+  float* pr = n->w_pre ? part + one : nullptr;
+  float* pg = !n->gate ? nullptr : u.per_gate > 1 ? part + 2 * one : dgate;
+  auto go = [&](auto kernel) {
+    kernel<<<grid, G, 0, st>>>((const T*)dr_out, (const T*)dh, (const T*)y, (const T*)r_out, (T*)dy, (T*)dr, pp, pr, pg, u, a);
+  };
+  if (norm_vecs(a.nvec) == 1) go(norm_bwd_kernel<T, 1, 64>);
+  else if (G <= 256) go(norm_bwd_kernel<T, 2, 256>);
+  else go(norm_bwd_kernel<T, 2, 1024>);
+  MS_LAUNCH_CHECK("norm_bwd_kernel");
+  c->launches += 1;
+  const bool reduce_gate = n->gate && u.per_gate > 1;
+  if (n->w_post || n->w_pre || reduce_gate) {
+    norm_reduce_kernel<<<dim3((p.d_model + 31) / 32, 2 + (reduce_gate ? gate_rows : 0)), 256, 0, st>>>(
+        pp, pr, pg, dw_post, dw_pre, dgate, grid, u.per_gate, p.d_model);
+    MS_LAUNCH_CHECK("norm_reduce_kernel");
+    c->launches += 1;
+  }
+  return MAXSCORE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+maxscore_status maxscore_expert_gemm(maxscore_ctx* c, const void* x, const void* w, const int32_t* expert_load, void* y,
+                                     int32_t d_in, int32_t d_out, int32_t w_layout, void* stream) {
+  maxscore_status s = check_expert(c, {x, w, y}, d_in, d_out, w_layout);
+  if (s) return s;
+  if (!expert_load || y == x || y == w) return MAXSCORE_ERR_INVALID_ARG;
+  return launch_expert<kEpiPlain>(c, x, w, nullptr, y, nullptr, expert_args(c, expert_load, 0, d_out, d_in), w_layout == 0,
+                                  (cudaStream_t)stream);
+}
+
+maxscore_status maxscore_expert_gemm_dw(maxscore_ctx* c, const void* x, const void* dy, const int32_t* expert_load, float* dw,
+                                        int32_t d_in, int32_t d_out, int32_t w_layout, int accumulate, void* stream) {
+  maxscore_status s = check_expert(c, {x, dy, dw}, d_in, d_out, w_layout);
+  if (s) return s;
+  if (!expert_load || (const void*)dw == x || (const void*)dw == dy) return MAXSCORE_ERR_INVALID_ARG;
+  // layout 1 is the transposed product: the two operands change places
+  const bool t = w_layout == 1;
+  return launch_expert<kEpiDw>(c, t ? dy : x, t ? x : dy, nullptr, dw, nullptr,
+                               expert_args(c, expert_load, t ? d_out : d_in, t ? d_in : d_out, 0, accumulate != 0), true,
+                               (cudaStream_t)stream);
+}
+
+maxscore_status maxscore_expert_glu(maxscore_ctx* c, const void* x, const void* w_up, const int32_t* expert_load, void* pre,
+                                    void* h, int32_t d_in, int32_t d_ff, int32_t w_layout, void* stream) {
+  maxscore_status s = check_expert(c, {x, w_up, h}, d_in, d_ff, w_layout);
+  if (s) return s;
+  if (!expert_load || !aligned16(pre) || h == x || h == w_up || pre == x || pre == w_up || pre == h) return MAXSCORE_ERR_INVALID_ARG;
+  return launch_expert<kEpiGlu>(c, x, w_up, nullptr, h, pre, expert_args(c, expert_load, 0, d_ff, d_in), w_layout == 0,
+                                (cudaStream_t)stream);
+}
+
+maxscore_status maxscore_expert_glu_bwd(maxscore_ctx* c, const void* dy, const void* w_down, const void* pre,
+                                        const int32_t* expert_load, void* dpre, int32_t d_out, int32_t d_ff, int32_t w_layout,
+                                        void* stream) {
+  maxscore_status s = check_expert(c, {dy, w_down, pre, dpre}, d_out, d_ff, w_layout);
+  if (s) return s;
+  if (!expert_load || dpre == dy || dpre == w_down || dpre == pre) return MAXSCORE_ERR_INVALID_ARG;
+  // dh = dy . W_down^T: the weight's d_ff side is the product's N side, contiguous in layout 1 ([E, d_out, d_ff])
+  return launch_expert<kEpiDact>(c, dy, w_down, pre, dpre, nullptr, expert_args(c, expert_load, 0, d_ff, d_out), w_layout == 1,
+                                 (cudaStream_t)stream);
+}
+
+maxscore_status maxscore_combine_norm(maxscore_ctx* c, const void* src, const int32_t* expert_idx, const int32_t* slot_idx,
+                                      const float* gate_w, const void* residual, const maxscore_norm* n, void* y, void* r_out,
+                                      void* h, void* stream) {
+  maxscore_status s = check_norm(c, n, true);
+  if (s) return s;
+  if (!src || !expert_idx || !slot_idx || !residual || !r_out || (h == nullptr) != (n->w_pre == nullptr)) return MAXSCORE_ERR_INVALID_ARG;
+  for (const void* p : {src, residual, (const void*)y, (const void*)r_out, (const void*)h})
+    if (!aligned16(p)) return MAXSCORE_ERR_INVALID_ARG;
+  if (y == r_out || y == residual || (h && (h == y || h == r_out || h == residual))) return MAXSCORE_ERR_INVALID_ARG;
+  if (c->p.io_dtype == MAXSCORE_BF16)
+    return launch_norm_fwd<__nv_bfloat16, 2>(c, nullptr, src, expert_idx, slot_idx, gate_w, residual, n, y, r_out, h, (cudaStream_t)stream);
+  return launch_norm_fwd<float, 2>(c, nullptr, src, expert_idx, slot_idx, gate_w, residual, n, y, r_out, h, (cudaStream_t)stream);
+}
+
+maxscore_status maxscore_block_norm(maxscore_ctx* c, const void* y, const void* residual, const maxscore_norm* n, void* r_out,
+                                    void* h, void* stream) {
+  maxscore_status s = check_norm(c, n, y != nullptr);
+  if (s) return s;
+  if (!residual || (!r_out && !h) || (h == nullptr) != (n->w_pre == nullptr)) return MAXSCORE_ERR_INVALID_ARG;
+  for (const void* p : {y, residual, (const void*)r_out, (const void*)h})
+    if (!aligned16(p)) return MAXSCORE_ERR_INVALID_ARG;
+  if ((r_out && r_out == y) || (h && (h == y || h == r_out || h == residual))) return MAXSCORE_ERR_INVALID_ARG;
+  const bool bf = c->p.io_dtype == MAXSCORE_BF16;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (y)
+    return bf ? launch_norm_fwd<__nv_bfloat16, 1>(c, y, nullptr, nullptr, nullptr, nullptr, residual, n, nullptr, r_out, h, st)
+              : launch_norm_fwd<float, 1>(c, y, nullptr, nullptr, nullptr, nullptr, residual, n, nullptr, r_out, h, st);
+  return bf ? launch_norm_fwd<__nv_bfloat16, 0>(c, nullptr, nullptr, nullptr, nullptr, nullptr, residual, n, nullptr, r_out, h, st)
+            : launch_norm_fwd<float, 0>(c, nullptr, nullptr, nullptr, nullptr, nullptr, residual, n, nullptr, r_out, h, st);
+}
+
+maxscore_status maxscore_block_norm_bwd(maxscore_ctx* c, const void* dr_out, const void* dh, const void* y, const void* r_out,
+                                        const maxscore_norm* n, void* dy, void* dr, float* dw_post, float* dgate, float* dw_pre,
+                                        void* stream) {
+  maxscore_status s = check_norm(c, n, y != nullptr);
+  if (s) return s;
+  if (!dr || (dy == nullptr) != (y == nullptr) || (dh == nullptr) != (n->w_pre == nullptr) || (n->w_pre && !r_out) ||
+      (dw_post == nullptr) != (n->w_post == nullptr) || (dgate == nullptr) != (n->gate == nullptr) ||
+      (dw_pre == nullptr) != (n->w_pre == nullptr))
+    return MAXSCORE_ERR_INVALID_ARG;
+  for (const void* p : {dr_out, dh, y, r_out, (const void*)dy, (const void*)dr, (const void*)dw_post, (const void*)dgate, (const void*)dw_pre})
+    if (!aligned16(p)) return MAXSCORE_ERR_INVALID_ARG;
+  for (const void* p : {dh, y, r_out}) if (p && (p == dr || p == dy)) return MAXSCORE_ERR_INVALID_ARG;
+  if (dy && (dy == dr || dy == dr_out)) return MAXSCORE_ERR_INVALID_ARG;
+  if (c->p.io_dtype == MAXSCORE_BF16)
+    return launch_norm_bwd<__nv_bfloat16>(c, dr_out, dh, y, r_out, n, dy, dr, dw_post, dgate, dw_pre, (cudaStream_t)stream);
+  return launch_norm_bwd<float>(c, dr_out, dh, y, r_out, n, dy, dr, dw_post, dgate, dw_pre, (cudaStream_t)stream);
+}
+
+}  // extern "C"
