@@ -1,0 +1,469 @@
+// Expert products on the tensor cores (bf16 I/O): persistent pairs of CTAs on 256 x 256 tiles.
+//
+// A pair (cluster of two, tcgen05 cta_group::2) owns 256 rows x 256 columns: each CTA stages its own 128 rows of A and 128
+// columns of B, the pair's MMA reads both halves, and each CTA's tensor memory ends up with its 128 rows of all 256 columns.
+// That halves the operand traffic per flop of a single CTA's 128 x 256 tile (64 bytes per clock and SM at full rate instead
+// of 96, which the L2 cannot deliver).  Two accumulators alternate, so the epilogue of a tile runs under the MMAs of the next.
+//   warp 0: TMA loads, six (five) stages of 64-deep slices;  warp 1: TMEM, and in the leading CTA the MMAs;
+//   warps 2-5: epilogue, one TMEM lane quarter each, out through swizzled staging boxes and TMA tile stores.
+// Both operand majors are read in place through the descriptors: no weight is ever transposed.
+//
+// Ragged loads.  Rows: a tile is whole or partial, rows behind the load come out as zeros.  Contraction over rows (dW): the
+// last slice goes up to the load only; the up to 15 rows between the load and the next multiple of the MMA depth are zeroed in
+// shared memory by the producer warp before the pair's MMA may read the slice.
+#pragma once
+#include "expert.cuh"
+
+namespace msr {
+
+// ---- cta_group::2 wrappers -----------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ uint32_t map_to_rank(uint32_t saddr, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+}
+__device__ __forceinline__ void mbar_expect_tx_cluster(uint32_t addr, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(addr), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t phase, uint32_t limit = 1u << 22) {
+  for (uint32_t it = 0; it < limit; ++it) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(smem_u32(bar)), "r"(phase) : "memory");
+    if (ok) return true;
+    if (it > 64) __nanosleep(32);
+  }
+  return false;
+}
+// loads into this CTA's shared memory that complete on a barrier of either CTA of the pair
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* tm, int x, int y, int z, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+               ::"r"(dst), "l"(tm), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm, int x, int y, int z, uint64_t* bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+               ::"r"(dst), "l"(tm), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* tm, int x, int y, int z, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(tm), "r"(src), "r"(x), "r"(y),
+               "r"(z) : "memory");
+}
+__device__ __forceinline__ void tma_add_3d(const CUtensorMap* tm, int x, int y, int z, uint32_t src) {
+  asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(tm), "r"(src),
+               "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void umma_bf16_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {     // arrives on the same barrier of both CTAs
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
+               "h"((uint16_t)3) : "memory");
+}
+
+// ---- the kernel ----------------------------------------------------------------------------------------------------
+constexpr int kXThreads = 192, kXTile = 256, kXBK = 64, kXStageBytes = 32768;
+__host__ __device__ constexpr int x_stages(int epi) { return epi == kEpiDact ? 5 : 6; }
+__host__ __device__ constexpr int x_out_bytes(int epi) { return epi == kEpiDact ? 65536 : 32768; }
+__host__ __device__ constexpr int x_smem(int epi) { return x_stages(epi) * kXStageBytes + x_out_bytes(epi) + 1024; }
+
+struct XSmem {
+  uint64_t full[6], empty[6], acc_full[2], acc_empty[2], tail, in[8];
+  uint32_t tmem;
+  int failed;
+  int rows[kMaxE], first[kMaxE + 1];     // rows in use; tiles before each expert
+};
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<uint32_t*>(&h);
+}
+
+struct XTile { int e, m, n, rows; };     // expert, tile row and column, rows of the expert in use
+
+// Walks the tiles t, t + step, ... (t only grows, so the expert is found by stepping on from the last one).
+template <int EPI>
+struct XWalk {
+  const XSmem& sm; const ExpertArgs& a; int ntn; int t, step, e;
+  __device__ XWalk(const XSmem& s, const ExpertArgs& args, int ntn_, int t0, int step_) : sm(s), a(args), ntn(ntn_), t(t0), step(step_), e(0) {}
+  __device__ bool next(XTile& x) {
+    if (t >= sm.first[a.E]) return false;
+    while (t >= sm.first[e + 1]) ++e;
+    const int l = t - sm.first[e];
+    x.e = e; x.m = l / ntn; x.n = l - x.m * ntn; x.rows = sm.rows[e];
+    t += step;
+    return true;
+  }
+};
+
+// Rows in use and tile counts of every expert, by the first warp; `per` = tiles of an expert with rows r.
+template <typename F>
+__device__ __forceinline__ void expert_prefix(const ExpertArgs& a, int* rows, int* first, F per) {
+  const int lane = threadIdx.x & 31;
+  int mine[kMaxE / 32], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kMaxE / 32; ++i) {
+    const int e = lane * (kMaxE / 32) + i;
+    const int r = e < a.E ? expert_rows(a, e) : 0;
+    if (e < a.E) rows[e] = r;
+    mine[i] = e < a.E ? per(r) : 0;
+    sum += mine[i];
+  }
+  int incl = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += v;
+  }
+  int run = incl - sum;
+#pragma unroll
+  for (int i = 0; i < kMaxE / 32; ++i) {
+    const int e = lane * (kMaxE / 32) + i;
+    if (e <= a.E) first[e] = run;
+    run += mine[i];
+  }
+  if (lane == 31 && a.E == kMaxE) first[kMaxE] = run;
+}
+
+// EPI as in expert.cuh.  B_MN: B is stored with its columns contiguous.  dW: both operands run along the rows.
+// Maps: tA; tB0 / tB1 = B of the leading / the other CTA (gate and up columns in the gated form, else the same);
+// tO0 = output (gated: h; backward: dg), tO1 / tO2 = g / u kept (gated), du (backward, tO1); tP0 / tP1 = g / u read (backward).
+template <int EPI, bool B_MN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kXThreads)
+expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUtensorMap tB0, const __grid_constant__ CUtensorMap tB1,
+                 const __grid_constant__ CUtensorMap tO0, const __grid_constant__ CUtensorMap tO1, const __grid_constant__ CUtensorMap tO2,
+                 const __grid_constant__ CUtensorMap tP0, const __grid_constant__ CUtensorMap tP1, char* out, char* pre_out,
+                 ExpertArgs a, unsigned* error_flag) {
+  constexpr bool kDw = EPI == kEpiDw, kA_MN = kDw;
+  constexpr int kStages = x_stages(EPI);
+  constexpr int kTileN = EPI == kEpiGlu ? 128 : kXTile;               // output columns of a tile
+  extern __shared__ unsigned char xsm_raw[];
+  unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(xsm_raw) + 1023) & ~(uintptr_t)1023);
+  __shared__ XSmem sm;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)cluster_rank();
+  const int ntn = (a.N + kTileN - 1) / kTileN, ntm_dw = (a.M + kXTile - 1) / kXTile;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) { mbar_init(&sm.full[s], 2); mbar_init(&sm.empty[s], 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(&sm.acc_full[b], 1); mbar_init(&sm.acc_empty[b], 8); }
+    mbar_init(&sm.tail, 1);
+    for (int i = 0; i < 8; ++i) mbar_init(&sm.in[i], 1);
+    sm.failed = 0;
+    fence_barrier_init();
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm.tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  if (warp == 2)
+    expert_prefix(a, sm.rows, sm.first, [&](int r) { return kDw ? ntm_dw * ntn : (r + kXTile - 1) / kXTile * ntn; });
+  tc_fence_before();
+  __syncwarp();
+  cluster_sync();                                       // barriers of both CTAs are ready, shared memory written above is seen
+  tc_fence_after();
+  const uint32_t tmem = sm.tmem;
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+
+  if (warp == 0) {
+    // ---- producer ----------------------------------------------------------------------------------------------
+    XWalk<EPI> walk(sm, a, ntn, pair, pairs);
+    XTile x;
+    int it = 0; uint32_t tail_phase = 0; bool ok = true;
+    const uint32_t full0 = map_to_rank(smem_u32(&sm.full[0]), 0);
+    const CUtensorMap* tB = rank ? &tB1 : &tB0;
+    while (ok && walk.next(x)) {
+      const int K = kDw ? x.rows : a.K;
+      const int nkb = (K + kXBK - 1) / kXBK;
+      const int ax = x.m * kXTile + 128 * rank;
+      const int bx = EPI == kEpiGlu ? x.n * 128 : x.n * kXTile + 128 * rank;
+      for (int kb = 0; kb < nkb && ok; ++kb, ++it) {
+        const int s = it % kStages;
+        const uint32_t ph = (uint32_t)((it / kStages) & 1);
+        const uint32_t sa = smem_u32(base) + (uint32_t)(s * kXStageBytes), sb = sa + 16384;
+        const uint32_t full = full0 + 8u * (uint32_t)s;
+        const int k0 = kb * kXBK;
+        const bool masked = kDw && kb == nkb - 1 && (K & 15);          // the load ends inside an MMA's depth
+        int good = 1;
+        if (lane == 0) {
+          if (it >= kStages) good = mbar_wait_bounded(&sm.empty[s], ph ^ 1);
+          if (good) {
+            if (!masked) mbar_expect_tx_cluster(full, kXStageBytes);
+            else mbar_expect_tx(&sm.tail, kXStageBytes);
+            auto put = [&](uint32_t dst, const CUtensorMap* tm, int xx, int yy) {
+              if (masked) tma_load_3d(dst, tm, xx, yy, x.e, &sm.tail);
+              else tma_load_3d_pair(dst, tm, xx, yy, x.e, full);
+            };
+            if (kA_MN) { put(sa, &tA, ax, k0); put(sa + 8192, &tA, ax + 64, k0); }
+            else put(sa, &tA, k0, ax);
+            if (B_MN) { put(sb, tB, bx, k0); put(sb + 8192, tB, bx + 64, k0); }
+            else put(sb, tB, k0, bx);
+          }
+        }
+        if (kDw && masked) {
+          // this CTA's copies land on its own barrier; rows from the load to the next multiple of 16 become zero
+          good = __shfl_sync(0xffffffffu, good, 0);
+          if (good) good = mbar_wait_bounded(&sm.tail, tail_phase);
+          good = __all_sync(0xffffffffu, good);
+          tail_phase ^= 1;
+          if (good) {
+            const int r0 = K - k0, r1 = (r0 + 15) & ~15;               // a row is 128 bytes of a box, whatever the swizzle
+            unsigned char* st = base + (size_t)s * kXStageBytes;
+            const int per_box = (r1 - r0) * 8;
+            for (int i = lane; i < 4 * per_box; i += 32)
+              *reinterpret_cast<uint4*>(st + (i / per_box) * 8192 + r0 * 128 + (i % per_box) * 16) = make_uint4(0, 0, 0, 0);
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(full);
+          }
+        }
+        ok = __shfl_sync(0xffffffffu, good, 0) != 0;
+      }
+    }
+    if (!ok && lane == 0) sm.failed = 1;
+  } else if (warp == 1 && rank == 0 && lane == 0) {
+    // ---- MMA issuer of the pair --------------------------------------------------------------------------------------
+    const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (kA_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
+                           ((uint32_t)(kXTile >> 3) << 17) | ((uint32_t)(kXTile >> 4) << 24);
+    XWalk<EPI> walk(sm, a, ntn, pair, pairs);
+    XTile x;
+    int it = 0, tile = 0; bool ok = true;
+    while (ok && walk.next(x)) {
+      const int K = kDw ? x.rows : a.K;
+      const int nkb = (K + kXBK - 1) / kXBK;
+      if (nkb == 0) continue;
+      const int buf = tile & 1;
+      if (tile >= 2) ok = mbar_wait_cluster(&sm.acc_empty[buf], (uint32_t)(((tile >> 1) & 1) ^ 1));
+      const uint32_t acc = tmem + (uint32_t)(buf * 256);
+      for (int kb = 0; kb < nkb && ok; ++kb, ++it) {
+        const int s = it % kStages;
+        ok = mbar_wait_cluster(&sm.full[s], (uint32_t)((it / kStages) & 1));
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t sa = smem_u32(base) + (uint32_t)(s * kXStageBytes), sb = sa + 16384;
+        const int steps = kb == nkb - 1 ? (K - kb * kXBK + 15) / 16 : 4;
+        for (int kk = 0; kk < steps; ++kk) {
+          // 16 deep: 32 bytes along a K-major row, 16 rows of 128 bytes in the other major
+          const uint64_t ad = kA_MN ? smem_desc_mn128(sa + kk * 2048u, 8192u) : smem_desc_k128(sa) + 2 * kk;
+          const uint64_t bd = B_MN ? smem_desc_mn128(sb + kk * 2048u, 8192u) : smem_desc_k128(sb) + 2 * kk;
+          umma_bf16_pair(acc, ad, bd, idesc, (kb > 0 || kk > 0) ? 1u : 0u);
+        }
+        umma_commit_pair(&sm.empty[s]);
+      }
+      umma_commit_pair(&sm.acc_full[buf]);
+      ++tile;
+    }
+    if (!ok) sm.failed = 1;
+  } else if (warp >= 2) {
+    // ---- epilogue ------------------------------------------------------------------------------------------------------
+    const int q = warp & 3;                             // TMEM lanes this warp may read
+    if constexpr (!kDw) {
+      const int worker = blockIdx.x * 128 + (warp - 2) * 32 + lane, workers = gridDim.x * 128;
+      expert_zero_behind(a, sm.rows, out, 2 * (size_t)(EPI == kEpiDact ? 2 * a.N : a.N), kXTile, worker, workers);
+      if (EPI == kEpiGlu && pre_out) expert_zero_behind(a, sm.rows, pre_out, 4 * (size_t)a.N, kXTile, worker, workers);
+    }
+    unsigned char* stage = base + kStages * kXStageBytes + (size_t)q * (x_out_bytes(EPI) / 4);
+    const uint32_t acc_empty0 = map_to_rank(smem_u32(&sm.acc_empty[0]), 0);
+    const uint32_t lanes = (uint32_t)(q * 32) << 16;
+    XWalk<EPI> walk(sm, a, ntn, pair, pairs);
+    XTile x;
+    int tile = 0, box = 0, in_count = 0; bool ok = true;
+    // a 32-row x 128-byte box in the 128-byte swizzle, out through one TMA store; two boxes alternate
+    auto begin_box = [&]() -> unsigned char* {
+      if (lane == 0 && box >= 2) bulk_wait_read<1>();
+      __syncwarp();
+      return stage + (box & 1) * 4096;
+    };
+    auto end_box = [&](const CUtensorMap* tm, int xx, int yy, int zz, bool in, bool add = false) {
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) {
+        const uint32_t src = smem_u32(stage + (box & 1) * 4096);
+        if (in) { if (add) tma_add_3d(tm, xx, yy, zz, src); else tma_store_3d(tm, xx, yy, zz, src); }
+        bulk_commit();
+      }
+      ++box;
+    };
+    while (ok && walk.next(x)) {
+      const int nkb = ((kDw ? x.rows : a.K) + kXBK - 1) / kXBK;
+      const int buf = tile & 1;
+      const int y0 = x.m * kXTile + 128 * rank + 32 * q;              // first row of this warp
+      const uint32_t acc = tmem + lanes + (uint32_t)(buf * 256);
+      if (nkb > 0) {
+        ok = mbar_wait_cluster(&sm.acc_full[buf], (uint32_t)((tile >> 1) & 1));
+        if (!ok) break;
+        tc_fence_after();
+      }
+      if constexpr (kDw) {
+        for (int c0 = 0; c0 < kXTile; c0 += 32) {
+          uint32_t u[2][16];
+          if (nkb > 0) {
+            tmem_ld16_issue(acc + c0, u[0]); tmem_ld16_issue(acc + c0 + 16, u[1]);
+            tmem_ld_wait();
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) u[0][i] = u[1][i] = 0;
+          }
+          unsigned char* row = begin_box() + lane * 128;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            *reinterpret_cast<uint4*>(row + ((i ^ (lane & 7)) << 4)) =
+                make_uint4(u[i >> 2][(i & 3) * 4], u[i >> 2][(i & 3) * 4 + 1], u[i >> 2][(i & 3) * 4 + 2], u[i >> 2][(i & 3) * 4 + 3]);
+          const int xx = x.n * kXTile + c0;
+          end_box(&tO0, xx, y0, x.e, xx < a.N && y0 < a.M && (nkb > 0 || !a.accumulate), a.accumulate);
+        }
+      } else {
+        const bool keep_row = y0 + lane < x.rows;                      // rows behind the load come out as zeros
+        const bool in_y = y0 < a.C;
+        if constexpr (EPI == kEpiPlain) {
+          for (int c0 = 0; c0 < kXTile; c0 += 64) {
+            uint32_t u[4][16];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tmem_ld16_issue(acc + c0 + 16 * i, u[i]);
+            tmem_ld_wait();
+            unsigned char* row = begin_box() + lane * 128;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              uint32_t w[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const int at = (i & 1) * 8 + 2 * j;
+                w[j] = keep_row ? pack_bf16(__uint_as_float(u[i >> 1][at]), __uint_as_float(u[i >> 1][at + 1])) : 0u;
+              }
+              *reinterpret_cast<uint4*>(row + ((i ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            const int xx = x.n * kXTile + c0;
+            end_box(&tO0, xx, y0, x.e, in_y && xx < a.N);
+          }
+        } else if constexpr (EPI == kEpiGlu) {
+          for (int c0 = 0; c0 < 128; c0 += 64) {
+            const int xx = x.n * 128 + c0;
+            uint32_t hw[32], gw[32], uw[32];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              uint32_t g[2][16], u[2][16];
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                tmem_ld16_issue(acc + c0 + half * 32 + 16 * i, g[i]);
+                tmem_ld16_issue(acc + 128 + c0 + half * 32 + 16 * i, u[i]);
+              }
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const float g0 = __uint_as_float(g[i >> 3][(i & 7) * 2]), g1 = __uint_as_float(g[i >> 3][(i & 7) * 2 + 1]);
+                const float u0 = __uint_as_float(u[i >> 3][(i & 7) * 2]), u1 = __uint_as_float(u[i >> 3][(i & 7) * 2 + 1]);
+                hw[half * 16 + i] = keep_row ? pack_bf16(silu_mul<true>(g0, u0), silu_mul<true>(g1, u1)) : 0u;
+                gw[half * 16 + i] = keep_row ? pack_bf16(g0, g1) : 0u;
+                uw[half * 16 + i] = keep_row ? pack_bf16(u0, u1) : 0u;
+              }
+            }
+            auto emit = [&](const CUtensorMap* tm, const uint32_t (&w)[32]) {
+              unsigned char* row = begin_box() + lane * 128;
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                *reinterpret_cast<uint4*>(row + ((i ^ (lane & 7)) << 4)) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+              end_box(tm, xx, y0, x.e, in_y && xx < a.N);
+            };
+            emit(&tO0, hw);
+            if (pre_out) { emit(&tO1, gw); emit(&tO2, uw); }
+          }
+        } else {
+          // dh in the accumulator; g and u come in through two 8 KB pairs of boxes, which dg and du then leave from
+          auto fetch = [&](int c, int slot) {
+            const int xx = x.n * kXTile + c * 64;
+            if (lane == 0) {
+              const uint32_t d = smem_u32(stage + slot * 8192);
+              uint64_t* bar = &sm.in[q * 2 + slot];
+              mbar_expect_tx(bar, 8192);
+              tma_load_3d(d, &tP0, xx, y0, x.e, bar);
+              tma_load_3d(d + 4096, &tP1, xx, y0, x.e, bar);
+            }
+          };
+          if (lane == 0) bulk_wait_read<0>();                          // the last tile's boxes have been read by their stores
+          __syncwarp();
+          fetch(0, 0);
+          for (int c = 0; c < 4 && ok; ++c) {
+            const int slot = c & 1;
+            if (c < 3) {
+              if (c >= 1) { if (lane == 0) bulk_wait_read<0>(); __syncwarp(); }
+              fetch(c + 1, slot ^ 1);
+            }
+            ok = mbar_wait_bounded(&sm.in[q * 2 + slot], (uint32_t)(in_count >> 1 & 1));
+            ++in_count;
+            if (!ok) break;
+            unsigned char* row = stage + slot * 8192 + lane * 128;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              uint32_t u[2][16];
+              tmem_ld16_issue(acc + c * 64 + half * 32, u[0]); tmem_ld16_issue(acc + c * 64 + half * 32 + 16, u[1]);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                uint4* pg = reinterpret_cast<uint4*>(row + (((half * 4 + i) ^ (lane & 7)) << 4));
+                uint4* pu = reinterpret_cast<uint4*>(row + 4096 + (((half * 4 + i) ^ (lane & 7)) << 4));
+                float g[8], up[8];
+                Vec16<__nv_bfloat16>::unpack(*pg, g); Vec16<__nv_bfloat16>::unpack(*pu, up);
+                uint32_t wg[4], wu[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  float d0, d1, e0, e1;
+                  const int at = (i & 1) * 8 + 2 * j;
+                  dact<true>(__uint_as_float(u[i >> 1][at]), g[2 * j], up[2 * j], d0, e0);
+                  dact<true>(__uint_as_float(u[i >> 1][at + 1]), g[2 * j + 1], up[2 * j + 1], d1, e1);
+                  wg[j] = keep_row ? pack_bf16(d0, d1) : 0u;
+                  wu[j] = keep_row ? pack_bf16(e0, e1) : 0u;
+                }
+                *pg = make_uint4(wg[0], wg[1], wg[2], wg[3]);
+                *pu = make_uint4(wu[0], wu[1], wu[2], wu[3]);
+              }
+            }
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) {
+              const int xx = x.n * kXTile + c * 64;
+              if (in_y && xx < a.N) {
+                const uint32_t src = smem_u32(stage + slot * 8192);
+                tma_store_3d(&tO0, xx, y0, x.e, src);
+                tma_store_3d(&tO1, xx, y0, x.e, src + 4096);
+              }
+              bulk_commit();
+            }
+          }
+        }
+      }
+      if (nkb > 0) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(acc_empty0 + 8u * (uint32_t)buf);
+        ++tile;
+      }
+    }
+    if (lane == 0) bulk_wait_all<0>();
+    if (!ok && lane == 0) sm.failed = 1;
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && sm.failed) {
+    atomicOr(error_flag, 4u);
+    for (int i = 0; i < 1000; ++i) __nanosleep(1000);   // a wait gave up: let the copies that were in flight land
+  }
+  __syncwarp();
+  cluster_sync();                                       // neither CTA leaves while the other may still reach its barriers
+  tc_fence_after();
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+}  // namespace msr

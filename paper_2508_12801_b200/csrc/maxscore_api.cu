@@ -20,6 +20,7 @@
 #include "reroute.cuh"
 #include "alg1.cuh"
 #include "expert.cuh"
+#include "expert_tc.cuh"
 #include "norm.cuh"
 
 using namespace msr;
@@ -203,6 +204,24 @@ maxscore_status make_tmap_bf16(const maxscore_ctx* c, CUtensorMap* tm, const voi
   CUresult r = c->encode(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    snprintf(g_last_error, sizeof(g_last_error), "cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
+    return MAXSCORE_ERR_CUDA;
+  }
+  return MAXSCORE_OK;
+}
+
+// One matrix per expert: [E][rows][inner] with given strides, boxes of one expert each, 128-byte swizzle.
+maxscore_status make_tmap_expert(const maxscore_ctx* c, CUtensorMap* tm, bool f32, const void* base, uint64_t inner, uint64_t rows,
+                                 uint64_t row_stride, uint64_t expert_stride, uint32_t box_rows) {
+  const uint64_t b = f32 ? 4 : 2;
+  cuuint64_t dims[3] = {inner, rows, (cuuint64_t)c->p.E};
+  cuuint64_t strides[2] = {row_stride * b, expert_stride * b};
+  cuuint32_t box[3] = {(cuuint32_t)(128 / b), box_rows, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = c->encode(tm, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims,
+                         strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                         CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
     snprintf(g_last_error, sizeof(g_last_error), "cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
     return MAXSCORE_ERR_CUDA;
@@ -480,6 +499,13 @@ maxscore_status maxscore_create(maxscore_ctx** out, const maxscore_params* param
   MS_CUDA(cudaFuncSetAttribute(gate_bwd_dh_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDhSmemMax));
   MS_CUDA(cudaFuncSetAttribute(gate_bwd_dw_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDwSmemMax));
   MS_CUDA(cudaFuncSetAttribute(dispatch_tma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kTmaWarps * kTmaStages * kTmaChunk));
+  MS_CUDA(cudaFuncSetAttribute(expert_tc_kernel<kEpiPlain, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, x_smem(kEpiPlain)));
+  MS_CUDA(cudaFuncSetAttribute(expert_tc_kernel<kEpiPlain, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, x_smem(kEpiPlain)));
+  MS_CUDA(cudaFuncSetAttribute(expert_tc_kernel<kEpiGlu, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, x_smem(kEpiGlu)));
+  MS_CUDA(cudaFuncSetAttribute(expert_tc_kernel<kEpiGlu, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, x_smem(kEpiGlu)));
+  MS_CUDA(cudaFuncSetAttribute(expert_tc_kernel<kEpiDact, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, x_smem(kEpiDact)));
+  MS_CUDA(cudaFuncSetAttribute(expert_tc_kernel<kEpiDact, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, x_smem(kEpiDact)));
+  MS_CUDA(cudaFuncSetAttribute(expert_tc_kernel<kEpiDw, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, x_smem(kEpiDw)));
   int coop = 0, sweep_occ = 0;
   MS_CUDA(cudaDeviceGetAttribute(&coop, cudaDevAttrCooperativeLaunch, dev));
   MS_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&sweep_occ, flow_sweeps_kernel, kSwThreads, 0));
@@ -998,14 +1024,64 @@ maxscore_status launch_fma(maxscore_ctx* c, const void* A, const void* B, const 
   return MAXSCORE_OK;
 }
 
-// b_mn: the weights' columns run along the product's N side in memory
+template <int EPI, bool B_MN>
+maxscore_status launch_tc(maxscore_ctx* c, const void* A, const void* B, const void* pre_in, void* out, void* pre_out,
+                          const ExpertArgs& a, cudaStream_t st) {
+  constexpr bool kDw = EPI == kEpiDw;
+  const uint64_t C = (uint64_t)c->C, M = (uint64_t)a.M, N = (uint64_t)a.N, K = (uint64_t)a.K;
+  typedef const __nv_bfloat16* P;
+  CUtensorMap tA, tB0, tB1, tO0, tO1, tO2, tP0, tP1;
+  maxscore_status s;
+#define MS_MAP(...) do { s = make_tmap_expert(c, __VA_ARGS__); if (s) return s; } while (0)
+  if (kDw) {
+    MS_MAP(&tA, false, A, M, C, M, C * M, 64);
+    MS_MAP(&tB0, false, B, N, C, N, C * N, 64);
+    tB1 = tB0;
+    MS_MAP(&tO0, true, out, N, M, N, M * N, 32);
+  } else {
+    MS_MAP(&tA, false, A, K, C, K, C * K, 128);
+    const uint64_t cols = EPI == kEpiGlu ? 2 * N : N;
+    if (B_MN) MS_MAP(&tB0, false, B, N, K, cols, K * cols, 64);
+    else MS_MAP(&tB0, false, B, K, N, K, cols * K, 128);
+    tB1 = tB0;
+    if (EPI == kEpiGlu) {
+      if (B_MN) MS_MAP(&tB1, false, (P)B + N, N, K, cols, K * cols, 64);
+      else MS_MAP(&tB1, false, (P)B + N * K, K, N, K, cols * K, 128);
+    }
+    if (EPI == kEpiDact) {
+      MS_MAP(&tO0, false, out, N, C, 2 * N, C * 2 * N, 32);
+      MS_MAP(&tO1, false, (P)out + N, N, C, 2 * N, C * 2 * N, 32);
+      MS_MAP(&tP0, false, pre_in, N, C, 2 * N, C * 2 * N, 32);
+      MS_MAP(&tP1, false, (P)pre_in + N, N, C, 2 * N, C * 2 * N, 32);
+    } else {
+      MS_MAP(&tO0, false, out, N, C, N, C * N, 32);
+    }
+    if (EPI == kEpiGlu && pre_out) {
+      MS_MAP(&tO1, false, pre_out, N, C, 2 * N, C * 2 * N, 32);
+      MS_MAP(&tO2, false, (P)pre_out + N, N, C, 2 * N, C * 2 * N, 32);
+    }
+  }
+#undef MS_MAP
+  if (EPI != kEpiDact) { tP0 = tP1 = tO0; if (!pre_out) tO1 = tO0; }
+  if (EPI != kEpiGlu || !pre_out) tO2 = tO0;
+  const long long tile_n = EPI == kEpiGlu ? 128 : kXTile;
+  const long long tiles = (long long)a.E * (((kDw ? M : C) + kXTile - 1) / kXTile) * ((N + tile_n - 1) / tile_n);
+  const int pairs = (int)std::min<long long>(c->sm_count / 2, tiles);
+  expert_tc_kernel<EPI, B_MN><<<2 * pairs, kXThreads, x_smem(EPI), st>>>(tA, tB0, tB1, tO0, tO1, tO2, tP0, tP1, (char*)out, (char*)pre_out, a,
+                                                                        error_flag_of(c));
+  MS_LAUNCH_CHECK("expert_tc_kernel");
+  c->launches += 1;
+  return MAXSCORE_OK;
+}
+
+// b_mn: the product's columns (N) run along memory in B
 template <int EPI>
 maxscore_status launch_expert(maxscore_ctx* c, const void* A, const void* B, const void* pre_in, void* out, void* pre_out,
                               const ExpertArgs& a, bool b_mn, cudaStream_t st) {
   if (c->p.io_dtype == MAXSCORE_BF16) {
-    if constexpr (EPI == kEpiDw) return launch_fma<__nv_bfloat16, EPI, true, true>(c, A, B, pre_in, out, pre_out, a, st);
-    else return b_mn ? launch_fma<__nv_bfloat16, EPI, false, true>(c, A, B, pre_in, out, pre_out, a, st)
-                     : launch_fma<__nv_bfloat16, EPI, false, false>(c, A, B, pre_in, out, pre_out, a, st);
+    if constexpr (EPI == kEpiDw) return launch_tc<EPI, true>(c, A, B, pre_in, out, pre_out, a, st);
+    else return b_mn ? launch_tc<EPI, true>(c, A, B, pre_in, out, pre_out, a, st)
+                     : launch_tc<EPI, false>(c, A, B, pre_in, out, pre_out, a, st);
   }
   if constexpr (EPI == kEpiDw) return launch_fma<float, EPI, true, true>(c, A, B, pre_in, out, pre_out, a, st);
   else return b_mn ? launch_fma<float, EPI, false, true>(c, A, B, pre_in, out, pre_out, a, st)
