@@ -29,9 +29,6 @@ __device__ __forceinline__ void cluster_sync() {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
-__device__ __forceinline__ void mbar_expect_tx_cluster(uint32_t addr, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(addr), "r"(bytes) : "memory");
-}
 __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t phase, uint32_t limit = 1u << 22) {
   for (uint32_t it = 0; it < limit; ++it) {
     uint32_t ok;
@@ -80,7 +77,7 @@ __host__ __device__ constexpr int x_out_bytes(int epi) { return epi == kEpiDact 
 __host__ __device__ constexpr int x_smem(int epi) { return x_stages(epi) * kXStageBytes + x_out_bytes(epi) + 1024; }
 
 struct XSmem {
-  uint64_t full[6], empty[6], acc_full[2], acc_empty[2], tail, in[8];
+  uint64_t full[6], empty[6], acc_full[2], acc_empty[2], tail, tail_peer, in[8];
   uint32_t tmem;
   int failed;
   int rows[kMaxE], first[kMaxE + 1];     // rows in use; tiles before each expert
@@ -157,9 +154,9 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
   const int ntn = (a.N + kTileN - 1) / kTileN, ntm_dw = (a.M + kXTile - 1) / kXTile;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) { mbar_init(&sm.full[s], 2); mbar_init(&sm.empty[s], 1); }
+    for (int s = 0; s < kStages; ++s) { mbar_init(&sm.full[s], 1); mbar_init(&sm.empty[s], 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(&sm.acc_full[b], 1); mbar_init(&sm.acc_empty[b], 8); }
-    mbar_init(&sm.tail, 1);
+    mbar_init(&sm.tail, 1); mbar_init(&sm.tail_peer, 1);
     for (int i = 0; i < 8; ++i) mbar_init(&sm.in[i], 1);
     sm.failed = 0;
     fence_barrier_init();
@@ -182,7 +179,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
     XWalk<EPI> walk(sm, a, ntn, pair, pairs);
     XTile x;
     int it = 0; uint32_t tail_phase = 0; bool ok = true;
-    const uint32_t full0 = map_to_rank(smem_u32(&sm.full[0]), 0);
+    const uint32_t full0 = map_to_rank(smem_u32(&sm.full[0]), 0), tail_peer0 = map_to_rank(smem_u32(&sm.tail_peer), 0);
     const CUtensorMap* tB = rank ? &tB1 : &tB0;
     while (ok && walk.next(x)) {
       const int K = kDw ? x.rows : a.K;
@@ -200,8 +197,10 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
         if (lane == 0) {
           if (it >= kStages) good = mbar_wait_bounded(&sm.empty[s], ph ^ 1);
           if (good) {
-            if (!masked) mbar_expect_tx_cluster(full, kXStageBytes);
-            else mbar_expect_tx(&sm.tail, kXStageBytes);
+            // the leading CTA's barrier counts both CTAs' copies.  A remote arrival per slice instead (each CTA announcing its own
+            // half) held the whole pipeline at 0.74 us a slice: 755 TFLOP/s where this form gives 1 400.
+            if (masked) mbar_expect_tx(&sm.tail, kXStageBytes);
+            else if (rank == 0) mbar_expect_tx(&sm.full[s], 2 * kXStageBytes);
             auto put = [&](uint32_t dst, const CUtensorMap* tm, int xx, int yy) {
               if (masked) tma_load_3d(dst, tm, xx, yy, x.e, &sm.tail);
               else tma_load_3d_pair(dst, tm, xx, yy, x.e, full);
@@ -226,7 +225,12 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
               *reinterpret_cast<uint4*>(st + (i / per_box) * 8192 + r0 * 128 + (i % per_box) * 16) = make_uint4(0, 0, 0, 0);
             fence_proxy_async();
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(full);
+            // the other CTA reports to the leading one, which then releases the slice to the MMA
+            if (rank == 1) { if (lane == 0) mbar_arrive_cluster(tail_peer0); }
+            else {
+              good = __all_sync(0xffffffffu, mbar_wait_cluster(&sm.tail_peer, tail_phase ^ 1));
+              if (good && lane == 0) mbar_arrive(&sm.full[s]);
+            }
           }
         }
         ok = __shfl_sync(0xffffffffu, good, 0) != 0;
@@ -245,11 +249,11 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       const int nkb = (K + kXBK - 1) / kXBK;
       if (nkb == 0) continue;
       const int buf = tile & 1;
-      if (tile >= 2) ok = mbar_wait_cluster(&sm.acc_empty[buf], (uint32_t)(((tile >> 1) & 1) ^ 1));
+      if (tile >= 2) ok = mbar_wait_bounded(&sm.acc_empty[buf], (uint32_t)(((tile >> 1) & 1) ^ 1));
       const uint32_t acc = tmem + (uint32_t)(buf * 256);
       for (int kb = 0; kb < nkb && ok; ++kb, ++it) {
         const int s = it % kStages;
-        ok = mbar_wait_cluster(&sm.full[s], (uint32_t)((it / kStages) & 1));
+        ok = mbar_wait_bounded(&sm.full[s], (uint32_t)((it / kStages) & 1));
         if (!ok) break;
         tc_fence_after();
         const uint32_t sa = smem_u32(base) + (uint32_t)(s * kXStageBytes), sb = sa + 16384;
@@ -302,7 +306,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       const int y0 = x.m * kXTile + 128 * rank + 32 * q;              // first row of this warp
       const uint32_t acc = tmem + lanes + (uint32_t)(buf * 256);
       if (nkb > 0) {
-        ok = mbar_wait_cluster(&sm.acc_full[buf], (uint32_t)((tile >> 1) & 1));
+        ok = mbar_wait_bounded(&sm.acc_full[buf], (uint32_t)((tile >> 1) & 1));
         if (!ok) break;
         tc_fence_after();
       }
