@@ -21,6 +21,7 @@ struct ExpertArgs {
   int E, C;
   int M, N, K;              // dW: M = d_in, N = d_out, K per expert; else M per expert, N = columns (d_ff for the gated ones)
   int accumulate;           // dW only
+  int a_chunks, b_chunks;   // tensor cores: the operand's map has the 64-column chunks as a dimension of their own
 };
 
 __device__ __forceinline__ int expert_rows(const ExpertArgs& a, int e) {

@@ -211,17 +211,19 @@ maxscore_status make_tmap_bf16(const maxscore_ctx* c, CUtensorMap* tm, const voi
   return MAXSCORE_OK;
 }
 
-// One matrix per expert: [E][rows][inner] with given strides, boxes of one expert each, 128-byte swizzle.
+// One matrix per expert: [E][rows][inner] with given strides, boxes of one expert each, 128-byte swizzle.  chunks: the
+// 64-column chunks are a dimension of their own and a box takes two of them (inner % 64 == 0, bf16).
 maxscore_status make_tmap_expert(const maxscore_ctx* c, CUtensorMap* tm, bool f32, const void* base, uint64_t inner, uint64_t rows,
-                                 uint64_t row_stride, uint64_t expert_stride, uint32_t box_rows) {
-  const uint64_t b = f32 ? 4 : 2;
-  cuuint64_t dims[3] = {inner, rows, (cuuint64_t)c->p.E};
-  cuuint64_t strides[2] = {row_stride * b, expert_stride * b};
-  cuuint32_t box[3] = {(cuuint32_t)(128 / b), box_rows, 1};
-  cuuint32_t estr[3] = {1, 1, 1};
-  CUresult r = c->encode(tm, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims,
-                         strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                         CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                                 uint64_t row_stride, uint64_t expert_stride, uint32_t box_rows, bool chunks = false) {
+  const uint64_t b = f32 ? 4 : 2, E = (uint64_t)c->p.E;
+  cuuint64_t dims3[3] = {inner, rows, E}, dims4[4] = {64, rows, inner / 64, E};
+  cuuint64_t strides3[2] = {row_stride * b, expert_stride * b}, strides4[3] = {row_stride * b, 128, expert_stride * b};
+  cuuint32_t box3[3] = {(cuuint32_t)(128 / b), box_rows, 1}, box4[4] = {64, box_rows, 2, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  CUresult r = c->encode(tm, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, chunks ? 4 : 3,
+                         const_cast<void*>(base), chunks ? dims4 : dims3, chunks ? strides4 : strides3, chunks ? box4 : box3, estr,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
     snprintf(g_last_error, sizeof(g_last_error), "cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
     return MAXSCORE_ERR_CUDA;
@@ -1026,26 +1028,28 @@ maxscore_status launch_fma(maxscore_ctx* c, const void* A, const void* B, const 
 
 template <int EPI, bool B_MN>
 maxscore_status launch_tc(maxscore_ctx* c, const void* A, const void* B, const void* pre_in, void* out, void* pre_out,
-                          const ExpertArgs& a, cudaStream_t st) {
+                          ExpertArgs a, cudaStream_t st) {
   constexpr bool kDw = EPI == kEpiDw;
+  a.a_chunks = kDw && a.M % 64 == 0;
+  a.b_chunks = B_MN && a.N % 64 == 0;
   const uint64_t C = (uint64_t)c->C, M = (uint64_t)a.M, N = (uint64_t)a.N, K = (uint64_t)a.K;
   typedef const __nv_bfloat16* P;
   CUtensorMap tA, tB0, tB1, tO0, tO1, tO2, tP0, tP1;
   maxscore_status s;
 #define MS_MAP(...) do { s = make_tmap_expert(c, __VA_ARGS__); if (s) return s; } while (0)
   if (kDw) {
-    MS_MAP(&tA, false, A, M, C, M, C * M, 64);
-    MS_MAP(&tB0, false, B, N, C, N, C * N, 64);
+    MS_MAP(&tA, false, A, M, C, M, C * M, 64, a.a_chunks);
+    MS_MAP(&tB0, false, B, N, C, N, C * N, 64, a.b_chunks);
     tB1 = tB0;
     MS_MAP(&tO0, true, out, N, M, N, M * N, 32);
   } else {
     MS_MAP(&tA, false, A, K, C, K, C * K, 128);
     const uint64_t cols = EPI == kEpiGlu ? 2 * N : N;
-    if (B_MN) MS_MAP(&tB0, false, B, N, K, cols, K * cols, 64);
+    if (B_MN) MS_MAP(&tB0, false, B, N, K, cols, K * cols, 64, a.b_chunks);
     else MS_MAP(&tB0, false, B, K, N, K, cols * K, 128);
     tB1 = tB0;
     if (EPI == kEpiGlu) {
-      if (B_MN) MS_MAP(&tB1, false, (P)B + N, N, K, cols, K * cols, 64);
+      if (B_MN) MS_MAP(&tB1, false, (P)B + N, N, K, cols, K * cols, 64, a.b_chunks);
       else MS_MAP(&tB1, false, (P)B + N * K, K, N, K, cols * K, 128);
     }
     if (EPI == kEpiDact) {
