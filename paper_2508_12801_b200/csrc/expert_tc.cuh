@@ -80,10 +80,12 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {     // arrives
 }
 
 // ---- the kernel ----------------------------------------------------------------------------------------------------
-constexpr int kXThreads = 192, kXTile = 256, kXBK = 64, kXStageBytes = 32768;
-__host__ __device__ constexpr int x_stages(int epi) { return epi == kEpiDact ? 5 : 6; }
+constexpr int kXThreads = 192, kXTile = 256, kXBK = 64;
+// W: column tiles of a pair at a time (1: 256 x 256, two accumulators in turn; 2: 256 x 512)
+__host__ __device__ constexpr int x_stage_bytes(int w) { return 16384 * (1 + w); }
+__host__ __device__ constexpr int x_stages(int epi, int w) { return w == 2 ? (epi == kEpiDact ? 3 : 4) : (epi == kEpiDact ? 5 : 6); }
 __host__ __device__ constexpr int x_out_bytes(int epi) { return epi == kEpiDact ? 65536 : 32768; }
-__host__ __device__ constexpr int x_smem(int epi) { return x_stages(epi) * kXStageBytes + x_out_bytes(epi) + 1024; }
+__host__ __device__ constexpr int x_smem(int epi, int w) { return x_stages(epi, w) * x_stage_bytes(w) + x_out_bytes(epi) + 1024; }
 
 struct XSmem {
   uint64_t full[6], empty[6], acc_full[2], acc_empty[2], tail, tail_peer, in[8];
@@ -97,18 +99,25 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return *reinterpret_cast<uint32_t*>(&h);
 }
 
-struct XTile { int e, m, n, rows; };     // expert, tile row and column, rows of the expert in use
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
+
+struct XTile { int e, m, n, subs, rows; };     // expert, tile row, first column tile and their number, rows of the expert in use
 
 // Walks the tiles t, t + step, ... (t only grows, so the expert is found by stepping on from the last one).
-template <int EPI>
+template <int W>
 struct XWalk {
-  const XSmem& sm; const ExpertArgs& a; int ntn; int t, step, e;
-  __device__ XWalk(const XSmem& s, const ExpertArgs& args, int ntn_, int t0, int step_) : sm(s), a(args), ntn(ntn_), t(t0), step(step_), e(0) {}
+  const XSmem& sm; const ExpertArgs& a; int ntn, ntw; int t, step, e;
+  __device__ XWalk(const XSmem& s, const ExpertArgs& args, int ntn_, int t0, int step_)
+      : sm(s), a(args), ntn(ntn_), ntw((ntn_ + W - 1) / W), t(t0), step(step_), e(0) {}
   __device__ bool next(XTile& x) {
     if (t >= sm.first[a.E]) return false;
     while (t >= sm.first[e + 1]) ++e;
     const int l = t - sm.first[e];
-    x.e = e; x.m = l / ntn; x.n = l - x.m * ntn; x.rows = sm.rows[e];
+    x.e = e; x.m = l / ntw; x.n = (l - x.m * ntw) * W; x.subs = min(W, ntn - x.n); x.rows = sm.rows[e];
     t += step;
     return true;
   }
@@ -146,14 +155,14 @@ __device__ __forceinline__ void expert_prefix(const ExpertArgs& a, int* rows, in
 // EPI as in expert.cuh.  B_MN: B is stored with its columns contiguous.  dW: both operands run along the rows.
 // Maps: tA; tB0 / tB1 = B of the leading / the other CTA (gate and up columns in the gated form, else the same);
 // tO0 = output (gated: h; backward: dg), tO1 / tO2 = g / u kept (gated), du (backward, tO1); tP0 / tP1 = g / u read (backward).
-template <int EPI, bool B_MN>
+template <int EPI, bool B_MN, int W>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kXThreads)
 expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUtensorMap tB0, const __grid_constant__ CUtensorMap tB1,
                  const __grid_constant__ CUtensorMap tO0, const __grid_constant__ CUtensorMap tO1, const __grid_constant__ CUtensorMap tO2,
                  const __grid_constant__ CUtensorMap tP0, const __grid_constant__ CUtensorMap tP1, char* out, char* pre_out,
                  ExpertArgs a, unsigned* error_flag) {
   constexpr bool kDw = EPI == kEpiDw, kA_MN = kDw;
-  constexpr int kStages = x_stages(EPI);
+  constexpr int kStages = x_stages(EPI, W), kStageBytes = x_stage_bytes(W);
   constexpr int kTileN = EPI == kEpiGlu ? 128 : kXTile;               // output columns of a tile
   extern __shared__ unsigned char xsm_raw[];
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(xsm_raw) + 1023) & ~(uintptr_t)1023);
@@ -175,7 +184,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   if (warp == 2)
-    expert_prefix(a, sm.rows, sm.first, [&](int r) { return kDw ? ntm_dw * ntn : (r + kXTile - 1) / kXTile * ntn; });
+    expert_prefix(a, sm.rows, sm.first, [&](int r) { return (kDw ? ntm_dw : (r + kXTile - 1) / kXTile) * ((ntn + W - 1) / W); });
   tc_fence_before();
   __syncwarp();
   cluster_sync();                                       // barriers of both CTAs are ready, shared memory written above is seen
@@ -185,7 +194,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
 
   if (warp == 0) {
     // ---- producer ----------------------------------------------------------------------------------------------
-    XWalk<EPI> walk(sm, a, ntn, pair, pairs);
+    XWalk<W> walk(sm, a, ntn, pair, pairs);
     XTile x;
     int it = 0; uint32_t tail_phase = 0; bool ok = true;
     const uint32_t full0 = map_to_rank(smem_u32(&sm.full[0]), 0), tail_peer0 = map_to_rank(smem_u32(&sm.tail_peer), 0);
@@ -195,10 +204,11 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       const int nkb = (K + kXBK - 1) / kXBK;
       const int ax = x.m * kXTile + 128 * rank;
       const int bx = EPI == kEpiGlu ? x.n * 128 : x.n * kXTile + 128 * rank;
+      const uint32_t bytes = 16384u * (uint32_t)(1 + x.subs);
       for (int kb = 0; kb < nkb && ok; ++kb, ++it) {
         const int s = it % kStages;
         const uint32_t ph = (uint32_t)((it / kStages) & 1);
-        const uint32_t sa = smem_u32(base) + (uint32_t)(s * kXStageBytes), sb = sa + 16384;
+        const uint32_t sa = smem_u32(base) + (uint32_t)(s * kStageBytes), sb = sa + 16384;
         const uint32_t full = full0 + 8u * (uint32_t)s;
         const int k0 = kb * kXBK;
         const bool masked = kDw && kb == nkb - 1 && (K & 15);          // the load ends inside an MMA's depth
@@ -208,8 +218,8 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
           if (good) {
             // the leading CTA's barrier counts both CTAs' copies.  A remote arrival per slice instead (each CTA announcing its own
             // half) held the whole pipeline at 0.74 us a slice: 755 TFLOP/s where this form gives 1 400.
-            if (masked) mbar_expect_tx(&sm.tail, kXStageBytes);
-            else if (rank == 0) mbar_expect_tx(&sm.full[s], 2 * kXStageBytes);
+            if (masked) mbar_expect_tx(&sm.tail, bytes);
+            else if (rank == 0) mbar_expect_tx(&sm.full[s], 2 * bytes);
             auto put = [&](uint32_t dst, const CUtensorMap* tm, int xx, int yy) {
               if (masked) tma_load_3d(dst, tm, xx, yy, x.e, &sm.tail);
               else tma_load_3d_pair(dst, tm, xx, yy, x.e, full);
@@ -222,7 +232,12 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
               else tma_load_4d_pair(dst, tm, k0, xx >> 6, x.e, full);
             };
             if (kA_MN) put_mn(sa, &tA, ax, a.a_chunks); else put(sa, &tA, k0, ax);
-            if (B_MN) put_mn(sb, tB, bx, a.b_chunks); else put(sb, tB, k0, bx);
+#pragma unroll
+            for (int h = 0; h < W; ++h)
+              if (h < x.subs) {
+                const int bh = bx + h * (EPI == kEpiGlu ? 128 : kXTile);
+                if (B_MN) put_mn(sb + h * 16384, tB, bh, a.b_chunks); else put(sb + h * 16384, tB, k0, bh);
+              }
           }
         }
         if (kDw && masked) {
@@ -233,9 +248,9 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
           tail_phase ^= 1;
           if (good) {
             const int r0 = K - k0, r1 = (r0 + 15) & ~15;               // a row is 128 bytes of a box, whatever the swizzle
-            unsigned char* st = base + (size_t)s * kXStageBytes;
+            unsigned char* st = base + (size_t)s * kStageBytes;
             const int per_box = (r1 - r0) * 8;
-            for (int i = lane; i < 4 * per_box; i += 32)
+            for (int i = lane; i < 2 * (1 + x.subs) * per_box; i += 32)
               *reinterpret_cast<uint4*>(st + (i / per_box) * 8192 + r0 * 128 + (i % per_box) * 16) = make_uint4(0, 0, 0, 0);
             fence_proxy_async();
             __syncwarp();
@@ -251,39 +266,62 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       }
     }
     if (!ok && lane == 0) sm.failed = 1;
-  } else if (warp == 1 && rank == 0 && lane == 0) {
+  } else if (warp == 1 && rank == 0) {
     // ---- MMA issuer of the pair --------------------------------------------------------------------------------------
+    // The tensor pipe holds little beyond the MMA it runs, so every clock between a slice's last MMA and the next one's
+    // first shows.  The whole warp walks and waits (its values stay in uniform registers, where the MMA wants them), one
+    // elected lane issues a slice's four MMAs and its commit in a row.
     const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (kA_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
                            ((uint32_t)(kXTile >> 3) << 17) | ((uint32_t)(kXTile >> 4) << 24);
-    XWalk<EPI> walk(sm, a, ntn, pair, pairs);
+    constexpr uint32_t kAStep = kA_MN ? 128 : 2, kBStep = B_MN ? 128 : 2;      // 16 deep, in descriptor units of 16 bytes
+    const uint64_t adesc0 = kA_MN ? smem_desc_mn128(smem_u32(base), 8192u) : smem_desc_k128(smem_u32(base));
+    const uint64_t bdesc0 = B_MN ? smem_desc_mn128(smem_u32(base) + 16384, 8192u) : smem_desc_k128(smem_u32(base) + 16384);
+    XWalk<W> walk(sm, a, ntn, pair, pairs);
     XTile x;
-    int it = 0, tile = 0; bool ok = true;
+    uint32_t acc_ph = 3, full_ph = 0;                   // bit b: parity to wait for at accumulator b; parity of the ring
+    int s0 = 0, turn = 0; bool ok = true;               // s0: ring position of slice kb
     while (ok && walk.next(x)) {
       const int K = kDw ? x.rows : a.K;
       const int nkb = (K + kXBK - 1) / kXBK;
       if (nkb == 0) continue;
-      const int buf = tile & 1;
-      if (tile >= 2) ok = mbar_wait_bounded(&sm.acc_empty[buf], (uint32_t)(((tile >> 1) & 1) ^ 1));
-      const uint32_t acc = tmem + (uint32_t)(buf * 256);
-      for (int kb = 0; kb < nkb && ok; ++kb, ++it) {
-        const int s = it % kStages;
-        ok = mbar_wait_bounded(&sm.full[s], (uint32_t)((it / kStages) & 1));
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t sa = smem_u32(base) + (uint32_t)(s * kXStageBytes), sb = sa + 16384;
-        const int steps = kb == nkb - 1 ? (K - kb * kXBK + 15) / 16 : 4;
-        for (int kk = 0; kk < steps; ++kk) {
-          // 16 deep: 32 bytes along a K-major row, 16 rows of 128 bytes in the other major
-          const uint64_t ad = kA_MN ? smem_desc_mn128(sa + kk * 2048u, 8192u) : smem_desc_k128(sa) + 2 * kk;
-          const uint64_t bd = B_MN ? smem_desc_mn128(sb + kk * 2048u, 8192u) : smem_desc_k128(sb) + 2 * kk;
-          umma_bf16_pair(acc, ad, bd, idesc, (kb > 0 || kk > 0) ? 1u : 0u);
+      // With two column tiles the first and the last slices are multiplied group-wise, the first column tile ahead of the
+      // second: its accumulator is complete (and free again) that much earlier, which is what hides the epilogues.
+      const int group = x.subs == 2 ? kStages : 1;
+      for (int kb = 0; kb < nkb && ok;) {
+        const int n = (kb == 0 || nkb - kb <= group) ? min(group, nkb - kb) : 1;
+        int s = s0;
+#pragma unroll
+        for (int h = 0; h < W; ++h) {
+          if (h >= x.subs) break;
+          const uint32_t buf = W == 2 ? h : turn & 1;
+          const uint32_t acc = tmem + buf * 256;
+          if (kb == 0) { ok = ok && mbar_wait_bounded(&sm.acc_empty[buf], (acc_ph >> buf) & 1); acc_ph ^= 1u << buf; }
+          s = s0;
+          uint32_t ph = full_ph;
+          for (int j = 0; j < n; ++j) {
+            if (h == 0) ok = ok && mbar_wait_bounded(&sm.full[s], ph);
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t ad = adesc0 + (uint64_t)(s * (kStageBytes / 16)), bd = bdesc0 + (uint64_t)(s * (kStageBytes / 16) + h * 1024);
+            const int left = K - (kb + j) * kXBK;
+            if (elect_one()) {
+              umma_bf16_pair(acc, ad, bd, idesc, kb + j > 0 ? 1u : 0u);
+              if (left > 16) umma_bf16_pair(acc, ad + kAStep, bd + kBStep, idesc, 1u);
+              if (left > 32) umma_bf16_pair(acc, ad + 2 * kAStep, bd + 2 * kBStep, idesc, 1u);
+              if (left > 48) umma_bf16_pair(acc, ad + 3 * kAStep, bd + 3 * kBStep, idesc, 1u);
+              if (h == x.subs - 1) umma_commit_pair(&sm.empty[s]);
+              if (kb + j == nkb - 1) umma_commit_pair(&sm.acc_full[buf]);
+            }
+            __syncwarp();
+            if (++s == kStages) { s = 0; ph ^= 1; }
+          }
+          if (h == x.subs - 1) full_ph = ph;
         }
-        umma_commit_pair(&sm.empty[s]);
+        s0 = s; kb += n;
       }
-      umma_commit_pair(&sm.acc_full[buf]);
-      ++tile;
+      ++turn;
     }
-    if (!ok) sm.failed = 1;
+    if (!ok && lane == 0) sm.failed = 1;
   } else if (warp >= 2) {
     // ---- epilogue ------------------------------------------------------------------------------------------------------
     const int q = warp & 3;                             // TMEM lanes this warp may read
@@ -292,12 +330,13 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       expert_zero_behind(a, sm.rows, out, 2 * (size_t)(EPI == kEpiDact ? 2 * a.N : a.N), kXTile, worker, workers);
       if (EPI == kEpiGlu && pre_out) expert_zero_behind(a, sm.rows, pre_out, 4 * (size_t)a.N, kXTile, worker, workers);
     }
-    unsigned char* stage = base + kStages * kXStageBytes + (size_t)q * (x_out_bytes(EPI) / 4);
+    unsigned char* stage = base + kStages * kStageBytes + (size_t)q * (x_out_bytes(EPI) / 4);
     const uint32_t acc_empty0 = map_to_rank(smem_u32(&sm.acc_empty[0]), 0);
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
-    XWalk<EPI> walk(sm, a, ntn, pair, pairs);
+    XWalk<W> walk(sm, a, ntn, pair, pairs);
     XTile x;
-    int tile = 0, box = 0, in_count = 0; bool ok = true;
+    uint32_t acc_ph = 0;                                // bit b: parity to wait for at accumulator b
+    int turn = 0, box = 0, in_count = 0; bool ok = true;
     // a 32-row x 128-byte box in the 128-byte swizzle, out through one TMA store; two boxes alternate
     auto begin_box = [&]() -> unsigned char* {
       if (lane == 0 && box >= 2) bulk_wait_read<1>();
@@ -316,11 +355,12 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
     };
     while (ok && walk.next(x)) {
       const int nkb = ((kDw ? x.rows : a.K) + kXBK - 1) / kXBK;
-      const int buf = tile & 1;
       const int y0 = x.m * kXTile + 128 * rank + 32 * q;              // first row of this warp
+      for (int sub = 0; sub < x.subs && ok; ++sub) {
+      const int buf = W == 2 ? sub : turn & 1, xn = x.n + sub;
       const uint32_t acc = tmem + lanes + (uint32_t)(buf * 256);
       if (nkb > 0) {
-        ok = mbar_wait_bounded(&sm.acc_full[buf], (uint32_t)((tile >> 1) & 1));
+        ok = mbar_wait_bounded(&sm.acc_full[buf], (acc_ph >> buf) & 1);
         if (!ok) break;
         tc_fence_after();
       }
@@ -339,7 +379,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
           for (int i = 0; i < 8; ++i)
             *reinterpret_cast<uint4*>(row + ((i ^ (lane & 7)) << 4)) =
                 make_uint4(u[i >> 2][(i & 3) * 4], u[i >> 2][(i & 3) * 4 + 1], u[i >> 2][(i & 3) * 4 + 2], u[i >> 2][(i & 3) * 4 + 3]);
-          const int xx = x.n * kXTile + c0;
+          const int xx = xn * kXTile + c0;
           end_box(&tO0, xx, y0, x.e, xx < a.N && y0 < a.M && (nkb > 0 || !a.accumulate), a.accumulate);
         }
       } else {
@@ -362,12 +402,12 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
               }
               *reinterpret_cast<uint4*>(row + ((i ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
             }
-            const int xx = x.n * kXTile + c0;
+            const int xx = xn * kXTile + c0;
             end_box(&tO0, xx, y0, x.e, in_y && xx < a.N);
           }
         } else if constexpr (EPI == kEpiGlu) {
           for (int c0 = 0; c0 < 128; c0 += 64) {
-            const int xx = x.n * 128 + c0;
+            const int xx = xn * 128 + c0;
             uint32_t hw[32], gw[32], uw[32];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -400,7 +440,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
         } else {
           // dh in the accumulator; g and u come in through two 8 KB pairs of boxes, which dg and du then leave from
           auto fetch = [&](int c, int slot) {
-            const int xx = x.n * kXTile + c * 64;
+            const int xx = xn * kXTile + c * 64;
             if (lane == 0) {
               const uint32_t d = smem_u32(stage + slot * 8192);
               uint64_t* bar = &sm.in[q * 2 + slot];
@@ -450,7 +490,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) {
-              const int xx = x.n * kXTile + c * 64;
+              const int xx = xn * kXTile + c * 64;
               if (in_y && xx < a.N) {
                 const uint32_t src = smem_u32(stage + slot * 8192);
                 tma_store_3d(&tO0, xx, y0, x.e, src);
@@ -465,8 +505,10 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(acc_empty0 + 8u * (uint32_t)buf);
-        ++tile;
+        acc_ph ^= 1u << buf;
       }
+      }
+      if (nkb > 0) ++turn;
     }
     if (lane == 0) bulk_wait_all<0>();
     if (!ok && lane == 0) sm.failed = 1;

@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdio.h>
+#include <stdlib.h>
 #include <string.h>
 
 #include <algorithm>
@@ -501,13 +502,18 @@ maxscore_status maxscore_create(maxscore_ctx** out, const maxscore_params* param
   MS_CUDA(cudaFuncSetAttribute(gate_bwd_dh_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDhSmemMax));
   MS_CUDA(cudaFuncSetAttribute(gate_bwd_dw_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDwSmemMax));
   MS_CUDA(cudaFuncSetAttribute(dispatch_tma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kTmaWarps * kTmaStages * kTmaChunk));
-  MS_CUDA(cudaFuncSetAttribute(expert_tc_kernel<kEpiPlain, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, x_smem(kEpiPlain)));
-  MS_CUDA(cudaFuncSetAttribute(expert_tc_kernel<kEpiPlain, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, x_smem(kEpiPlain)));
-  MS_CUDA(cudaFuncSetAttribute(expert_tc_kernel<kEpiGlu, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, x_smem(kEpiGlu)));
-  MS_CUDA(cudaFuncSetAttribute(expert_tc_kernel<kEpiGlu, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, x_smem(kEpiGlu)));
-  MS_CUDA(cudaFuncSetAttribute(expert_tc_kernel<kEpiDact, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, x_smem(kEpiDact)));
-  MS_CUDA(cudaFuncSetAttribute(expert_tc_kernel<kEpiDact, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, x_smem(kEpiDact)));
-  MS_CUDA(cudaFuncSetAttribute(expert_tc_kernel<kEpiDw, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, x_smem(kEpiDw)));
+  {
+    cudaError_t e_ = cudaSuccess;
+    auto room = [&](auto kernel, int bytes) { if (e_ == cudaSuccess) e_ = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
+    room(expert_tc_kernel<kEpiPlain, false, 1>, x_smem(kEpiPlain, 1)); room(expert_tc_kernel<kEpiPlain, false, 2>, x_smem(kEpiPlain, 2));
+    room(expert_tc_kernel<kEpiPlain, true, 1>, x_smem(kEpiPlain, 1)); room(expert_tc_kernel<kEpiPlain, true, 2>, x_smem(kEpiPlain, 2));
+    room(expert_tc_kernel<kEpiGlu, false, 1>, x_smem(kEpiGlu, 1)); room(expert_tc_kernel<kEpiGlu, false, 2>, x_smem(kEpiGlu, 2));
+    room(expert_tc_kernel<kEpiGlu, true, 1>, x_smem(kEpiGlu, 1)); room(expert_tc_kernel<kEpiGlu, true, 2>, x_smem(kEpiGlu, 2));
+    room(expert_tc_kernel<kEpiDact, false, 1>, x_smem(kEpiDact, 1)); room(expert_tc_kernel<kEpiDact, false, 2>, x_smem(kEpiDact, 2));
+    room(expert_tc_kernel<kEpiDact, true, 1>, x_smem(kEpiDact, 1)); room(expert_tc_kernel<kEpiDact, true, 2>, x_smem(kEpiDact, 2));
+    room(expert_tc_kernel<kEpiDw, true, 1>, x_smem(kEpiDw, 1)); room(expert_tc_kernel<kEpiDw, true, 2>, x_smem(kEpiDw, 2));
+    if (e_ != cudaSuccess) return cuda_fail(e_, "cudaFuncSetAttribute(expert_tc_kernel)");
+  }
   int coop = 0, sweep_occ = 0;
   MS_CUDA(cudaDeviceGetAttribute(&coop, cudaDevAttrCooperativeLaunch, dev));
   MS_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&sweep_occ, flow_sweeps_kernel, kSwThreads, 0));
@@ -1071,8 +1077,12 @@ maxscore_status launch_tc(maxscore_ctx* c, const void* A, const void* B, const v
   const long long tile_n = EPI == kEpiGlu ? 128 : kXTile;
   const long long tiles = (long long)a.E * (((kDw ? M : C) + kXTile - 1) / kXTile) * ((N + tile_n - 1) / tile_n);
   const int pairs = (int)std::min<long long>(c->sm_count / 2, tiles);
-  expert_tc_kernel<EPI, B_MN><<<2 * pairs, kXThreads, x_smem(EPI), st>>>(tA, tB0, tB1, tO0, tO1, tO2, tP0, tP1, (char*)out, (char*)pre_out, a,
-                                                                        error_flag_of(c));
+  auto go = [&](auto kernel, int w) {
+    kernel<<<2 * pairs, kXThreads, x_smem(EPI, w), st>>>(tA, tB0, tB1, tO0, tO1, tO2, tP0, tP1, (char*)out, (char*)pre_out, a, error_flag_of(c));
+  };
+  static const int force = getenv("XW") ? atoi(getenv("XW")) : 2;
+  if (force == 2) go(expert_tc_kernel<EPI, B_MN, 2>, 2);
+  else go(expert_tc_kernel<EPI, B_MN, 1>, 1);
   MS_LAUNCH_CHECK("expert_tc_kernel");
   c->launches += 1;
   return MAXSCORE_OK;
