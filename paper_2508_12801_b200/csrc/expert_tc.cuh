@@ -80,12 +80,12 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {     // arrives
 }
 
 // ---- the kernel ----------------------------------------------------------------------------------------------------
-constexpr int kXThreads = 192, kXTile = 256, kXBK = 64;
+constexpr int kXThreads = 320, kXTile = 256, kXBK = 64;
 // W: column tiles of a pair at a time (1: 256 x 256, two accumulators in turn; 2: 256 x 512)
 __host__ __device__ constexpr int x_stage_bytes(int w) { return 16384 * (1 + w); }
-__host__ __device__ constexpr int x_stages(int epi, int w) { return w == 2 ? (epi == kEpiDact ? 3 : 4) : (epi == kEpiDact ? 5 : 6); }
-__host__ __device__ constexpr int x_out_bytes(int epi) { return epi == kEpiDact ? 65536 : 32768; }
-__host__ __device__ constexpr int x_smem(int epi, int w) { return x_stages(epi, w) * x_stage_bytes(w) + x_out_bytes(epi) + 1024; }
+__host__ __device__ constexpr int x_stages(int w) { return w == 2 ? 3 : 5; }
+constexpr int kXOutBytes = 65536;        // 8 KB of staging for each epilogue warp
+__host__ __device__ constexpr int x_smem(int w) { return x_stages(w) * x_stage_bytes(w) + kXOutBytes + 1024; }
 
 struct XSmem {
   uint64_t full[6], empty[6], acc_full[2], acc_empty[2], tail, tail_peer, in[8];
@@ -162,7 +162,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
                  const __grid_constant__ CUtensorMap tP0, const __grid_constant__ CUtensorMap tP1, char* out, char* pre_out,
                  ExpertArgs a, unsigned* error_flag) {
   constexpr bool kDw = EPI == kEpiDw, kA_MN = kDw;
-  constexpr int kStages = x_stages(EPI, W), kStageBytes = x_stage_bytes(W);
+  constexpr int kStages = x_stages(W), kStageBytes = x_stage_bytes(W);
   constexpr int kTileN = EPI == kEpiGlu ? 128 : kXTile;               // output columns of a tile
   extern __shared__ unsigned char xsm_raw[];
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(xsm_raw) + 1023) & ~(uintptr_t)1023);
@@ -173,7 +173,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) { mbar_init(&sm.full[s], 1); mbar_init(&sm.empty[s], 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(&sm.acc_full[b], 1); mbar_init(&sm.acc_empty[b], 8); }
+    for (int b = 0; b < 2; ++b) { mbar_init(&sm.acc_full[b], 1); mbar_init(&sm.acc_empty[b], 16); }
     mbar_init(&sm.tail, 1); mbar_init(&sm.tail_peer, 1);
     for (int i = 0; i < 8; ++i) mbar_init(&sm.in[i], 1);
     sm.failed = 0;
@@ -324,13 +324,13 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
     if (!ok && lane == 0) sm.failed = 1;
   } else if (warp >= 2) {
     // ---- epilogue ------------------------------------------------------------------------------------------------------
-    const int q = warp & 3;                             // TMEM lanes this warp may read
+    const int q = warp & 3, part = (warp - 2) >> 2;     // TMEM lanes this warp may read; its half of a tile's columns
     if constexpr (!kDw) {
-      const int worker = blockIdx.x * 128 + (warp - 2) * 32 + lane, workers = gridDim.x * 128;
+      const int worker = blockIdx.x * 256 + (warp - 2) * 32 + lane, workers = gridDim.x * 256;
       expert_zero_behind(a, sm.rows, out, 2 * (size_t)(EPI == kEpiDact ? 2 * a.N : a.N), kXTile, worker, workers);
       if (EPI == kEpiGlu && pre_out) expert_zero_behind(a, sm.rows, pre_out, 4 * (size_t)a.N, kXTile, worker, workers);
     }
-    unsigned char* stage = base + kStages * kStageBytes + (size_t)q * (x_out_bytes(EPI) / 4);
+    unsigned char* stage = base + kStages * kStageBytes + (size_t)(warp - 2) * 8192;
     const uint32_t acc_empty0 = map_to_rank(smem_u32(&sm.acc_empty[0]), 0);
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
     XWalk<W> walk(sm, a, ntn, pair, pairs);
@@ -359,13 +359,25 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       for (int sub = 0; sub < x.subs && ok; ++sub) {
       const int buf = W == 2 ? sub : turn & 1, xn = x.n + sub;
       const uint32_t acc = tmem + lanes + (uint32_t)(buf * 256);
+      // backward: a chunk of g and u into the pair of boxes
+      auto fetch = [&](int xx) {
+        if (lane == 0) {
+          uint64_t* bar = &sm.in[warp - 2];
+          bulk_wait_read<0>();                                         // the last boxes have been read by their stores
+          mbar_expect_tx(bar, 8192);
+          tma_load_3d(smem_u32(stage), &tP0, xx, y0, x.e, bar);
+          tma_load_3d(smem_u32(stage) + 4096, &tP1, xx, y0, x.e, bar);
+        }
+        __syncwarp();
+      };
+      if (EPI == kEpiDact) fetch(xn * kXTile + part * 128);
       if (nkb > 0) {
         ok = mbar_wait_bounded(&sm.acc_full[buf], (acc_ph >> buf) & 1);
         if (!ok) break;
         tc_fence_after();
       }
       if constexpr (kDw) {
-        for (int c0 = 0; c0 < kXTile; c0 += 32) {
+        for (int c0 = part * 128; c0 < part * 128 + 128; c0 += 32) {
           uint32_t u[2][16];
           if (nkb > 0) {
             tmem_ld16_issue(acc + c0, u[0]); tmem_ld16_issue(acc + c0 + 16, u[1]);
@@ -386,7 +398,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
         const bool keep_row = y0 + lane < x.rows;                      // rows behind the load come out as zeros
         const bool in_y = y0 < a.C;
         if constexpr (EPI == kEpiPlain) {
-          for (int c0 = 0; c0 < kXTile; c0 += 64) {
+          for (int c0 = part * 128; c0 < part * 128 + 128; c0 += 64) {
             uint32_t u[4][16];
 #pragma unroll
             for (int i = 0; i < 4; ++i) tmem_ld16_issue(acc + c0 + 16 * i, u[i]);
@@ -406,8 +418,8 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
             end_box(&tO0, xx, y0, x.e, in_y && xx < a.N);
           }
         } else if constexpr (EPI == kEpiGlu) {
-          for (int c0 = 0; c0 < 128; c0 += 64) {
-            const int xx = xn * 128 + c0;
+          {
+            const int c0 = part * 64, xx = xn * 128 + c0;
             uint32_t hw[32], gw[32], uw[32];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -438,30 +450,14 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
             if (pre_out) { emit(&tO1, gw); emit(&tO2, uw); }
           }
         } else {
-          // dh in the accumulator; g and u come in through two 8 KB pairs of boxes, which dg and du then leave from
-          auto fetch = [&](int c, int slot) {
+          // dh in the accumulator; g and u come in through a pair of boxes, which dg and du then leave from
+          for (int c = part * 2; c < part * 2 + 2 && ok; ++c) {
             const int xx = xn * kXTile + c * 64;
-            if (lane == 0) {
-              const uint32_t d = smem_u32(stage + slot * 8192);
-              uint64_t* bar = &sm.in[q * 2 + slot];
-              mbar_expect_tx(bar, 8192);
-              tma_load_3d(d, &tP0, xx, y0, x.e, bar);
-              tma_load_3d(d + 4096, &tP1, xx, y0, x.e, bar);
-            }
-          };
-          if (lane == 0) bulk_wait_read<0>();                          // the last tile's boxes have been read by their stores
-          __syncwarp();
-          fetch(0, 0);
-          for (int c = 0; c < 4 && ok; ++c) {
-            const int slot = c & 1;
-            if (c < 3) {
-              if (c >= 1) { if (lane == 0) bulk_wait_read<0>(); __syncwarp(); }
-              fetch(c + 1, slot ^ 1);
-            }
-            ok = mbar_wait_bounded(&sm.in[q * 2 + slot], (uint32_t)(in_count >> 1 & 1));
+            if (c & 1) fetch(xx);                                      // the first one was asked for ahead of the accumulator
+            ok = mbar_wait_bounded(&sm.in[warp - 2], (uint32_t)(in_count & 1));
             ++in_count;
             if (!ok) break;
-            unsigned char* row = stage + slot * 8192 + lane * 128;
+            unsigned char* row = stage + lane * 128;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
               uint32_t u[2][16];
@@ -490,9 +486,8 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) {
-              const int xx = xn * kXTile + c * 64;
               if (in_y && xx < a.N) {
-                const uint32_t src = smem_u32(stage + slot * 8192);
+                const uint32_t src = smem_u32(stage);
                 tma_store_3d(&tO0, xx, y0, x.e, src);
                 tma_store_3d(&tO1, xx, y0, x.e, src + 4096);
               }

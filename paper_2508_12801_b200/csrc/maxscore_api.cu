@@ -505,13 +505,13 @@ maxscore_status maxscore_create(maxscore_ctx** out, const maxscore_params* param
   {
     cudaError_t e_ = cudaSuccess;
     auto room = [&](auto kernel, int bytes) { if (e_ == cudaSuccess) e_ = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
-    room(expert_tc_kernel<kEpiPlain, false, 1>, x_smem(kEpiPlain, 1)); room(expert_tc_kernel<kEpiPlain, false, 2>, x_smem(kEpiPlain, 2));
-    room(expert_tc_kernel<kEpiPlain, true, 1>, x_smem(kEpiPlain, 1)); room(expert_tc_kernel<kEpiPlain, true, 2>, x_smem(kEpiPlain, 2));
-    room(expert_tc_kernel<kEpiGlu, false, 1>, x_smem(kEpiGlu, 1)); room(expert_tc_kernel<kEpiGlu, false, 2>, x_smem(kEpiGlu, 2));
-    room(expert_tc_kernel<kEpiGlu, true, 1>, x_smem(kEpiGlu, 1)); room(expert_tc_kernel<kEpiGlu, true, 2>, x_smem(kEpiGlu, 2));
-    room(expert_tc_kernel<kEpiDact, false, 1>, x_smem(kEpiDact, 1)); room(expert_tc_kernel<kEpiDact, false, 2>, x_smem(kEpiDact, 2));
-    room(expert_tc_kernel<kEpiDact, true, 1>, x_smem(kEpiDact, 1)); room(expert_tc_kernel<kEpiDact, true, 2>, x_smem(kEpiDact, 2));
-    room(expert_tc_kernel<kEpiDw, true, 1>, x_smem(kEpiDw, 1)); room(expert_tc_kernel<kEpiDw, true, 2>, x_smem(kEpiDw, 2));
+    room(expert_tc_kernel<kEpiPlain, false, 1>, x_smem(1)); room(expert_tc_kernel<kEpiPlain, false, 2>, x_smem(2));
+    room(expert_tc_kernel<kEpiPlain, true, 1>, x_smem(1)); room(expert_tc_kernel<kEpiPlain, true, 2>, x_smem(2));
+    room(expert_tc_kernel<kEpiGlu, false, 1>, x_smem(1)); room(expert_tc_kernel<kEpiGlu, false, 2>, x_smem(2));
+    room(expert_tc_kernel<kEpiGlu, true, 1>, x_smem(1)); room(expert_tc_kernel<kEpiGlu, true, 2>, x_smem(2));
+    room(expert_tc_kernel<kEpiDact, false, 1>, x_smem(1)); room(expert_tc_kernel<kEpiDact, false, 2>, x_smem(2));
+    room(expert_tc_kernel<kEpiDact, true, 1>, x_smem(1)); room(expert_tc_kernel<kEpiDact, true, 2>, x_smem(2));
+    room(expert_tc_kernel<kEpiDw, true, 1>, x_smem(1)); room(expert_tc_kernel<kEpiDw, true, 2>, x_smem(2));
     if (e_ != cudaSuccess) return cuda_fail(e_, "cudaFuncSetAttribute(expert_tc_kernel)");
   }
   int coop = 0, sweep_occ = 0;
@@ -1078,7 +1078,7 @@ maxscore_status launch_tc(maxscore_ctx* c, const void* A, const void* B, const v
   const long long tiles = (long long)a.E * (((kDw ? M : C) + kXTile - 1) / kXTile) * ((N + tile_n - 1) / tile_n);
   const int pairs = (int)std::min<long long>(c->sm_count / 2, tiles);
   auto go = [&](auto kernel, int w) {
-    kernel<<<2 * pairs, kXThreads, x_smem(EPI, w), st>>>(tA, tB0, tB1, tO0, tO1, tO2, tP0, tP1, (char*)out, (char*)pre_out, a, error_flag_of(c));
+    kernel<<<2 * pairs, kXThreads, x_smem(w), st>>>(tA, tB0, tB1, tO0, tO1, tO2, tP0, tP1, (char*)out, (char*)pre_out, a, error_flag_of(c));
   };
   static const int force = getenv("XW") ? atoi(getenv("XW")) : 2;
   if (force == 2) go(expert_tc_kernel<EPI, B_MN, 2>, 2);
