@@ -5,7 +5,7 @@
 // That halves the operand traffic per flop of a single CTA's 128 x 256 tile (64 bytes per clock and SM at full rate instead
 // of 96, which the L2 cannot deliver).  Two accumulators alternate, so the epilogue of a tile runs under the MMAs of the next.
 //   warp 0: TMA loads, six (five) stages of 64-deep slices;  warp 1: TMEM, and in the leading CTA the MMAs;
-//   warps 2-5: epilogue, one TMEM lane quarter each, out through swizzled staging boxes and TMA tile stores.
+//   warps 2-9: epilogue, a TMEM lane quarter and half of the columns each, out through staging boxes as whole lines.
 // Both operand majors are read in place through the descriptors: no weight is ever transposed.
 //
 // Ragged loads.  Rows: a tile is whole or partial, rows behind the load come out as zeros.  Contraction over rows (dW): the
@@ -28,6 +28,11 @@ __device__ __forceinline__ void cluster_sync() {
 }
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+}
+// Arrival that orders nothing: a release at cluster scope waits for every global store of the warp (4 500 clocks an epilogue).
+// Enough where what the other side waits for has already been consumed into registers.
+__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
 __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t phase, uint32_t limit = 1u << 22) {
   for (uint32_t it = 0; it < limit; ++it) {
@@ -64,10 +69,6 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* tm, int x, int y
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(tm), "r"(src), "r"(x), "r"(y),
                "r"(z) : "memory");
 }
-__device__ __forceinline__ void tma_add_3d(const CUtensorMap* tm, int x, int y, int z, uint32_t src) {
-  asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(tm), "r"(src),
-               "r"(x), "r"(y), "r"(z) : "memory");
-}
 __device__ __forceinline__ void umma_bf16_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
@@ -83,12 +84,13 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {     // arrives
 constexpr int kXThreads = 320, kXTile = 256, kXBK = 64;
 // W: column tiles of a pair at a time (1: 256 x 256, two accumulators in turn; 2: 256 x 512)
 __host__ __device__ constexpr int x_stage_bytes(int w) { return 16384 * (1 + w); }
-__host__ __device__ constexpr int x_stages(int w) { return w == 2 ? 3 : 5; }
-constexpr int kXOutBytes = 65536;        // 8 KB of staging for each epilogue warp
-__host__ __device__ constexpr int x_smem(int w) { return x_stages(w) * x_stage_bytes(w) + kXOutBytes + 1024; }
+// Staging of an epilogue warp: 4 KB boxes, one for dW, a pair for the others.
+__host__ __device__ constexpr int x_box_bytes(int epi) { return epi == kEpiDw ? 4096 : 8192; }
+__host__ __device__ constexpr int x_stages(int epi, int w) { return (w == 2 ? 3 : 5) + (epi == kEpiDw ? 1 : 0); }
+__host__ __device__ constexpr int x_smem(int epi, int w) { return x_stages(epi, w) * x_stage_bytes(w) + 8 * x_box_bytes(epi) + 1024; }
 
 struct XSmem {
-  uint64_t full[6], empty[6], acc_full[2], acc_empty[2], tail, tail_peer, in[8];
+  uint64_t full[6], empty[6], acc_full[2], acc_empty[2], tail, tail_peer;
   uint32_t tmem;
   int failed;
   int rows[kMaxE], first[kMaxE + 1];     // rows in use; tiles before each expert
@@ -153,16 +155,15 @@ __device__ __forceinline__ void expert_prefix(const ExpertArgs& a, int* rows, in
 }
 
 // EPI as in expert.cuh.  B_MN: B is stored with its columns contiguous.  dW: both operands run along the rows.
-// Maps: tA; tB0 / tB1 = B of the leading / the other CTA (gate and up columns in the gated form, else the same);
-// tO0 = output (gated: h; backward: dg), tO1 / tO2 = g / u kept (gated), du (backward, tO1); tP0 / tP1 = g / u read (backward).
+// Maps: tA; tB0 / tB1 = B of the leading / the other CTA (gate and up columns in the gated form, else the same).
+// tO0: y or h; tO1 / tO2: g / u kept (gated).  out: y, h, dpre or dW; pre_out: [g | u] kept or null; pre_in: [g | u] (backward).
 template <int EPI, bool B_MN, int W>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kXThreads)
 expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUtensorMap tB0, const __grid_constant__ CUtensorMap tB1,
                  const __grid_constant__ CUtensorMap tO0, const __grid_constant__ CUtensorMap tO1, const __grid_constant__ CUtensorMap tO2,
-                 const __grid_constant__ CUtensorMap tP0, const __grid_constant__ CUtensorMap tP1, char* out, char* pre_out,
-                 ExpertArgs a, unsigned* error_flag) {
+                 char* __restrict__ out, char* __restrict__ pre_out, const char* __restrict__ pre_in, ExpertArgs a, unsigned* error_flag) {
   constexpr bool kDw = EPI == kEpiDw, kA_MN = kDw;
-  constexpr int kStages = x_stages(W), kStageBytes = x_stage_bytes(W);
+  constexpr int kStages = x_stages(EPI, W), kStageBytes = x_stage_bytes(W);
   constexpr int kTileN = EPI == kEpiGlu ? 128 : kXTile;               // output columns of a tile
   extern __shared__ unsigned char xsm_raw[];
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(xsm_raw) + 1023) & ~(uintptr_t)1023);
@@ -175,7 +176,6 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
     for (int s = 0; s < kStages; ++s) { mbar_init(&sm.full[s], 1); mbar_init(&sm.empty[s], 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(&sm.acc_full[b], 1); mbar_init(&sm.acc_empty[b], 16); }
     mbar_init(&sm.tail, 1); mbar_init(&sm.tail_peer, 1);
-    for (int i = 0; i < 8; ++i) mbar_init(&sm.in[i], 1);
     sm.failed = 0;
     fence_barrier_init();
   }
@@ -330,80 +330,114 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       expert_zero_behind(a, sm.rows, out, 2 * (size_t)(EPI == kEpiDact ? 2 * a.N : a.N), kXTile, worker, workers);
       if (EPI == kEpiGlu && pre_out) expert_zero_behind(a, sm.rows, pre_out, 4 * (size_t)a.N, kXTile, worker, workers);
     }
-    unsigned char* stage = base + kStages * kStageBytes + (size_t)(warp - 2) * 8192;
+    unsigned char* stage = base + kStages * kStageBytes + (size_t)(warp - 2) * x_box_bytes(EPI);
     const uint32_t acc_empty0 = map_to_rank(smem_u32(&sm.acc_empty[0]), 0);
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
-    XWalk<W> walk(sm, a, ntn, pair, pairs);
-    XTile x;
-    uint32_t acc_ph = 0;                                // bit b: parity to wait for at accumulator b
-    int turn = 0, box = 0, in_count = 0; bool ok = true;
-    // a 32-row x 128-byte box in the 128-byte swizzle, out through one TMA store; two boxes alternate
-    auto begin_box = [&]() -> unsigned char* {
+    // A lane computes 128 bytes of its own row; a box of 32 such rows turns them into whole lines for memory.  16-byte chunk c
+    // of row r sits at c ^ (r & 7) (the copy engine's 128-byte swizzle), which spreads both sides over the banks.
+    // y and h leave through tile stores, two boxes in turn: 1 331 TFLOP/s in a long run at E 128, C 4096, 4096 -> 2048 against
+    // 1 260 with stores by the warp (less energy, so a higher clock under the power cap).  dW and the backward of the activation
+    // leave through the warp's own stores: their boxes come faster than the copy engine, busy with operands, takes them.
+    auto to_box = [&](unsigned char* box, int i, uint4 v) { *reinterpret_cast<uint4*>(box + lane * 128 + ((i ^ (lane & 7)) << 4)) = v; };
+    // box -> memory: rows and bytes beyond the tensor are left out; add: fp32 sums instead of stores
+    auto box_out = [&](const unsigned char* box, char* dst, size_t stride, int rows, int bytes, bool add) {
+      __syncwarp();
+      const int c = lane & 7;
+      float4 old[8];
+      if (kDw && add) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = i * 4 + (lane >> 3);
+          if (r < rows && c * 16 < bytes) old[i] = *reinterpret_cast<const float4*>(dst + r * stride + c * 16);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = i * 4 + (lane >> 3);
+        uint4 v = *reinterpret_cast<const uint4*>(box + r * 128 + ((c ^ (r & 7)) << 4));
+        if (r < rows && c * 16 < bytes) {
+          if (kDw && add)
+            v = make_uint4(__float_as_uint(old[i].x + __uint_as_float(v.x)), __float_as_uint(old[i].y + __uint_as_float(v.y)),
+                           __float_as_uint(old[i].z + __uint_as_float(v.z)), __float_as_uint(old[i].w + __uint_as_float(v.w)));
+          *reinterpret_cast<uint4*>(dst + r * stride + c * 16) = v;
+        }
+      }
+      __syncwarp();
+    };
+    int box = 0;
+    auto next_box = [&]() -> unsigned char* {                          // for tile stores: the box the store before last has left
       if (lane == 0 && box >= 2) bulk_wait_read<1>();
       __syncwarp();
       return stage + (box & 1) * 4096;
     };
-    auto end_box = [&](const CUtensorMap* tm, int xx, int yy, int zz, bool in, bool add = false) {
+    auto box_store = [&](const CUtensorMap* tm, int xx, int yy, int zz, bool in) {
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) {
-        const uint32_t src = smem_u32(stage + (box & 1) * 4096);
-        if (in) { if (add) tma_add_3d(tm, xx, yy, zz, src); else tma_store_3d(tm, xx, yy, zz, src); }
+        if (in) tma_store_3d(tm, xx, yy, zz, smem_u32(stage + (box & 1) * 4096));
         bulk_commit();
       }
       ++box;
     };
+    // backward: 64 columns of g and of u into the pair of boxes, 16-byte copies that do not pass the copy engine either
+    auto fetch = [&](size_t row0, int rows, int col) {
+      const int c = lane & 7;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = i * 4 + (lane >> 3);
+        const bool in = r < rows && col + c * 8 < a.N;
+        const char* g = in ? pre_in + ((row0 + r) * 2 * a.N + col + c * 8) * 2 : pre_in;     // out of the tensor: zeros, nothing is read
+        const uint32_t d = smem_u32(stage + r * 128 + ((c ^ (r & 7)) << 4));
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(g), "r"(in ? 16 : 0) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d + 4096), "l"(g + (size_t)a.N * 2), "r"(in ? 16 : 0) : "memory");
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    XWalk<W> walk(sm, a, ntn, pair, pairs);
+    XTile x;
+    uint32_t acc_ph = 0;                                // bit b: parity to wait for at accumulator b
+    int turn = 0; bool ok = true;
     while (ok && walk.next(x)) {
       const int nkb = ((kDw ? x.rows : a.K) + kXBK - 1) / kXBK;
       const int y0 = x.m * kXTile + 128 * rank + 32 * q;              // first row of this warp
+      const int rows = min(32, (kDw ? a.M : a.C) - y0);               // rows of the tensor; may be none
+      const size_t row0 = (size_t)x.e * (kDw ? a.M : a.C) + y0;
       for (int sub = 0; sub < x.subs && ok; ++sub) {
-      const int buf = W == 2 ? sub : turn & 1, xn = x.n + sub;
-      const uint32_t acc = tmem + lanes + (uint32_t)(buf * 256);
-      // backward: a chunk of g and u into the pair of boxes
-      auto fetch = [&](int xx) {
-        if (lane == 0) {
-          uint64_t* bar = &sm.in[warp - 2];
-          bulk_wait_read<0>();                                         // the last boxes have been read by their stores
-          mbar_expect_tx(bar, 8192);
-          tma_load_3d(smem_u32(stage), &tP0, xx, y0, x.e, bar);
-          tma_load_3d(smem_u32(stage) + 4096, &tP1, xx, y0, x.e, bar);
+        const int buf = W == 2 ? sub : turn & 1;
+        const int col0 = EPI == kEpiGlu ? (x.n + sub) * 128 + part * 64 : (x.n + sub) * kXTile + part * 128;
+        const uint32_t acc = tmem + lanes + (uint32_t)(buf * 256) + (EPI == kEpiGlu ? part * 64 : part * 128);
+        const bool keep_row = kDw || y0 + lane < x.rows;              // rows behind the load come out as zeros
+        if (EPI == kEpiDact) fetch(row0, rows, col0);
+        if (nkb > 0) {
+          ok = mbar_wait_bounded(&sm.acc_full[buf], (acc_ph >> buf) & 1);
+          if (!ok) break;
+          tc_fence_after();
         }
-        __syncwarp();
-      };
-      if (EPI == kEpiDact) fetch(xn * kXTile + part * 128);
-      if (nkb > 0) {
-        ok = mbar_wait_bounded(&sm.acc_full[buf], (acc_ph >> buf) & 1);
-        if (!ok) break;
-        tc_fence_after();
-      }
-      if constexpr (kDw) {
-        for (int c0 = part * 128; c0 < part * 128 + 128; c0 += 32) {
-          uint32_t u[2][16];
-          if (nkb > 0) {
-            tmem_ld16_issue(acc + c0, u[0]); tmem_ld16_issue(acc + c0 + 16, u[1]);
-            tmem_ld_wait();
-          } else {
+        if constexpr (kDw) {
+#pragma unroll 1
+          for (int c0 = 0; c0 < 128; c0 += 32) {
+            uint32_t u[2][16];
+            if (nkb > 0) {
+              tmem_ld16_issue(acc + c0, u[0]); tmem_ld16_issue(acc + c0 + 16, u[1]);
+              tmem_ld_wait();
+            } else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) u[0][i] = u[1][i] = 0;
+              for (int i = 0; i < 16; ++i) u[0][i] = u[1][i] = 0;
+            }
+            if (nkb == 0 && a.accumulate) continue;                    // an expert without rows adds nothing
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              to_box(stage, i, make_uint4(u[i >> 2][(i & 3) * 4], u[i >> 2][(i & 3) * 4 + 1], u[i >> 2][(i & 3) * 4 + 2], u[i >> 2][(i & 3) * 4 + 3]));
+            box_out(stage, out + (row0 * a.N + col0 + c0) * 4, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 4, a.accumulate != 0);
           }
-          unsigned char* row = begin_box() + lane * 128;
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            *reinterpret_cast<uint4*>(row + ((i ^ (lane & 7)) << 4)) =
-                make_uint4(u[i >> 2][(i & 3) * 4], u[i >> 2][(i & 3) * 4 + 1], u[i >> 2][(i & 3) * 4 + 2], u[i >> 2][(i & 3) * 4 + 3]);
-          const int xx = xn * kXTile + c0;
-          end_box(&tO0, xx, y0, x.e, xx < a.N && y0 < a.M && (nkb > 0 || !a.accumulate), a.accumulate);
-        }
-      } else {
-        const bool keep_row = y0 + lane < x.rows;                      // rows behind the load come out as zeros
-        const bool in_y = y0 < a.C;
-        if constexpr (EPI == kEpiPlain) {
-          for (int c0 = part * 128; c0 < part * 128 + 128; c0 += 64) {
+        } else if constexpr (EPI == kEpiPlain) {
+#pragma unroll 1
+          for (int c0 = 0; c0 < 128; c0 += 64) {
             uint32_t u[4][16];
 #pragma unroll
             for (int i = 0; i < 4; ++i) tmem_ld16_issue(acc + c0 + 16 * i, u[i]);
             tmem_ld_wait();
-            unsigned char* row = begin_box() + lane * 128;
+            unsigned char* to = next_box();
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               uint32_t w[4];
@@ -412,99 +446,84 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
                 const int at = (i & 1) * 8 + 2 * j;
                 w[j] = keep_row ? pack_bf16(__uint_as_float(u[i >> 1][at]), __uint_as_float(u[i >> 1][at + 1])) : 0u;
               }
-              *reinterpret_cast<uint4*>(row + ((i ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+              to_box(to, i, make_uint4(w[0], w[1], w[2], w[3]));
             }
-            const int xx = xn * kXTile + c0;
-            end_box(&tO0, xx, y0, x.e, in_y && xx < a.N);
+            box_store(&tO0, col0 + c0, y0, x.e, rows > 0 && col0 + c0 < a.N);
           }
         } else if constexpr (EPI == kEpiGlu) {
-          {
-            const int c0 = part * 64, xx = xn * 128 + c0;
-            uint32_t hw[32], gw[32], uw[32];
+          uint32_t hw[32], gw[32], uw[32];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              uint32_t g[2][16], u[2][16];
+          for (int half = 0; half < 2; ++half) {
+            uint32_t g[2][16], u[2][16];
 #pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                tmem_ld16_issue(acc + c0 + half * 32 + 16 * i, g[i]);
-                tmem_ld16_issue(acc + 128 + c0 + half * 32 + 16 * i, u[i]);
-              }
-              tmem_ld_wait();
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const float g0 = __uint_as_float(g[i >> 3][(i & 7) * 2]), g1 = __uint_as_float(g[i >> 3][(i & 7) * 2 + 1]);
-                const float u0 = __uint_as_float(u[i >> 3][(i & 7) * 2]), u1 = __uint_as_float(u[i >> 3][(i & 7) * 2 + 1]);
-                hw[half * 16 + i] = keep_row ? pack_bf16(silu_mul<true>(g0, u0), silu_mul<true>(g1, u1)) : 0u;
-                gw[half * 16 + i] = keep_row ? pack_bf16(g0, g1) : 0u;
-                uw[half * 16 + i] = keep_row ? pack_bf16(u0, u1) : 0u;
-              }
+            for (int i = 0; i < 2; ++i) {
+              tmem_ld16_issue(acc + half * 32 + 16 * i, g[i]);
+              tmem_ld16_issue(acc + 128 + half * 32 + 16 * i, u[i]);
             }
-            auto emit = [&](const CUtensorMap* tm, const uint32_t (&w)[32]) {
-              unsigned char* row = begin_box() + lane * 128;
+            tmem_ld_wait();
 #pragma unroll
-              for (int i = 0; i < 8; ++i)
-                *reinterpret_cast<uint4*>(row + ((i ^ (lane & 7)) << 4)) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-              end_box(tm, xx, y0, x.e, in_y && xx < a.N);
-            };
-            emit(&tO0, hw);
-            if (pre_out) { emit(&tO1, gw); emit(&tO2, uw); }
+            for (int i = 0; i < 16; ++i) {
+              const float g0 = __uint_as_float(g[i >> 3][(i & 7) * 2]), g1 = __uint_as_float(g[i >> 3][(i & 7) * 2 + 1]);
+              const float u0 = __uint_as_float(u[i >> 3][(i & 7) * 2]), u1 = __uint_as_float(u[i >> 3][(i & 7) * 2 + 1]);
+              hw[half * 16 + i] = keep_row ? pack_bf16(silu_mul<true>(g0, u0), silu_mul<true>(g1, u1)) : 0u;
+              gw[half * 16 + i] = keep_row ? pack_bf16(g0, g1) : 0u;
+              uw[half * 16 + i] = keep_row ? pack_bf16(u0, u1) : 0u;
+            }
           }
+          auto emit = [&](const CUtensorMap* tm, const uint32_t (&w)[32]) {
+            unsigned char* to = next_box();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) to_box(to, i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+            box_store(tm, col0, y0, x.e, rows > 0 && col0 < a.N);
+          };
+          emit(&tO0, hw);
+          if (pre_out) { emit(&tO1, gw); emit(&tO2, uw); }
         } else {
-          // dh in the accumulator; g and u come in through a pair of boxes, which dg and du then leave from
-          for (int c = part * 2; c < part * 2 + 2 && ok; ++c) {
-            const int xx = xn * kXTile + c * 64;
-            if (c & 1) fetch(xx);                                      // the first one was asked for ahead of the accumulator
-            ok = mbar_wait_bounded(&sm.in[warp - 2], (uint32_t)(in_count & 1));
-            ++in_count;
-            if (!ok) break;
+          // dh in the accumulator; g and u sit in a pair of boxes, which dg and du then leave from
+#pragma unroll 1
+          for (int c0 = 0; c0 < 128; c0 += 64) {
+            if (c0) fetch(row0, rows, col0 + c0);                      // the first one was asked for ahead of the accumulator
+            uint32_t u[4][16];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tmem_ld16_issue(acc + c0 + 16 * i, u[i]);
+            tmem_ld_wait();
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncwarp();
             unsigned char* row = stage + lane * 128;
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              uint32_t u[2][16];
-              tmem_ld16_issue(acc + c * 64 + half * 32, u[0]); tmem_ld16_issue(acc + c * 64 + half * 32 + 16, u[1]);
-              tmem_ld_wait();
+            for (int i = 0; i < 8; ++i) {
+              uint4* pg = reinterpret_cast<uint4*>(row + ((i ^ (lane & 7)) << 4));
+              uint4* pu = reinterpret_cast<uint4*>(row + 4096 + ((i ^ (lane & 7)) << 4));
+              float g[8], up[8];
+              Vec16<__nv_bfloat16>::unpack(*pg, g); Vec16<__nv_bfloat16>::unpack(*pu, up);
+              uint32_t wg[4], wu[4];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                uint4* pg = reinterpret_cast<uint4*>(row + (((half * 4 + i) ^ (lane & 7)) << 4));
-                uint4* pu = reinterpret_cast<uint4*>(row + 4096 + (((half * 4 + i) ^ (lane & 7)) << 4));
-                float g[8], up[8];
-                Vec16<__nv_bfloat16>::unpack(*pg, g); Vec16<__nv_bfloat16>::unpack(*pu, up);
-                uint32_t wg[4], wu[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  float d0, d1, e0, e1;
-                  const int at = (i & 1) * 8 + 2 * j;
-                  dact<true>(__uint_as_float(u[i >> 1][at]), g[2 * j], up[2 * j], d0, e0);
-                  dact<true>(__uint_as_float(u[i >> 1][at + 1]), g[2 * j + 1], up[2 * j + 1], d1, e1);
-                  wg[j] = keep_row ? pack_bf16(d0, d1) : 0u;
-                  wu[j] = keep_row ? pack_bf16(e0, e1) : 0u;
-                }
-                *pg = make_uint4(wg[0], wg[1], wg[2], wg[3]);
-                *pu = make_uint4(wu[0], wu[1], wu[2], wu[3]);
+              for (int j = 0; j < 4; ++j) {
+                float d0, d1, e0, e1;
+                const int at = (i & 1) * 8 + 2 * j;
+                dact<true>(__uint_as_float(u[i >> 1][at]), g[2 * j], up[2 * j], d0, e0);
+                dact<true>(__uint_as_float(u[i >> 1][at + 1]), g[2 * j + 1], up[2 * j + 1], d1, e1);
+                wg[j] = keep_row ? pack_bf16(d0, d1) : 0u;
+                wu[j] = keep_row ? pack_bf16(e0, e1) : 0u;
               }
+              *pg = make_uint4(wg[0], wg[1], wg[2], wg[3]);
+              *pu = make_uint4(wu[0], wu[1], wu[2], wu[3]);
             }
-            fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) {
-              if (in_y && xx < a.N) {
-                const uint32_t src = smem_u32(stage);
-                tma_store_3d(&tO0, xx, y0, x.e, src);
-                tma_store_3d(&tO1, xx, y0, x.e, src + 4096);
-              }
-              bulk_commit();
-            }
+            char* dst = out + (row0 * 2 * a.N + col0 + c0) * 2;
+            box_out(stage, dst, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 2, false);
+            box_out(stage + 4096, dst + (size_t)a.N * 2, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 2, false);
           }
         }
-      }
-      if (nkb > 0) {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(acc_empty0 + 8u * (uint32_t)buf);
-        acc_ph ^= 1u << buf;
-      }
+        if (nkb > 0) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster_relaxed(acc_empty0 + 8u * (uint32_t)buf);
+          acc_ph ^= 1u << buf;
+        }
       }
       if (nkb > 0) ++turn;
     }
+    if (EPI == kEpiDact) asm volatile("cp.async.wait_group 0;" ::: "memory");
     if (lane == 0) bulk_wait_all<0>();
     if (!ok && lane == 0) sm.failed = 1;
   }

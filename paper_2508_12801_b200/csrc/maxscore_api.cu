@@ -213,18 +213,17 @@ maxscore_status make_tmap_bf16(const maxscore_ctx* c, CUtensorMap* tm, const voi
 }
 
 // One matrix per expert: [E][rows][inner] with given strides, boxes of one expert each, 128-byte swizzle.  chunks: the
-// 64-column chunks are a dimension of their own and a box takes two of them (inner % 64 == 0, bf16).
-maxscore_status make_tmap_expert(const maxscore_ctx* c, CUtensorMap* tm, bool f32, const void* base, uint64_t inner, uint64_t rows,
+// 64-column chunks are a dimension of their own and a box takes two of them (inner % 64 == 0).
+maxscore_status make_tmap_expert(const maxscore_ctx* c, CUtensorMap* tm, const void* base, uint64_t inner, uint64_t rows,
                                  uint64_t row_stride, uint64_t expert_stride, uint32_t box_rows, bool chunks = false) {
-  const uint64_t b = f32 ? 4 : 2, E = (uint64_t)c->p.E;
+  const uint64_t E = (uint64_t)c->p.E;
   cuuint64_t dims3[3] = {inner, rows, E}, dims4[4] = {64, rows, inner / 64, E};
-  cuuint64_t strides3[2] = {row_stride * b, expert_stride * b}, strides4[3] = {row_stride * b, 128, expert_stride * b};
-  cuuint32_t box3[3] = {(cuuint32_t)(128 / b), box_rows, 1}, box4[4] = {64, box_rows, 2, 1};
+  cuuint64_t strides3[2] = {row_stride * 2, expert_stride * 2}, strides4[3] = {row_stride * 2, 128, expert_stride * 2};
+  cuuint32_t box3[3] = {64, box_rows, 1}, box4[4] = {64, box_rows, 2, 1};
   cuuint32_t estr[4] = {1, 1, 1, 1};
-  CUresult r = c->encode(tm, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, chunks ? 4 : 3,
-                         const_cast<void*>(base), chunks ? dims4 : dims3, chunks ? strides4 : strides3, chunks ? box4 : box3, estr,
-                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  CUresult r = c->encode(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, chunks ? 4 : 3, const_cast<void*>(base), chunks ? dims4 : dims3,
+                         chunks ? strides4 : strides3, chunks ? box4 : box3, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
     snprintf(g_last_error, sizeof(g_last_error), "cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
     return MAXSCORE_ERR_CUDA;
@@ -505,13 +504,13 @@ maxscore_status maxscore_create(maxscore_ctx** out, const maxscore_params* param
   {
     cudaError_t e_ = cudaSuccess;
     auto room = [&](auto kernel, int bytes) { if (e_ == cudaSuccess) e_ = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
-    room(expert_tc_kernel<kEpiPlain, false, 1>, x_smem(1)); room(expert_tc_kernel<kEpiPlain, false, 2>, x_smem(2));
-    room(expert_tc_kernel<kEpiPlain, true, 1>, x_smem(1)); room(expert_tc_kernel<kEpiPlain, true, 2>, x_smem(2));
-    room(expert_tc_kernel<kEpiGlu, false, 1>, x_smem(1)); room(expert_tc_kernel<kEpiGlu, false, 2>, x_smem(2));
-    room(expert_tc_kernel<kEpiGlu, true, 1>, x_smem(1)); room(expert_tc_kernel<kEpiGlu, true, 2>, x_smem(2));
-    room(expert_tc_kernel<kEpiDact, false, 1>, x_smem(1)); room(expert_tc_kernel<kEpiDact, false, 2>, x_smem(2));
-    room(expert_tc_kernel<kEpiDact, true, 1>, x_smem(1)); room(expert_tc_kernel<kEpiDact, true, 2>, x_smem(2));
-    room(expert_tc_kernel<kEpiDw, true, 1>, x_smem(1)); room(expert_tc_kernel<kEpiDw, true, 2>, x_smem(2));
+    room(expert_tc_kernel<kEpiPlain, false, 1>, x_smem(kEpiPlain, 1)); room(expert_tc_kernel<kEpiPlain, false, 2>, x_smem(kEpiPlain, 2));
+    room(expert_tc_kernel<kEpiPlain, true, 1>, x_smem(kEpiPlain, 1)); room(expert_tc_kernel<kEpiPlain, true, 2>, x_smem(kEpiPlain, 2));
+    room(expert_tc_kernel<kEpiGlu, false, 1>, x_smem(kEpiGlu, 1)); room(expert_tc_kernel<kEpiGlu, false, 2>, x_smem(kEpiGlu, 2));
+    room(expert_tc_kernel<kEpiGlu, true, 1>, x_smem(kEpiGlu, 1)); room(expert_tc_kernel<kEpiGlu, true, 2>, x_smem(kEpiGlu, 2));
+    room(expert_tc_kernel<kEpiDact, false, 1>, x_smem(kEpiDact, 1)); room(expert_tc_kernel<kEpiDact, false, 2>, x_smem(kEpiDact, 2));
+    room(expert_tc_kernel<kEpiDact, true, 1>, x_smem(kEpiDact, 1)); room(expert_tc_kernel<kEpiDact, true, 2>, x_smem(kEpiDact, 2));
+    room(expert_tc_kernel<kEpiDw, true, 1>, x_smem(kEpiDw, 1)); room(expert_tc_kernel<kEpiDw, true, 2>, x_smem(kEpiDw, 2));
     if (e_ != cudaSuccess) return cuda_fail(e_, "cudaFuncSetAttribute(expert_tc_kernel)");
   }
   int coop = 0, sweep_occ = 0;
@@ -1040,45 +1039,37 @@ maxscore_status launch_tc(maxscore_ctx* c, const void* A, const void* B, const v
   a.b_chunks = B_MN && a.N % 64 == 0;
   const uint64_t C = (uint64_t)c->C, M = (uint64_t)a.M, N = (uint64_t)a.N, K = (uint64_t)a.K;
   typedef const __nv_bfloat16* P;
-  CUtensorMap tA, tB0, tB1, tO0, tO1, tO2, tP0, tP1;
+  CUtensorMap tA, tB0, tB1, tO0, tO1, tO2;
   maxscore_status s;
 #define MS_MAP(...) do { s = make_tmap_expert(c, __VA_ARGS__); if (s) return s; } while (0)
   if (kDw) {
-    MS_MAP(&tA, false, A, M, C, M, C * M, 64, a.a_chunks);
-    MS_MAP(&tB0, false, B, N, C, N, C * N, 64, a.b_chunks);
+    MS_MAP(&tA, A, M, C, M, C * M, 64, a.a_chunks);
+    MS_MAP(&tB0, B, N, C, N, C * N, 64, a.b_chunks);
     tB1 = tB0;
-    MS_MAP(&tO0, true, out, N, M, N, M * N, 32);
   } else {
-    MS_MAP(&tA, false, A, K, C, K, C * K, 128);
+    MS_MAP(&tA, A, K, C, K, C * K, 128);
     const uint64_t cols = EPI == kEpiGlu ? 2 * N : N;
-    if (B_MN) MS_MAP(&tB0, false, B, N, K, cols, K * cols, 64, a.b_chunks);
-    else MS_MAP(&tB0, false, B, K, N, K, cols * K, 128);
+    if (B_MN) MS_MAP(&tB0, B, N, K, cols, K * cols, 64, a.b_chunks);
+    else MS_MAP(&tB0, B, K, N, K, cols * K, 128);
     tB1 = tB0;
     if (EPI == kEpiGlu) {
-      if (B_MN) MS_MAP(&tB1, false, (P)B + N, N, K, cols, K * cols, 64, a.b_chunks);
-      else MS_MAP(&tB1, false, (P)B + N * K, K, N, K, cols * K, 128);
+      if (B_MN) MS_MAP(&tB1, (P)B + N, N, K, cols, K * cols, 64, a.b_chunks);
+      else MS_MAP(&tB1, (P)B + N * K, K, N, K, cols * K, 128);
     }
-    if (EPI == kEpiDact) {
-      MS_MAP(&tO0, false, out, N, C, 2 * N, C * 2 * N, 32);
-      MS_MAP(&tO1, false, (P)out + N, N, C, 2 * N, C * 2 * N, 32);
-      MS_MAP(&tP0, false, pre_in, N, C, 2 * N, C * 2 * N, 32);
-      MS_MAP(&tP1, false, (P)pre_in + N, N, C, 2 * N, C * 2 * N, 32);
-    } else {
-      MS_MAP(&tO0, false, out, N, C, N, C * N, 32);
-    }
+    if (EPI != kEpiDact) MS_MAP(&tO0, out, N, C, N, C * N, 32);
     if (EPI == kEpiGlu && pre_out) {
-      MS_MAP(&tO1, false, pre_out, N, C, 2 * N, C * 2 * N, 32);
-      MS_MAP(&tO2, false, (P)pre_out + N, N, C, 2 * N, C * 2 * N, 32);
+      MS_MAP(&tO1, pre_out, N, C, 2 * N, C * 2 * N, 32);
+      MS_MAP(&tO2, (P)pre_out + N, N, C, 2 * N, C * 2 * N, 32);
     }
   }
 #undef MS_MAP
-  if (EPI != kEpiDact) { tP0 = tP1 = tO0; if (!pre_out) tO1 = tO0; }
-  if (EPI != kEpiGlu || !pre_out) tO2 = tO0;
+  if (kDw || EPI == kEpiDact) tO0 = tA;                  // not used
+  if (EPI != kEpiGlu || !pre_out) tO1 = tO2 = tO0;       // not used
   const long long tile_n = EPI == kEpiGlu ? 128 : kXTile;
   const long long tiles = (long long)a.E * (((kDw ? M : C) + kXTile - 1) / kXTile) * ((N + tile_n - 1) / tile_n);
   const int pairs = (int)std::min<long long>(c->sm_count / 2, tiles);
   auto go = [&](auto kernel, int w) {
-    kernel<<<2 * pairs, kXThreads, x_smem(w), st>>>(tA, tB0, tB1, tO0, tO1, tO2, tP0, tP1, (char*)out, (char*)pre_out, a, error_flag_of(c));
+    kernel<<<2 * pairs, kXThreads, x_smem(EPI, w), st>>>(tA, tB0, tB1, tO0, tO1, tO2, (char*)out, (char*)pre_out, (const char*)pre_in, a, error_flag_of(c));
   };
   static const int force = getenv("XW") ? atoi(getenv("XW")) : 2;
   if (force == 2) go(expert_tc_kernel<EPI, B_MN, 2>, 2);
