@@ -5,7 +5,7 @@
 // That halves the operand traffic per flop of a single CTA's 128 x 256 tile (64 bytes per clock and SM at full rate instead
 // of 96, which the L2 cannot deliver).  Two accumulators alternate, so the epilogue of a tile runs under the MMAs of the next.
 //   warp 0: TMA loads, six (five) stages of 64-deep slices;  warp 1: TMEM, and in the leading CTA the MMAs;
-//   warps 2-9: epilogue, a TMEM lane quarter and half of the columns each, out through staging boxes as whole lines.
+//   the other eight (sixteen): epilogue, a TMEM lane quarter and a part of the columns each, out through staging boxes.
 // Both operand majors are read in place through the descriptors: no weight is ever transposed.
 //
 // Ragged loads.  Rows: a tile is whole or partial, rows behind the load come out as zeros.  Contraction over rows (dW): the
@@ -81,13 +81,19 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {     // arrives
 }
 
 // ---- the kernel ----------------------------------------------------------------------------------------------------
-constexpr int kXThreads = 320, kXTile = 256, kXBK = 64;
+constexpr int kXTile = 256, kXBK = 64;
 // W: column tiles of a pair at a time (1: 256 x 256, two accumulators in turn; 2: 256 x 512)
 __host__ __device__ constexpr int x_stage_bytes(int w) { return 16384 * (1 + w); }
-// Staging of an epilogue warp: 4 KB boxes, one for dW, a pair for the others.
-__host__ __device__ constexpr int x_box_bytes(int epi) { return epi == kEpiDw ? 4096 : 8192; }
+// Epilogue warps: two for each of the four TMEM lane quarters; four in the backward of the activation, whose epilogue (two
+// operands in, two results out, an exponential and a quotient each) is what bounds it up to K of a few thousand.
+__host__ __device__ constexpr int x_epi_warps(int epi) { return epi == kEpiDact ? 16 : 8; }
+__host__ __device__ constexpr int x_threads(int epi) { return 64 + 32 * x_epi_warps(epi); }
+// Staging of an epilogue warp: boxes of 32 rows of 128 bytes (64 bytes in the backward), one for dW, a pair for the others.
+__host__ __device__ constexpr int x_box_bytes(int epi) { return epi == kEpiDw || epi == kEpiDact ? 4096 : 8192; }
 __host__ __device__ constexpr int x_stages(int epi, int w) { return (w == 2 ? 3 : 5) + (epi == kEpiDw ? 1 : 0); }
-__host__ __device__ constexpr int x_smem(int epi, int w) { return x_stages(epi, w) * x_stage_bytes(w) + 8 * x_box_bytes(epi) + 1024; }
+__host__ __device__ constexpr int x_smem(int epi, int w) {
+  return x_stages(epi, w) * x_stage_bytes(w) + x_epi_warps(epi) * x_box_bytes(epi) + 1024;
+}
 
 struct XSmem {
   uint64_t full[6], empty[6], acc_full[2], acc_empty[2], tail, tail_peer;
@@ -158,11 +164,12 @@ __device__ __forceinline__ void expert_prefix(const ExpertArgs& a, int* rows, in
 // Maps: tA; tB0 / tB1 = B of the leading / the other CTA (gate and up columns in the gated form, else the same).
 // tO0: y or h; tO1 / tO2: g / u kept (gated).  out: y, h, dpre or dW; pre_out: [g | u] kept or null; pre_in: [g | u] (backward).
 template <int EPI, bool B_MN, int W>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kXThreads)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(x_threads(EPI))
 expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUtensorMap tB0, const __grid_constant__ CUtensorMap tB1,
                  const __grid_constant__ CUtensorMap tO0, const __grid_constant__ CUtensorMap tO1, const __grid_constant__ CUtensorMap tO2,
                  char* __restrict__ out, char* __restrict__ pre_out, const char* __restrict__ pre_in, ExpertArgs a, unsigned* error_flag) {
   constexpr bool kDw = EPI == kEpiDw, kA_MN = kDw;
+  constexpr int kEpiWarps = x_epi_warps(EPI);
   constexpr int kStages = x_stages(EPI, W), kStageBytes = x_stage_bytes(W);
   constexpr int kTileN = EPI == kEpiGlu ? 128 : kXTile;               // output columns of a tile
   extern __shared__ unsigned char xsm_raw[];
@@ -174,7 +181,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) { mbar_init(&sm.full[s], 1); mbar_init(&sm.empty[s], 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(&sm.acc_full[b], 1); mbar_init(&sm.acc_empty[b], 16); }
+    for (int b = 0; b < 2; ++b) { mbar_init(&sm.acc_full[b], 1); mbar_init(&sm.acc_empty[b], 2 * kEpiWarps); }
     mbar_init(&sm.tail, 1); mbar_init(&sm.tail_peer, 1);
     sm.failed = 0;
     fence_barrier_init();
@@ -324,9 +331,9 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
     if (!ok && lane == 0) sm.failed = 1;
   } else if (warp >= 2) {
     // ---- epilogue ------------------------------------------------------------------------------------------------------
-    const int q = warp & 3, part = (warp - 2) >> 2;     // TMEM lanes this warp may read; its half of a tile's columns
+    const int q = warp & 3, part = (warp - 2) >> 2;     // TMEM lanes this warp may read; its part of a tile's columns
     if constexpr (!kDw) {
-      const int worker = blockIdx.x * 256 + (warp - 2) * 32 + lane, workers = gridDim.x * 256;
+      const int worker = (blockIdx.x * kEpiWarps + warp - 2) * 32 + lane, workers = gridDim.x * kEpiWarps * 32;
       expert_zero_behind(a, sm.rows, out, 2 * (size_t)(EPI == kEpiDact ? 2 * a.N : a.N), kXTile, worker, workers);
       if (EPI == kEpiGlu && pre_out) expert_zero_behind(a, sm.rows, pre_out, 4 * (size_t)a.N, kXTile, worker, workers);
     }
@@ -338,23 +345,25 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
     // y and h leave through tile stores, two boxes in turn: 1 331 TFLOP/s in a long run at E 128, C 4096, 4096 -> 2048 against
     // 1 260 with stores by the warp (less energy, so a higher clock under the power cap).  dW and the backward of the activation
     // leave through the warp's own stores: their boxes come faster than the copy engine, busy with operands, takes them.
-    auto to_box = [&](unsigned char* box, int i, uint4 v) { *reinterpret_cast<uint4*>(box + lane * 128 + ((i ^ (lane & 7)) << 4)) = v; };
+    constexpr int kRow = EPI == kEpiDact ? 64 : 128, kPer = kRow / 16, kRows = 32 / kPer;      // bytes of a box row; chunks; rows a warp moves at once
+    auto swz = [](int r) { return kRow == 128 ? r & 7 : (r >> 1) & 3; };
+    auto to_box = [&](unsigned char* box, int i, uint4 v) { *reinterpret_cast<uint4*>(box + lane * kRow + ((i ^ swz(lane)) << 4)) = v; };
     // box -> memory: rows and bytes beyond the tensor are left out; add: fp32 sums instead of stores
     auto box_out = [&](const unsigned char* box, char* dst, size_t stride, int rows, int bytes, bool add) {
       __syncwarp();
-      const int c = lane & 7;
-      float4 old[8];
+      const int c = lane % kPer;
+      float4 old[kPer];
       if (kDw && add) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int r = i * 4 + (lane >> 3);
+        for (int i = 0; i < kPer; ++i) {
+          const int r = i * kRows + lane / kPer;
           if (r < rows && c * 16 < bytes) old[i] = *reinterpret_cast<const float4*>(dst + r * stride + c * 16);
         }
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = i * 4 + (lane >> 3);
-        uint4 v = *reinterpret_cast<const uint4*>(box + r * 128 + ((c ^ (r & 7)) << 4));
+      for (int i = 0; i < kPer; ++i) {
+        const int r = i * kRows + lane / kPer;
+        uint4 v = *reinterpret_cast<const uint4*>(box + r * kRow + ((c ^ swz(r)) << 4));
         if (r < rows && c * 16 < bytes) {
           if (kDw && add)
             v = make_uint4(__float_as_uint(old[i].x + __uint_as_float(v.x)), __float_as_uint(old[i].y + __uint_as_float(v.y)),
@@ -379,17 +388,17 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       }
       ++box;
     };
-    // backward: 64 columns of g and of u into the pair of boxes, 16-byte copies that do not pass the copy engine either
+    // backward: 32 columns of g and of u into the pair of boxes, 16-byte copies that do not pass the copy engine either
     auto fetch = [&](size_t row0, int rows, int col) {
-      const int c = lane & 7;
+      const int c = lane % kPer;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = i * 4 + (lane >> 3);
+      for (int i = 0; i < kPer; ++i) {
+        const int r = i * kRows + lane / kPer;
         const bool in = r < rows && col + c * 8 < a.N;
         const char* g = in ? pre_in + ((row0 + r) * 2 * a.N + col + c * 8) * 2 : pre_in;     // out of the tensor: zeros, nothing is read
-        const uint32_t d = smem_u32(stage + r * 128 + ((c ^ (r & 7)) << 4));
+        const uint32_t d = smem_u32(stage + r * kRow + ((c ^ swz(r)) << 4));
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(g), "r"(in ? 16 : 0) : "memory");
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d + 4096), "l"(g + (size_t)a.N * 2), "r"(in ? 16 : 0) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d + 32 * kRow), "l"(g + (size_t)a.N * 2), "r"(in ? 16 : 0) : "memory");
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -404,8 +413,9 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       const size_t row0 = (size_t)x.e * (kDw ? a.M : a.C) + y0;
       for (int sub = 0; sub < x.subs && ok; ++sub) {
         const int buf = W == 2 ? sub : turn & 1;
-        const int col0 = EPI == kEpiGlu ? (x.n + sub) * 128 + part * 64 : (x.n + sub) * kXTile + part * 128;
-        const uint32_t acc = tmem + lanes + (uint32_t)(buf * 256) + (EPI == kEpiGlu ? part * 64 : part * 128);
+        constexpr int kTileCols = EPI == kEpiGlu ? 128 : kXTile, kCols = kTileCols / (kEpiWarps / 4);     // columns of this warp
+        const int col0 = (x.n + sub) * kTileCols + part * kCols;
+        const uint32_t acc = tmem + lanes + (uint32_t)(buf * 256 + part * kCols);
         const bool keep_row = kDw || y0 + lane < x.rows;              // rows behind the load come out as zeros
         if (EPI == kEpiDact) fetch(row0, rows, col0);
         if (nkb > 0) {
@@ -481,19 +491,18 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
         } else {
           // dh in the accumulator; g and u sit in a pair of boxes, which dg and du then leave from
 #pragma unroll 1
-          for (int c0 = 0; c0 < 128; c0 += 64) {
+          for (int c0 = 0; c0 < kCols; c0 += 32) {
             if (c0) fetch(row0, rows, col0 + c0);                      // the first one was asked for ahead of the accumulator
-            uint32_t u[4][16];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) tmem_ld16_issue(acc + c0 + 16 * i, u[i]);
+            uint32_t u[2][16];
+            tmem_ld16_issue(acc + c0, u[0]); tmem_ld16_issue(acc + c0 + 16, u[1]);
             tmem_ld_wait();
             asm volatile("cp.async.wait_group 0;" ::: "memory");
             __syncwarp();
-            unsigned char* row = stage + lane * 128;
+            unsigned char* row = stage + lane * kRow;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              uint4* pg = reinterpret_cast<uint4*>(row + ((i ^ (lane & 7)) << 4));
-              uint4* pu = reinterpret_cast<uint4*>(row + 4096 + ((i ^ (lane & 7)) << 4));
+            for (int i = 0; i < 4; ++i) {
+              uint4* pg = reinterpret_cast<uint4*>(row + ((i ^ swz(lane)) << 4));
+              uint4* pu = reinterpret_cast<uint4*>(row + 32 * kRow + ((i ^ swz(lane)) << 4));
               float g[8], up[8];
               Vec16<__nv_bfloat16>::unpack(*pg, g); Vec16<__nv_bfloat16>::unpack(*pu, up);
               uint32_t wg[4], wu[4];
@@ -511,7 +520,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
             }
             char* dst = out + (row0 * 2 * a.N + col0 + c0) * 2;
             box_out(stage, dst, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 2, false);
-            box_out(stage + 4096, dst + (size_t)a.N * 2, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 2, false);
+            box_out(stage + 32 * kRow, dst + (size_t)a.N * 2, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 2, false);
           }
         }
         if (nkb > 0) {

@@ -6,7 +6,6 @@
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdio.h>
-#include <stdlib.h>
 #include <string.h>
 
 #include <algorithm>
@@ -508,9 +507,8 @@ maxscore_status maxscore_create(maxscore_ctx** out, const maxscore_params* param
     room(expert_tc_kernel<kEpiPlain, true, 1>, x_smem(kEpiPlain, 1)); room(expert_tc_kernel<kEpiPlain, true, 2>, x_smem(kEpiPlain, 2));
     room(expert_tc_kernel<kEpiGlu, false, 1>, x_smem(kEpiGlu, 1)); room(expert_tc_kernel<kEpiGlu, false, 2>, x_smem(kEpiGlu, 2));
     room(expert_tc_kernel<kEpiGlu, true, 1>, x_smem(kEpiGlu, 1)); room(expert_tc_kernel<kEpiGlu, true, 2>, x_smem(kEpiGlu, 2));
-    room(expert_tc_kernel<kEpiDact, false, 1>, x_smem(kEpiDact, 1)); room(expert_tc_kernel<kEpiDact, false, 2>, x_smem(kEpiDact, 2));
-    room(expert_tc_kernel<kEpiDact, true, 1>, x_smem(kEpiDact, 1)); room(expert_tc_kernel<kEpiDact, true, 2>, x_smem(kEpiDact, 2));
-    room(expert_tc_kernel<kEpiDw, true, 1>, x_smem(kEpiDw, 1)); room(expert_tc_kernel<kEpiDw, true, 2>, x_smem(kEpiDw, 2));
+    room(expert_tc_kernel<kEpiDact, false, 1>, x_smem(kEpiDact, 1)); room(expert_tc_kernel<kEpiDact, true, 1>, x_smem(kEpiDact, 1));
+    room(expert_tc_kernel<kEpiDw, true, 2>, x_smem(kEpiDw, 2));
     if (e_ != cudaSuccess) return cuda_fail(e_, "cudaFuncSetAttribute(expert_tc_kernel)");
   }
   int coop = 0, sweep_occ = 0;
@@ -1069,10 +1067,15 @@ maxscore_status launch_tc(maxscore_ctx* c, const void* A, const void* B, const v
   const long long tiles = (long long)a.E * (((kDw ? M : C) + kXTile - 1) / kXTile) * ((N + tile_n - 1) / tile_n);
   const int pairs = (int)std::min<long long>(c->sm_count / 2, tiles);
   auto go = [&](auto kernel, int w) {
-    kernel<<<2 * pairs, kXThreads, x_smem(EPI, w), st>>>(tA, tB0, tB1, tO0, tO1, tO2, (char*)out, (char*)pre_out, (const char*)pre_in, a, error_flag_of(c));
+    kernel<<<2 * pairs, x_threads(EPI), x_smem(EPI, w), st>>>(tA, tB0, tB1, tO0, tO1, tO2, (char*)out, (char*)pre_out, (const char*)pre_in, a, error_flag_of(c));
   };
-  static const int force = getenv("XW") ? atoi(getenv("XW")) : 2;
-  if (force == 2) go(expert_tc_kernel<EPI, B_MN, 2>, 2);
+  // Two column tiles at a time read a quarter less per flop, but their epilogues hide less well.  Long runs, 256 x 512 against
+  // 256 x 256: y at C 4096, K 4096 1 248 / 1 234 TFLOP/s, at C 1024, K 2048 1 150 / 1 145, K 1024 1 041 / 1 055, K 512 853 / 904;
+  // h 1 286 / 1 257 at K 4096, 1 125 / 1 178 at K 2048.  dW gains at every size (4096 x 2048 over 4096 rows: 1 187 / 1 000,
+  // over 300 rows 434 / 388); the backward of the activation loses at every size (1 022 / 1 058 at K 4096, 561 / 705 at 1024).
+  if constexpr (kDw) go(expert_tc_kernel<EPI, B_MN, 2>, 2);
+  else if constexpr (EPI == kEpiDact) go(expert_tc_kernel<EPI, B_MN, 1>, 1);
+  else if (a.K >= 4096 && tiles >= 4 * pairs) go(expert_tc_kernel<EPI, B_MN, 2>, 2);
   else go(expert_tc_kernel<EPI, B_MN, 1>, 1);
   MS_LAUNCH_CHECK("expert_tc_kernel");
   c->launches += 1;
