@@ -57,6 +57,17 @@ __device__ void expert_zero_behind(const ExpertArgs& a, const int* rows, char* y
   }
 }
 
+// The same where rows are few: a warp per row of the whole buffer, so that many experts with next to nothing cost one step.
+__device__ void expert_zero_behind_rows(const ExpertArgs& a, const int* rows, char* y, size_t row_bytes, int warp, int warps) {
+  const int vecs = (int)(row_bytes / 16), lane = threadIdx.x & 31;
+  for (int r = warp; r < a.E * a.C; r += warps) {
+    const int e = r / a.C;
+    if (r - e * a.C < rows[e]) continue;
+    uint4* p = reinterpret_cast<uint4*>(y + (size_t)r * row_bytes);
+    for (int v = lane; v < vecs; v += 32) p[v] = make_uint4(0, 0, 0, 0);
+  }
+}
+
 // ---- FMA tiles -----------------------------------------------------------------------------------------------------
 // A CTA of 256 threads owns a BM x BN tile, a thread TM x TN of it in two halves along each side (so that shared-memory
 // reads are conflict-free and a thread of the gated product holds the gate and the up value of the same column).  The

@@ -47,6 +47,7 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t phase,
   }
   return false;
 }
+__device__ __forceinline__ void prefetch_tmap(const CUtensorMap* tm) { asm volatile("prefetch.tensormap [%0];" ::"l"(tm) : "memory"); }
 // loads into this CTA's shared memory that complete on a barrier of either CTA of the pair
 __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* tm, int x, int y, int z, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
@@ -180,6 +181,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
   const int ntn = (a.N + kTileN - 1) / kTileN, ntm_dw = (a.M + kXTile - 1) / kXTile;
 
   if (threadIdx.x == 0) {
+    prefetch_tmap(&tA); prefetch_tmap(rank ? &tB1 : &tB0);
     for (int s = 0; s < kStages; ++s) { mbar_init(&sm.full[s], 1); mbar_init(&sm.empty[s], 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(&sm.acc_full[b], 1); mbar_init(&sm.acc_empty[b], 2 * kEpiWarps); }
     mbar_init(&sm.tail, 1); mbar_init(&sm.tail_peer, 1);

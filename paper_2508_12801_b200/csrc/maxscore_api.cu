@@ -21,6 +21,7 @@
 #include "alg1.cuh"
 #include "expert.cuh"
 #include "expert_tc.cuh"
+#include "expert_few.cuh"
 #include "norm.cuh"
 
 using namespace msr;
@@ -509,7 +510,9 @@ maxscore_status maxscore_create(maxscore_ctx** out, const maxscore_params* param
     room(expert_tc_kernel<kEpiGlu, true, 1>, x_smem(kEpiGlu, 1)); room(expert_tc_kernel<kEpiGlu, true, 2>, x_smem(kEpiGlu, 2));
     room(expert_tc_kernel<kEpiDact, false, 1>, x_smem(kEpiDact, 1)); room(expert_tc_kernel<kEpiDact, true, 1>, x_smem(kEpiDact, 1));
     room(expert_tc_kernel<kEpiDw, true, 2>, x_smem(kEpiDw, 2));
-    if (e_ != cudaSuccess) return cuda_fail(e_, "cudaFuncSetAttribute(expert_tc_kernel)");
+    room(expert_few_kernel<kEpiPlain, false>, few_smem(kEpiPlain, kFewRows)); room(expert_few_kernel<kEpiPlain, true>, few_smem(kEpiPlain, kFewRows));
+    room(expert_few_kernel<kEpiGlu, false>, few_smem(kEpiGlu, kFewRows)); room(expert_few_kernel<kEpiGlu, true>, few_smem(kEpiGlu, kFewRows));
+    if (e_ != cudaSuccess) return cuda_fail(e_, "cudaFuncSetAttribute(expert kernels)");
   }
   int coop = 0, sweep_occ = 0;
   MS_CUDA(cudaDeviceGetAttribute(&coop, cudaDevAttrCooperativeLaunch, dev));
@@ -1082,11 +1085,41 @@ maxscore_status launch_tc(maxscore_ctx* c, const void* A, const void* B, const v
   return MAXSCORE_OK;
 }
 
+template <int EPI, bool B_MN>
+maxscore_status launch_few(maxscore_ctx* c, const void* x, const void* w, void* out, void* pre_out, ExpertArgs a, cudaStream_t st) {
+  const uint64_t C = (uint64_t)c->C, N = (uint64_t)a.N, K = (uint64_t)a.K, cols = EPI == kEpiGlu ? 2 * N : N;
+  const int pad = few_pad(c->C);
+  typedef const __nv_bfloat16* P;
+  CUtensorMap tW0, tW1, tX;
+  maxscore_status s;
+  a.b_chunks = EPI == kEpiPlain && B_MN && N % 64 == 0;
+  s = make_tmap_expert(c, &tX, x, K, C, K, C * K, (uint32_t)pad);
+  if (s) return s;
+  const uint32_t box = B_MN || EPI == kEpiGlu ? 64 : 128;
+  s = B_MN ? make_tmap_expert(c, &tW0, w, N, K, cols, K * cols, box, a.b_chunks) : make_tmap_expert(c, &tW0, w, K, N, K, cols * K, box);
+  if (s) return s;
+  tW1 = tW0;
+  if (EPI == kEpiGlu) {
+    s = B_MN ? make_tmap_expert(c, &tW1, (P)w + N, N, K, cols, K * cols, box) : make_tmap_expert(c, &tW1, (P)w + N * K, K, N, K, cols * K, box);
+    if (s) return s;
+  }
+  const long long items = (long long)a.E * ((a.N + (EPI == kEpiGlu ? 63 : 127)) / (EPI == kEpiGlu ? 64 : 128));
+  const int grid = (int)std::min<long long>(c->sm_count, items);
+  expert_few_kernel<EPI, B_MN><<<grid, kFewThreads, few_smem(EPI, pad), st>>>(tW0, tW1, tX, (__nv_bfloat16*)out, (__nv_bfloat16*)pre_out, a, pad,
+                                                                             error_flag_of(c));
+  MS_LAUNCH_CHECK("expert_few_kernel");
+  c->launches += 1;
+  return MAXSCORE_OK;
+}
+
 // b_mn: the product's columns (N) run along memory in B
 template <int EPI>
 maxscore_status launch_expert(maxscore_ctx* c, const void* A, const void* B, const void* pre_in, void* out, void* pre_out,
                               const ExpertArgs& a, bool b_mn, cudaStream_t st) {
   if (c->p.io_dtype == MAXSCORE_BF16) {
+    if constexpr (EPI == kEpiPlain || EPI == kEpiGlu)
+      if (c->C <= kFewRows)
+        return b_mn ? launch_few<EPI, true>(c, A, B, out, pre_out, a, st) : launch_few<EPI, false>(c, A, B, out, pre_out, a, st);
     if constexpr (EPI == kEpiDw) return launch_tc<EPI, true>(c, A, B, pre_in, out, pre_out, a, st);
     else return b_mn ? launch_tc<EPI, true>(c, A, B, pre_in, out, pre_out, a, st)
                      : launch_tc<EPI, false>(c, A, B, pre_in, out, pre_out, a, st);
