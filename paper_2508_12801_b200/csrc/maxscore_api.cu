@@ -163,6 +163,20 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
 
 constexpr int kDhSmemMax = 2 * 2 * 16384 + kDhStages * 2 * 16384 + kDhOutBytes + 1024;     // Kpad = 128
 constexpr int kDwSmemMax = kDwStages * (16384 + 2 * 2 * 8192) + 1024;
+constexpr int kNormRing = 210 * 1024;    // shared memory of an SM that the norms' row rings share
+
+template <typename T, int SRC, typename F>
+void norm_fwd_room(F& room) {
+  room(norm_fwd_kernel<T, 4, SRC, 512, 1>, kNormRing); room(norm_fwd_kernel<T, 2, SRC, 512, 1>, kNormRing);
+  room(norm_fwd_kernel<T, 1, SRC, 512, 2>, kNormRing / 2); room(norm_fwd_kernel<T, 1, SRC, 256, 4>, kNormRing / 4);
+  room(norm_fwd_kernel<T, 1, SRC, 128, 6>, kNormRing / 6);
+}
+template <typename T, typename F>
+void norm_room(F& room) {
+  norm_fwd_room<T, 0>(room); norm_fwd_room<T, 1>(room); norm_fwd_room<T, 2>(room);
+  room(norm_bwd_kernel<T, 4, 512, 1>, kNormRing); room(norm_bwd_kernel<T, 2, 512, 1>, kNormRing); room(norm_bwd_kernel<T, 1, 512, 1>, kNormRing);
+  room(norm_bwd_kernel<T, 1, 256, 2>, kNormRing / 2); room(norm_bwd_kernel<T, 1, 128, 4>, kNormRing / 4);
+}
 
 }  // namespace
 
@@ -512,7 +526,8 @@ maxscore_status maxscore_create(maxscore_ctx** out, const maxscore_params* param
     room(expert_tc_kernel<kEpiDw, true, 2>, x_smem(kEpiDw, 2));
     room(expert_few_kernel<kEpiPlain, false>, few_smem(kEpiPlain, kFewRows)); room(expert_few_kernel<kEpiPlain, true>, few_smem(kEpiPlain, kFewRows));
     room(expert_few_kernel<kEpiGlu, false>, few_smem(kEpiGlu, kFewRows)); room(expert_few_kernel<kEpiGlu, true>, few_smem(kEpiGlu, kFewRows));
-    if (e_ != cudaSuccess) return cuda_fail(e_, "cudaFuncSetAttribute(expert kernels)");
+    norm_room<float>(room); norm_room<__nv_bfloat16>(room);
+    if (e_ != cudaSuccess) return cuda_fail(e_, "cudaFuncSetAttribute(expert and norm kernels)");
   }
   int coop = 0, sweep_occ = 0;
   MS_CUDA(cudaDeviceGetAttribute(&coop, cudaDevAttrCooperativeLaunch, dev));
@@ -1155,9 +1170,20 @@ NormArgs norm_args(const maxscore_ctx* c, const maxscore_norm* n) {
   return a;
 }
 
-// Threads of a row: one 16-byte vector each up to 64 vectors, two beyond.
-int norm_vecs(int nvec) { return nvec <= 64 ? 1 : 2; }
-int norm_threads(int nvec) { const int v = norm_vecs(nvec); return ((nvec + v - 1) / v + 31) / 32 * 32; }
+// How a row of nvec 16-byte vectors is worked on: V vectors a thread, G threads, CTAs of an SM, and the ring of row buffers
+// that a CTA's share of shared memory holds.
+struct NormShape { int V, G, ctas, slots; size_t smem; };
+NormShape norm_shape(int nvec, bool bwd) {
+  NormShape s{};
+  s.V = nvec <= 512 ? 1 : nvec <= 1024 ? 2 : 4;
+  s.G = ((nvec + s.V - 1) / s.V + 31) / 32 * 32;
+  // as many CTAs as registers allow; the backward keeps three column sums for each of a thread's values
+  s.ctas = s.V > 1 ? 1 : s.G <= 128 ? (bwd ? 4 : 6) : s.G <= 256 ? (bwd ? 2 : 4) : (bwd ? 1 : 2);
+  const size_t row = (size_t)nvec * 16, budget = kNormRing / s.ctas - sizeof(NormSmem);
+  s.slots = (int)std::min<size_t>(kNormSlots, budget / row);
+  s.smem = s.slots * row;
+  return s;
+}
 
 template <typename T, int SRC>
 maxscore_status launch_norm_fwd(maxscore_ctx* c, const void* y_in, const void* src, const int32_t* expert_idx, const int32_t* slot_idx,
@@ -1165,15 +1191,17 @@ maxscore_status launch_norm_fwd(maxscore_ctx* c, const void* y_in, const void* s
                                 cudaStream_t st) {
   const maxscore_params& p = c->p;
   const NormArgs a = norm_args(c, n);
-  const int G = norm_threads(a.nvec);
-  const int grid = std::min(p.T, c->sm_count * std::max(1, 2048 / G));
+  const NormShape f = norm_shape(a.nvec, false);
+  const int grid = std::min(p.T, c->sm_count * f.ctas);
   auto go = [&](auto kernel) {
-    kernel<<<grid, G, 0, st>>>((const T*)y_in, (const T*)src, expert_idx, slot_idx, gate_w, p.E, p.k, c->C, (const T*)residual,
-                               (T*)y_out, (T*)r_out, (T*)h, a);
+    kernel<<<grid, f.G + 32, f.smem, st>>>((const T*)y_in, (const T*)src, expert_idx, slot_idx, gate_w, p.E, p.k, c->C, (const T*)residual,
+                                           (T*)y_out, (T*)r_out, (T*)h, a, f.slots, error_flag_of(c));
   };
-  if (norm_vecs(a.nvec) == 1) go(norm_fwd_kernel<T, 1, SRC, 64>);
-  else if (G <= 256) go(norm_fwd_kernel<T, 2, SRC, 256>);
-  else go(norm_fwd_kernel<T, 2, SRC, 1024>);
+  if (f.V == 4) go(norm_fwd_kernel<T, 4, SRC, 512, 1>);
+  else if (f.V == 2) go(norm_fwd_kernel<T, 2, SRC, 512, 1>);
+  else if (f.G > 256) go(norm_fwd_kernel<T, 1, SRC, 512, 2>);
+  else if (f.G > 128) go(norm_fwd_kernel<T, 1, SRC, 256, 4>);
+  else go(norm_fwd_kernel<T, 1, SRC, 128, 6>);
   MS_LAUNCH_CHECK("norm_fwd_kernel");
   c->launches += 1;
   return MAXSCORE_OK;
@@ -1185,9 +1213,9 @@ maxscore_status launch_norm_bwd(maxscore_ctx* c, const void* dr_out, const void*
                                 cudaStream_t st) {
   const maxscore_params& p = c->p;
   const NormArgs a = norm_args(c, n);
-  const int G = norm_threads(a.nvec);
+  const NormShape f = norm_shape(a.nvec, true);
   const int parts = std::min(p.T, kNormParts);                       // rows of each partial matrix in the workspace
-  const int ctas = std::min(parts, c->sm_count * std::max(1, std::min(4, 512 / G)));
+  const int ctas = std::min(parts, c->sm_count * f.ctas);
   const int gate_rows = (p.T + a.rows_per_gate - 1) / a.rows_per_gate;
   NormUnits u{};
   u.per_gate = std::max(1, std::min(a.rows_per_gate, ctas / gate_rows));
@@ -1200,11 +1228,14 @@ maxscore_status launch_norm_bwd(maxscore_ctx* c, const void* dr_out, const void*
   float* pr = n->w_pre ? part + one : nullptr;
   float* pg = !n->gate ? nullptr : u.per_gate > 1 ? part + 2 * one : dgate;
   auto go = [&](auto kernel) {
-    kernel<<<grid, G, 0, st>>>((const T*)dr_out, (const T*)dh, (const T*)y, (const T*)r_out, (T*)dy, (T*)dr, pp, pr, pg, u, a);
+    kernel<<<grid, f.G + 32, f.smem, st>>>((const T*)dr_out, (const T*)dh, (const T*)y, (const T*)r_out, (T*)dy, (T*)dr, pp, pr, pg, u, a, f.slots,
+                                           error_flag_of(c));
   };
-  if (norm_vecs(a.nvec) == 1) go(norm_bwd_kernel<T, 1, 64>);
-  else if (G <= 256) go(norm_bwd_kernel<T, 2, 256>);
-  else go(norm_bwd_kernel<T, 2, 1024>);
+  if (f.V == 4) go(norm_bwd_kernel<T, 4, 512, 1>);
+  else if (f.V == 2) go(norm_bwd_kernel<T, 2, 512, 1>);
+  else if (f.G > 256) go(norm_bwd_kernel<T, 1, 512, 1>);
+  else if (f.G > 128) go(norm_bwd_kernel<T, 1, 256, 2>);
+  else go(norm_bwd_kernel<T, 1, 128, 4>);
   MS_LAUNCH_CHECK("norm_bwd_kernel");
   c->launches += 1;
   const bool reduce_gate = n->gate && u.per_gate > 1;
