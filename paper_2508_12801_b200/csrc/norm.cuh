@@ -28,7 +28,7 @@ struct NormSmem {
   uint64_t full[kNormSlots], empty[kNormSlots];
   float weight[kNormSlots][kMaxK];     // combine weights of the token whose residual row is in this slot
   int count[kNormSlots];               // and how many expert rows follow
-  float red[2][3][kNormWarps];
+  float red[2][4][kNormWarps];
 };
 
 // The consumers' side of the ring and their sums.  A wait that gives up leaves ok false: the thread goes on through the
@@ -46,30 +46,42 @@ struct NormGroup {
     if ((threadIdx.x & 31) == 0) mbar_arrive(&sm.empty[s]);
     if (++s == slots) { s = 0; ph ^= 1; }
   }
-  // Sums of N values over the group, the same on every thread and in the same order every time.  Two buffers in turn, so one
-  // barrier a sum is enough.
-  template <int N>
-  __device__ void sum(float (&v)[N]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
-    if (warps == 1) return;
+  // Sum over the group, the same on every thread and in the same order every time.  Two buffers in turn, so one barrier is
+  // enough.
+  __device__ float sum(float v) {
+    v = warp_sum(v);
+    if (warps == 1) return v;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (lane == 0)
-#pragma unroll
-      for (int i = 0; i < N; ++i) sm.red[turn][i][warp] = v[i];
+    if (lane == 0) sm.red[turn][0][warp] = v;
     asm volatile("bar.sync 1, %0;" ::"r"(G) : "memory");
+    v = sm.red[turn][0][lane & (kNormWarps - 1)];                  // warps that do not exist left zeros
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      float t = 0.f;
-#pragma unroll
-      for (int w = 0; w < kNormWarps; w += 4)
-        if (w < warps) {
-          const float4 x = *reinterpret_cast<const float4*>(&sm.red[turn][i][w]);
-          t += (x.x + x.y) + (x.z + x.w);                          // warps that do not exist left zeros
-        }
-      v[i] = t;
-    }
+    for (int o = kNormWarps / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     turn ^= 1;
+    return v;
+  }
+  // Three at once: the butterfly keeps half of the values on either side of the first two exchanges, so that a quarter of the
+  // lanes ends up with each of them (6 shuffles instead of 15).
+  __device__ void sum3(float& x, float& y, float& z) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const bool hi = lane & 16, odd = lane & 8;
+    float p = hi ? z : x, q = hi ? 0.f : y;
+    p += __shfl_xor_sync(0xffffffffu, hi ? x : z, 16);
+    q += __shfl_xor_sync(0xffffffffu, hi ? y : 0.f, 16);
+    float v = odd ? q : p;
+    v += __shfl_xor_sync(0xffffffffu, odd ? p : q, 8);
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (warps > 1) {                                               // lane / 8: 0 x, 1 y, 2 z
+      if ((lane & 7) == 0) sm.red[turn][lane >> 3][warp] = v;
+      asm volatile("bar.sync 1, %0;" ::"r"(G) : "memory");
+      const float2 t = *reinterpret_cast<const float2*>(&sm.red[turn][lane >> 3][(lane & 7) * 2]);
+      v = t.x + t.y;
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      turn ^= 1;
+    }
+    x = __shfl_sync(0xffffffffu, v, 0); y = __shfl_sync(0xffffffffu, v, 8); z = __shfl_sync(0xffffffffu, v, 16);
   }
 };
 // The producer's side: lane 0 of its warp.
@@ -89,7 +101,7 @@ __device__ __forceinline__ void norm_ring_init(NormSmem& sm, int slots, int warp
     for (int i = 0; i < slots; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], warps); }
     fence_barrier_init();
   }
-  for (int i = threadIdx.x; i < 2 * 3 * kNormWarps; i += blockDim.x) (&sm.red[0][0][0])[i] = 0.f;
+  for (int i = threadIdx.x; i < 2 * 4 * kNormWarps; i += blockDim.x) (&sm.red[0][0][0])[i] = 0.f;
   __syncthreads();
 }
 __device__ __forceinline__ void norm_ring_end(bool ok, unsigned* error_flag) {
@@ -99,24 +111,56 @@ __device__ __forceinline__ void norm_ring_end(bool ok, unsigned* error_flag) {
   }
 }
 
-template <typename T>
-__device__ __forceinline__ void unpack_w(const uint4& raw, float offset, float (&w)[Vec16<T>::N]) {
-  Vec16<T>::unpack(raw, w);
+// ---- pairs of floats: one instruction for two values ----------------------------------------------------------------
+// The kernels are short of instruction slots before they are short of bandwidth (a token passes 8 to 48 bytes an element
+// through some twenty operations each), so the arithmetic is done on packed pairs.
+typedef unsigned long long u64;
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  u64 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<u64&>(a)), "l"(reinterpret_cast<u64&>(b)));
+  return reinterpret_cast<float2&>(r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  u64 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<u64&>(a)), "l"(reinterpret_cast<u64&>(b)));
+  return reinterpret_cast<float2&>(r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  u64 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(reinterpret_cast<u64&>(a)), "l"(reinterpret_cast<u64&>(b)), "l"(reinterpret_cast<u64&>(c)));
+  return reinterpret_cast<float2&>(r);
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+template <typename T> __device__ __forceinline__ void unpack2(const uint4& v, float2 (&f)[Vec16<T>::N / 2]);
+template <> __device__ __forceinline__ void unpack2<float>(const uint4& v, float2 (&f)[2]) {
+  f[0] = make_float2(__uint_as_float(v.x), __uint_as_float(v.y)); f[1] = make_float2(__uint_as_float(v.z), __uint_as_float(v.w));
+}
+template <> __device__ __forceinline__ void unpack2<__nv_bfloat16>(const uint4& v, float2 (&f)[4]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int j = 0; j < Vec16<T>::N; ++j) w[j] += offset;
+  for (int i = 0; i < 4; ++i) f[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
 }
-template <typename T> __device__ __forceinline__ uint4 pack16(const float (&f)[Vec16<T>::N]);
-template <> __device__ __forceinline__ uint4 pack16<float>(const float (&f)[4]) {
-  return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+template <typename T> __device__ __forceinline__ uint4 pack2(const float2 (&f)[Vec16<T>::N / 2]);
+template <> __device__ __forceinline__ uint4 pack2<float>(const float2 (&f)[2]) {
+  return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y));
 }
-template <> __device__ __forceinline__ uint4 pack16<__nv_bfloat16>(const float (&f)[8]) {
+template <> __device__ __forceinline__ uint4 pack2<__nv_bfloat16>(const float2 (&f)[4]) {
   uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+    __nv_bfloat162 h = __floats2bfloat162_rn(f[i].x, f[i].y);
     w[i] = *reinterpret_cast<uint32_t*>(&h);
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// vector v of a weight row (offset added), ones without one
+template <typename T>
+__device__ __forceinline__ void load_weight(const void* w, size_t v, bool in, float offset, float2 (&f)[Vec16<T>::N / 2]) {
+  if (w && in) {
+    unpack2<T>(ldg16((const uint4*)w + v), f);
+#pragma unroll
+    for (int i = 0; i < Vec16<T>::N / 2; ++i) f[i] = add2(f[i], both(offset));
+  } else {
+#pragma unroll
+    for (int i = 0; i < Vec16<T>::N / 2; ++i) f[i] = both(1.f);
+  }
 }
 
 // SRC 0: no y (r' = res_scale * r), 1: y given, 2: y combined from the expert buffers.  The last warp is the producer.
@@ -172,18 +216,25 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
     norm_ring_end(feed.ok || lane != 0, error_flag);
     return;
   }
+  constexpr int P = N / 2;
   const uint4 zero = make_uint4(0, 0, 0, 0);
-  uint4 wpost[V], wpre[V], gat[V];
+  float2 wpre[V][P], gw[V][P];                          // gw: after-norm weight times gate, per gate row
+  auto gate_weights = [&](int g) {
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const int v = threadIdx.x + j * G;
-    const bool in = v < a.nvec;
-    wpost[j] = (in && a.w_post) ? ldg16((const uint4*)a.w_post + v) : zero;
-    wpre[j] = (in && a.w_pre) ? ldg16((const uint4*)a.w_pre + v) : zero;
-    gat[j] = zero;
-  }
+    for (int j = 0; j < V; ++j) {
+      const int v = threadIdx.x + j * G;
+      float2 x[P];
+      load_weight<T>(a.w_post, v, v < a.nvec, a.w_offset, gw[j]);
+      load_weight<T>(a.gate, (size_t)g * a.nvec + v, v < a.nvec, 0.f, x);
+#pragma unroll
+      for (int i = 0; i < P; ++i) gw[j][i] = mul2(gw[j][i], x[i]);
+    }
+  };
+#pragma unroll
+  for (int j = 0; j < V; ++j) load_weight<T>(a.w_pre, threadIdx.x + j * G, threadIdx.x + j * G < a.nvec, a.w_offset, wpre[j]);
   NormGroup group(sm, norm_ring, row_bytes, slots, G);
   const float inv_d = 1.f / (float)a.d;
+  const float2 scale = both(a.res_scale);
   int gate_row = -1;
   for (int tok = blockIdx.x; tok < a.T; tok += gridDim.x) {
     const size_t row = (size_t)tok * a.d;
@@ -199,11 +250,11 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
 #pragma unroll
       for (int c = 0; c < kMaxK; ++c) wgt[c] = sm.weight[group.s][c];
       group.release();
-      float acc[V][N];
+      float2 acc[V][P];
 #pragma unroll
       for (int j = 0; j < V; ++j)
 #pragma unroll
-        for (int i = 0; i < N; ++i) acc[j][i] = 0.f;
+        for (int i = 0; i < P; ++i) acc[j][i] = both(0.f);
 #pragma unroll
       for (int c = 0; c < kMaxK; ++c)
         if (c < n) {
@@ -211,17 +262,17 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
 #pragma unroll
           for (int j = 0; j < V; ++j) {
             const int v = threadIdx.x + j * G;
-            float x[N];
-            Vec16<T>::unpack(v < a.nvec ? p[v] : zero, x);
+            float2 x[P];
+            unpack2<T>(v < a.nvec ? p[v] : zero, x);
 #pragma unroll
-            for (int i = 0; i < N; ++i) acc[j][i] = fmaf(wgt[c], x[i], acc[j][i]);
+            for (int i = 0; i < P; ++i) acc[j][i] = fma2(both(wgt[c]), x[i], acc[j][i]);
           }
           group.release();
         }
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const int v = threadIdx.x + j * G;
-        yv[j] = pack16<T>(acc[j]);
+        yv[j] = pack2<T>(acc[j]);
         if (y_out && v < a.nvec && group.ok) *reinterpret_cast<uint4*>(y_out + row + (size_t)v * N) = yv[j];
       }
     } else {
@@ -233,69 +284,52 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
         group.release();
       }
     }
-    if (SRC && a.gate) {
-      const int g = tok / a.rows_per_gate;
-      if (g != gate_row) {
-        gate_row = g;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const int v = threadIdx.x + j * G;
-          if (v < a.nvec) gat[j] = ldg16((const T*)a.gate + (size_t)g * a.d + (size_t)v * N);
-        }
-      }
+    if (SRC) {
+      const int g = a.gate ? tok / a.rows_per_gate : 0;
+      if (g != gate_row) { gate_row = g; gate_weights(g); }
     }
     float inv_y = 1.f;
     if (SRC && a.w_post) {
-      float s[1] = {0.f};
+      float2 s = both(0.f);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        float y[N];
-        Vec16<T>::unpack(yv[j], y);
+        float2 y[P];
+        unpack2<T>(yv[j], y);
 #pragma unroll
-        for (int i = 0; i < N; ++i) s[0] = fmaf(y[i], y[i], s[0]);
+        for (int i = 0; i < P; ++i) s = fma2(y[i], y[i], s);
       }
-      group.sum(s);
-      inv_y = rsqrtf(s[0] * inv_d + a.eps);
+      inv_y = rsqrtf(group.sum(s.x + s.y) * inv_d + a.eps);
     }
-    float s[1] = {0.f};
+    float2 s = both(0.f);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const int v = threadIdx.x + j * G;
-      float r[N], y[N], w[N], g[N];
-      Vec16<T>::unpack(rv[j], r);
-      if (SRC) Vec16<T>::unpack(yv[j], y);
-      unpack_w<T>(wpost[j], a.w_offset, w);
-      Vec16<T>::unpack(gat[j], g);
+      float2 r[P], y[P];
+      unpack2<T>(rv[j], r);
+      if (SRC) unpack2<T>(yv[j], y);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        float n = 0.f;
-        if (SRC) {
-          n = y[i];
-          if (a.w_post) n = n * inv_y * w[i];
-          if (a.gate) n *= g[i];
-        }
-        r[i] = SRC ? fmaf(a.res_scale, r[i], n) : a.res_scale * r[i];
+      for (int i = 0; i < P; ++i) {
+        r[i] = mul2(scale, r[i]);
+        if (SRC) r[i] = fma2(mul2(y[i], both(inv_y)), gw[j][i], r[i]);
       }
-      rv[j] = pack16<T>(r);
+      rv[j] = pack2<T>(r);
       if (v < a.nvec) {
         if (r_out && group.ok) *reinterpret_cast<uint4*>(r_out + row + (size_t)v * N) = rv[j];
-        Vec16<T>::unpack(rv[j], r);
+        unpack2<T>(rv[j], r);
 #pragma unroll
-        for (int i = 0; i < N; ++i) s[0] = fmaf(r[i], r[i], s[0]);
+        for (int i = 0; i < P; ++i) s = fma2(r[i], r[i], s);
       }
     }
     if (h) {
-      group.sum(s);
-      const float inv = rsqrtf(s[0] * inv_d + a.eps);
+      const float2 inv = both(rsqrtf(group.sum(s.x + s.y) * inv_d + a.eps));
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const int v = threadIdx.x + j * G;
-        float r[N], w[N];
-        Vec16<T>::unpack(rv[j], r);
-        unpack_w<T>(wpre[j], a.w_offset, w);
+        float2 r[P];
+        unpack2<T>(rv[j], r);
 #pragma unroll
-        for (int i = 0; i < N; ++i) r[i] = r[i] * inv * w[i];
-        if (v < a.nvec && group.ok) Vec16<T>::store(h + row + (size_t)v * N, r);
+        for (int i = 0; i < P; ++i) r[i] = mul2(mul2(r[i], inv), wpre[j][i]);
+        if (v < a.nvec && group.ok) *reinterpret_cast<uint4*>(h + row + (size_t)v * N) = pack2<T>(r);
       }
     }
   }
@@ -327,6 +361,7 @@ norm_bwd_kernel(const T* dr_out, const T* dh, const T* y, const T* r_out, T* __r
   const uint4 zero = make_uint4(0, 0, 0, 0);
   const float inv_d = 1.f / (float)a.d;
   norm_ring_init(sm, slots, G >> 5);
+  const bool dh_given = dh != nullptr, y_given = y != nullptr, dro_given = dr_out != nullptr;
   int grow, t0, t1;
   if (threadIdx.x >= G) {
     if (threadIdx.x == G) {
@@ -344,114 +379,111 @@ norm_bwd_kernel(const T* dr_out, const T* dh, const T* y, const T* r_out, T* __r
     }
     return;
   }
+  constexpr int P = N / 2;
   NormGroup group(sm, norm_ring, row_bytes, slots, G);
-  uint4 wpost[V], wpre[V], gat[V];
-  float apost[V][N], apre[V][N], agate[V][N];
+  // Per column only two sums run along the tokens: S = sum dr y / rms(y) (within a gate row: dgate = w_post S, and gate S goes
+  // to dw_post when the unit ends) and dw_pre.
+  float2 wpre[V][P], gw[V][P], acc[V][P], apre[V][P], apost[V][P];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const int v = threadIdx.x + j * G;
-    const bool in = v < a.nvec;
-    wpost[j] = (in && a.w_post) ? ldg16((const uint4*)a.w_post + v) : zero;
-    wpre[j] = (in && a.w_pre) ? ldg16((const uint4*)a.w_pre + v) : zero;
-    gat[j] = zero;
+    load_weight<T>(a.w_pre, threadIdx.x + j * G, threadIdx.x + j * G < a.nvec, a.w_offset, wpre[j]);
 #pragma unroll
-    for (int i = 0; i < N; ++i) apost[j][i] = apre[j][i] = 0.f;
+    for (int i = 0; i < P; ++i) apost[j][i] = apre[j][i] = both(0.f);
   }
+  const float2 scale = both(a.res_scale);
   for (int unit = blockIdx.x; unit < u.n_units; unit += gridDim.x) {
     unit_range(u, a, unit, grow, t0, t1);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const int v = threadIdx.x + j * G;
-      if (a.gate && v < a.nvec) gat[j] = ldg16((const T*)a.gate + (size_t)grow * a.d + (size_t)v * N);
+      float2 x[P];
+      load_weight<T>(a.w_post, v, v < a.nvec, a.w_offset, gw[j]);
+      load_weight<T>(a.gate, (size_t)grow * a.nvec + v, v < a.nvec, 0.f, x);
 #pragma unroll
-      for (int i = 0; i < N; ++i) agate[j][i] = 0.f;
+      for (int i = 0; i < P; ++i) { gw[j][i] = mul2(gw[j][i], x[i]); acc[j][i] = both(0.f); }
     }
     for (int tok = t0; tok < t1; ++tok) {
       const size_t row = (size_t)tok * a.d;
-      uint4 rdo[V], rdh[V], ry[V], rr[V];
-      auto take = [&](uint4 (&to)[V], bool given) {
+      float2 o[V][P], g[V][P], r[V][P], y[V][P];
+      auto take = [&](float2 (&to)[V][P], bool given) {
         if (given) {
           const uint4* p = group.row();
 #pragma unroll
-          for (int j = 0; j < V; ++j) { const int v = threadIdx.x + j * G; to[j] = v < a.nvec ? p[v] : zero; }
+          for (int j = 0; j < V; ++j) { const int v = threadIdx.x + j * G; unpack2<T>(v < a.nvec ? p[v] : zero, to[j]); }
           group.release();
         } else {
 #pragma unroll
-          for (int j = 0; j < V; ++j) to[j] = zero;
+          for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < P; ++i) to[j][i] = both(0.f);
         }
       };
-      take(rr, dh != nullptr); take(rdh, dh != nullptr); take(ry, y != nullptr); take(rdo, dr_out != nullptr);
-      float s[3] = {0.f, 0.f, 0.f};     // sum r^2, sum dh w r, sum y^2
+      take(r, dh_given); take(g, dh_given); take(y, y_given); take(o, dro_given);
+      float2 sr = both(0.f), sg = both(0.f), sy = both(0.f);      // sum r^2, sum dh w r, sum y^2
+      float2 pre[V][P];
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        float g[N], r[N], yy[N], w[N];
-        Vec16<T>::unpack(rdh[j], g); Vec16<T>::unpack(rr[j], r); Vec16<T>::unpack(ry[j], yy);
-        unpack_w<T>(wpre[j], a.w_offset, w);
+      for (int j = 0; j < V; ++j)
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          s[0] = fmaf(r[i], r[i], s[0]);
-          s[1] = fmaf(g[i] * w[i], r[i], s[1]);
-          s[2] = fmaf(yy[i], yy[i], s[2]);
+        for (int i = 0; i < P; ++i) {
+          pre[j][i] = mul2(g[j][i], wpre[j][i]);
+          sr = fma2(r[j][i], r[j][i], sr);
+          sg = fma2(pre[j][i], r[j][i], sg);
+          sy = fma2(y[j][i], y[j][i], sy);
         }
-      }
-      group.sum(s);
-      const float inv_r = rsqrtf(s[0] * inv_d + a.eps), inv_y = rsqrtf(s[2] * inv_d + a.eps);
-      const float c_r = s[1] * inv_r * inv_r * inv_d;       // mean(dh w r / rms) / rms
-      float b[1] = {0.f};                                   // sum dn w_post y
-      float tot[V][N];
+      float s0 = sr.x + sr.y, s1 = sg.x + sg.y, s2 = sy.x + sy.y;
+      group.sum3(s0, s1, s2);
+      const float inv_r = rsqrtf(s0 * inv_d + a.eps), inv_y = a.w_post ? rsqrtf(s2 * inv_d + a.eps) : 1.f;
+      const float2 ir = both(inv_r), iy = both(inv_y), c_r = both(-s1 * inv_r * inv_r * inv_r * inv_d);   // -mean(dh w r / rms) / rms^2
+      float2 sb = both(0.f);                                      // sum dn w_post y
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const int v = threadIdx.x + j * G;
-        float o[N], g[N], r[N], w[N], yy[N], gt[N], wp[N], out[N];
-        Vec16<T>::unpack(rdo[j], o); Vec16<T>::unpack(rdh[j], g); Vec16<T>::unpack(rr[j], r); Vec16<T>::unpack(ry[j], yy);
-        unpack_w<T>(wpre[j], a.w_offset, w); unpack_w<T>(wpost[j], a.w_offset, wp); Vec16<T>::unpack(gat[j], gt);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const float t = o[i] + inv_r * (g[i] * w[i] - r[i] * c_r);
-          apre[j][i] = fmaf(g[i], r[i] * inv_r, apre[j][i]);
-          out[i] = a.res_scale * t;
-          const float yn = a.w_post ? yy[i] * inv_y : yy[i];
-          agate[j][i] = fmaf(t, a.w_post ? yn * wp[i] : yn, agate[j][i]);
-          const float dn = a.gate ? t * gt[i] : t;
-          apost[j][i] = fmaf(dn, yn, apost[j][i]);
-          tot[j][i] = dn;
-          b[0] = fmaf(dn * wp[i], yy[i], b[0]);
+        for (int i = 0; i < P; ++i) {
+          const float2 t = fma2(r[j][i], c_r, fma2(pre[j][i], ir, o[j][i]));       // gradient of r'
+          apre[j][i] = fma2(mul2(g[j][i], r[j][i]), ir, apre[j][i]);
+          acc[j][i] = fma2(mul2(t, y[j][i]), iy, acc[j][i]);
+          pre[j][i] = mul2(t, gw[j][i]);                                           // dn w_post
+          sb = fma2(pre[j][i], y[j][i], sb);
+          o[j][i] = mul2(scale, t);
         }
-        if (v < a.nvec && group.ok) Vec16<T>::store(dr + row + (size_t)v * N, out);
+        if (v < a.nvec && group.ok) *reinterpret_cast<uint4*>(dr + row + (size_t)v * N) = pack2<T>(o[j]);
       }
-      if (dy) {
-        float c_y = 0.f;
-        if (a.w_post) { group.sum(b); c_y = b[0] * inv_y * inv_y * inv_d; }
+      if (y_given) {
+        float2 c_y = both(0.f);
+        if (a.w_post) c_y = both(-group.sum(sb.x + sb.y) * inv_y * inv_y * inv_y * inv_d);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           const int v = threadIdx.x + j * G;
-          float yy[N], wp[N], out[N];
-          Vec16<T>::unpack(ry[j], yy); unpack_w<T>(wpost[j], a.w_offset, wp);
 #pragma unroll
-          for (int i = 0; i < N; ++i) out[i] = a.w_post ? inv_y * (tot[j][i] * wp[i] - yy[i] * c_y) : tot[j][i];
-          if (v < a.nvec && group.ok) Vec16<T>::store(dy + row + (size_t)v * N, out);
+          for (int i = 0; i < P; ++i) pre[j][i] = fma2(y[j][i], c_y, mul2(pre[j][i], iy));
+          if (v < a.nvec && group.ok) *reinterpret_cast<uint4*>(dy + row + (size_t)v * N) = pack2<T>(pre[j]);
         }
       }
     }
-    if (part_gate)
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int v = threadIdx.x + j * G;
-        if (v < a.nvec)
+    for (int j = 0; j < V; ++j) {
+      const int v = threadIdx.x + j * G;
+      float2 x[P];
+      load_weight<T>(a.gate, (size_t)grow * a.nvec + v, v < a.nvec, 0.f, x);
 #pragma unroll
-          for (int i = 0; i < N; i += 4)
-            *reinterpret_cast<float4*>(part_gate + (size_t)unit * a.d + (size_t)v * N + i) = make_float4(agate[j][i], agate[j][i + 1], agate[j][i + 2], agate[j][i + 3]);
+      for (int i = 0; i < P; ++i) apost[j][i] = fma2(acc[j][i], x[i], apost[j][i]);
+      if (part_gate && v < a.nvec) {
+        load_weight<T>(a.w_post, v, true, a.w_offset, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) *reinterpret_cast<float2*>(part_gate + (size_t)unit * a.d + (size_t)v * N + 2 * i) = mul2(acc[j][i], x[i]);
       }
+    }
   }
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     const int v = threadIdx.x + j * G;
     if (v < a.nvec)
 #pragma unroll
-      for (int i = 0; i < N; i += 4) {
-        const size_t at = (size_t)blockIdx.x * a.d + (size_t)v * N + i;
-        if (part_post) *reinterpret_cast<float4*>(part_post + at) = make_float4(apost[j][i], apost[j][i + 1], apost[j][i + 2], apost[j][i + 3]);
-        if (part_pre) *reinterpret_cast<float4*>(part_pre + at) = make_float4(apre[j][i], apre[j][i + 1], apre[j][i + 2], apre[j][i + 3]);
+      for (int i = 0; i < P; ++i) {
+        const size_t at = (size_t)blockIdx.x * a.d + (size_t)v * N + 2 * i;
+        if (part_post) *reinterpret_cast<float2*>(part_post + at) = apost[j][i];
+        if (part_pre) *reinterpret_cast<float2*>(part_pre + at) = apre[j][i];
       }
   }
   norm_ring_end(group.ok, error_flag);
