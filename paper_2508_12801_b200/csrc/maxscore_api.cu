@@ -11,6 +11,7 @@
 #include <algorithm>
 #include <initializer_list>
 #include <new>
+#include <type_traits>
 
 #include "common.cuh"
 #include "flow.cuh"
@@ -165,17 +166,18 @@ constexpr int kDhSmemMax = 2 * 2 * 16384 + kDhStages * 2 * 16384 + kDhOutBytes +
 constexpr int kDwSmemMax = kDwStages * (16384 + 2 * 2 * 8192) + 1024;
 constexpr int kNormRing = 210 * 1024;    // shared memory of an SM that the norms' row rings share
 
-template <typename T, int SRC, typename F>
+template <typename T, int SRC, bool Full, typename F>
 void norm_fwd_room(F& room) {
-  room(norm_fwd_kernel<T, 4, SRC, 512, 1>, kNormRing); room(norm_fwd_kernel<T, 2, SRC, 512, 1>, kNormRing);
-  room(norm_fwd_kernel<T, 1, SRC, 512, 2>, kNormRing / 2); room(norm_fwd_kernel<T, 1, SRC, 256, 4>, kNormRing / 4);
-  room(norm_fwd_kernel<T, 1, SRC, 128, 6>, kNormRing / 6);
+  room(norm_fwd_kernel<T, 4, SRC, Full, 512, 1>, kNormRing); room(norm_fwd_kernel<T, 2, SRC, Full, 512, 1>, kNormRing);
+  room(norm_fwd_kernel<T, 2, SRC, Full, 256, 2>, kNormRing / 2); room(norm_fwd_kernel<T, 2, SRC, Full, 128, 4>, kNormRing / 4);
+  room(norm_fwd_kernel<T, 2, SRC, Full, 64, 8>, kNormRing / 8);
 }
-template <typename T, typename F>
+template <typename T, bool Full, typename F>
 void norm_room(F& room) {
-  norm_fwd_room<T, 0>(room); norm_fwd_room<T, 1>(room); norm_fwd_room<T, 2>(room);
-  room(norm_bwd_kernel<T, 4, 512, 1>, kNormRing); room(norm_bwd_kernel<T, 2, 512, 1>, kNormRing); room(norm_bwd_kernel<T, 1, 512, 1>, kNormRing);
-  room(norm_bwd_kernel<T, 1, 256, 2>, kNormRing / 2); room(norm_bwd_kernel<T, 1, 128, 4>, kNormRing / 4);
+  norm_fwd_room<T, 0, Full>(room); norm_fwd_room<T, 1, Full>(room); norm_fwd_room<T, 2, Full>(room);
+  room(norm_bwd_kernel<T, 4, Full, 512, 1>, kNormRing); room(norm_bwd_kernel<T, 2, Full, 512, 1>, kNormRing);
+  room(norm_bwd_kernel<T, 1, Full, 512, 1>, kNormRing); room(norm_bwd_kernel<T, 1, Full, 256, 2>, kNormRing / 2);
+  room(norm_bwd_kernel<T, 1, Full, 128, 4>, kNormRing / 4); room(norm_bwd_kernel<T, 1, Full, 64, 8>, kNormRing / 8);
 }
 
 }  // namespace
@@ -526,7 +528,7 @@ maxscore_status maxscore_create(maxscore_ctx** out, const maxscore_params* param
     room(expert_tc_kernel<kEpiDw, true, 2>, x_smem(kEpiDw, 2));
     room(expert_few_kernel<kEpiPlain, false>, few_smem(kEpiPlain, kFewRows)); room(expert_few_kernel<kEpiPlain, true>, few_smem(kEpiPlain, kFewRows));
     room(expert_few_kernel<kEpiGlu, false>, few_smem(kEpiGlu, kFewRows)); room(expert_few_kernel<kEpiGlu, true>, few_smem(kEpiGlu, kFewRows));
-    norm_room<float>(room); norm_room<__nv_bfloat16>(room);
+    norm_room<float, true>(room); norm_room<float, false>(room); norm_room<__nv_bfloat16, true>(room); norm_room<__nv_bfloat16, false>(room);
     if (e_ != cudaSuccess) return cuda_fail(e_, "cudaFuncSetAttribute(expert and norm kernels)");
   }
   int coop = 0, sweep_occ = 0;
@@ -1170,18 +1172,18 @@ NormArgs norm_args(const maxscore_ctx* c, const maxscore_norm* n) {
   return a;
 }
 
-// How a row of nvec 16-byte vectors is worked on: V vectors a thread, G threads, CTAs of an SM, and the ring of row buffers
-// that a CTA's share of shared memory holds.
-struct NormShape { int V, G, ctas, slots; size_t smem; };
-NormShape norm_shape(int nvec, bool bwd) {
+// How a row of nvec 16-byte vectors is worked on: V vectors a thread, G threads, CTAs of an SM, and the ring of slots (of
+// `rows` row buffers each) that a CTA's share of shared memory holds.
+struct NormShape { int V, G, ctas, slots; size_t smem; bool full; };
+NormShape norm_shape(int nvec, bool bwd, int rows) {
   NormShape s{};
-  s.V = nvec <= 512 ? 1 : nvec <= 1024 ? 2 : 4;
+  s.V = bwd ? (nvec <= 512 ? 1 : nvec <= 1024 ? 2 : 4) : nvec <= 1024 ? 2 : 4;
   s.G = ((nvec + s.V - 1) / s.V + 31) / 32 * 32;
-  // as many CTAs as registers allow; the backward keeps three column sums for each of a thread's values
-  s.ctas = s.V > 1 ? 1 : s.G <= 128 ? (bwd ? 4 : 6) : s.G <= 256 ? (bwd ? 2 : 4) : (bwd ? 1 : 2);
-  const size_t row = (size_t)nvec * 16, budget = kNormRing / s.ctas - sizeof(NormSmem);
-  s.slots = (int)std::min<size_t>(kNormSlots, budget / row);
-  s.smem = s.slots * row;
+  s.ctas = s.V == 1 || !bwd ? (s.G <= 64 ? 8 : s.G <= 128 ? 4 : s.G <= 256 ? 2 : 1) : 1;
+  s.full = nvec == s.V * s.G;
+  const size_t slot = (size_t)nvec * 16 * rows, budget = kNormRing / s.ctas - sizeof(NormSmem);
+  s.slots = (int)std::min<size_t>(kNormSlots, budget / slot);
+  s.smem = s.slots * slot;
   return s;
 }
 
@@ -1191,17 +1193,21 @@ maxscore_status launch_norm_fwd(maxscore_ctx* c, const void* y_in, const void* s
                                 cudaStream_t st) {
   const maxscore_params& p = c->p;
   const NormArgs a = norm_args(c, n);
-  const NormShape f = norm_shape(a.nvec, false);
+  const NormShape f = norm_shape(a.nvec, false, SRC == 1 ? 2 : 1);
   const int grid = std::min(p.T, c->sm_count * f.ctas);
   auto go = [&](auto kernel) {
     kernel<<<grid, f.G + 32, f.smem, st>>>((const T*)y_in, (const T*)src, expert_idx, slot_idx, gate_w, p.E, p.k, c->C, (const T*)residual,
                                            (T*)y_out, (T*)r_out, (T*)h, a, f.slots, error_flag_of(c));
   };
-  if (f.V == 4) go(norm_fwd_kernel<T, 4, SRC, 512, 1>);
-  else if (f.V == 2) go(norm_fwd_kernel<T, 2, SRC, 512, 1>);
-  else if (f.G > 256) go(norm_fwd_kernel<T, 1, SRC, 512, 2>);
-  else if (f.G > 128) go(norm_fwd_kernel<T, 1, SRC, 256, 4>);
-  else go(norm_fwd_kernel<T, 1, SRC, 128, 6>);
+  auto pick = [&](auto full) {
+    constexpr bool F = decltype(full)::value;
+    if (f.V == 4) go(norm_fwd_kernel<T, 4, SRC, F, 512, 1>);
+    else if (f.G > 256) go(norm_fwd_kernel<T, 2, SRC, F, 512, 1>);
+    else if (f.G > 128) go(norm_fwd_kernel<T, 2, SRC, F, 256, 2>);
+    else if (f.G > 64) go(norm_fwd_kernel<T, 2, SRC, F, 128, 4>);
+    else go(norm_fwd_kernel<T, 2, SRC, F, 64, 8>);
+  };
+  if (f.full) pick(std::true_type{}); else pick(std::false_type{});
   MS_LAUNCH_CHECK("norm_fwd_kernel");
   c->launches += 1;
   return MAXSCORE_OK;
@@ -1213,7 +1219,7 @@ maxscore_status launch_norm_bwd(maxscore_ctx* c, const void* dr_out, const void*
                                 cudaStream_t st) {
   const maxscore_params& p = c->p;
   const NormArgs a = norm_args(c, n);
-  const NormShape f = norm_shape(a.nvec, true);
+  const NormShape f = norm_shape(a.nvec, true, std::max(1, (dh ? 2 : 0) + (y ? 1 : 0) + (dr_out ? 1 : 0)));
   const int parts = std::min(p.T, kNormParts);                       // rows of each partial matrix in the workspace
   const int ctas = std::min(parts, c->sm_count * f.ctas);
   const int gate_rows = (p.T + a.rows_per_gate - 1) / a.rows_per_gate;
@@ -1231,11 +1237,16 @@ maxscore_status launch_norm_bwd(maxscore_ctx* c, const void* dr_out, const void*
     kernel<<<grid, f.G + 32, f.smem, st>>>((const T*)dr_out, (const T*)dh, (const T*)y, (const T*)r_out, (T*)dy, (T*)dr, pp, pr, pg, u, a, f.slots,
                                            error_flag_of(c));
   };
-  if (f.V == 4) go(norm_bwd_kernel<T, 4, 512, 1>);
-  else if (f.V == 2) go(norm_bwd_kernel<T, 2, 512, 1>);
-  else if (f.G > 256) go(norm_bwd_kernel<T, 1, 512, 1>);
-  else if (f.G > 128) go(norm_bwd_kernel<T, 1, 256, 2>);
-  else go(norm_bwd_kernel<T, 1, 128, 4>);
+  auto pick = [&](auto full) {
+    constexpr bool F = decltype(full)::value;
+    if (f.V == 4) go(norm_bwd_kernel<T, 4, F, 512, 1>);
+    else if (f.V == 2) go(norm_bwd_kernel<T, 2, F, 512, 1>);
+    else if (f.G > 256) go(norm_bwd_kernel<T, 1, F, 512, 1>);
+    else if (f.G > 128) go(norm_bwd_kernel<T, 1, F, 256, 2>);
+    else if (f.G > 64) go(norm_bwd_kernel<T, 1, F, 128, 4>);
+    else go(norm_bwd_kernel<T, 1, F, 64, 8>);
+  };
+  if (f.full) pick(std::true_type{}); else pick(std::false_type{});
   MS_LAUNCH_CHECK("norm_bwd_kernel");
   c->launches += 1;
   const bool reduce_gate = n->gate && u.per_gate > 1;

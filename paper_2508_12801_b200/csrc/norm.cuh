@@ -34,14 +34,14 @@ struct NormSmem {
 // The consumers' side of the ring and their sums.  A wait that gives up leaves ok false: the thread goes on through the
 // barriers without waiting or storing, so that all end together.
 struct NormGroup {
-  NormSmem& sm; const unsigned char* ring; uint32_t row_bytes; int slots, G, warps;
+  NormSmem& sm; const unsigned char* ring; uint32_t slot_bytes; int slots, G, warps;
   int s = 0, turn = 0; uint32_t ph = 0; bool ok = true;
-  __device__ NormGroup(NormSmem& m, const unsigned char* r, uint32_t b, int n, int g) : sm(m), ring(r), row_bytes(b), slots(n), G(g), warps(g >> 5) {}
-  __device__ const uint4* row() {                                  // the next row, once it has landed
+  __device__ NormGroup(NormSmem& m, const unsigned char* r, uint32_t b, int n, int g) : sm(m), ring(r), slot_bytes(b), slots(n), G(g), warps(g >> 5) {}
+  __device__ const uint4* take() {                                 // the next slot, once its rows have landed
     if (ok) ok = mbar_wait_bounded(&sm.full[s], ph);
-    return reinterpret_cast<const uint4*>(ring + (size_t)s * row_bytes);
+    return reinterpret_cast<const uint4*>(ring + (uint32_t)s * slot_bytes);
   }
-  __device__ void release() {                                      // the row has been read by this warp
+  __device__ void release() {                                      // the slot has been read by this warp
     __syncwarp();
     if ((threadIdx.x & 31) == 0) mbar_arrive(&sm.empty[s]);
     if (++s == slots) { s = 0; ph ^= 1; }
@@ -86,15 +86,13 @@ struct NormGroup {
 };
 // The producer's side: lane 0 of its warp.
 struct NormFeed {
-  NormSmem& sm; unsigned char* ring; uint32_t row_bytes; int slots;
+  NormSmem& sm; unsigned char* ring; uint32_t slot_bytes; int slots;
   int s = 0; uint32_t ph = 1; bool ok = true;
-  __device__ NormFeed(NormSmem& m, unsigned char* r, uint32_t b, int n) : sm(m), ring(r), row_bytes(b), slots(n) {}
+  __device__ NormFeed(NormSmem& m, unsigned char* r, uint32_t b, int n) : sm(m), ring(r), slot_bytes(b), slots(n) {}
   __device__ bool room() { return ok = ok && mbar_wait_bounded(&sm.empty[s], ph); }
-  __device__ void row(const void* src) {
-    mbar_expect_tx(&sm.full[s], row_bytes);
-    bulk_g2s(ring + (size_t)s * row_bytes, src, row_bytes, &sm.full[s]);
-    if (++s == slots) { s = 0; ph ^= 1; }
-  }
+  __device__ void expect(uint32_t bytes) { mbar_expect_tx(&sm.full[s], bytes); }
+  __device__ void row(uint32_t at, const void* src, uint32_t bytes) { bulk_g2s(ring + (uint32_t)s * slot_bytes + at, src, bytes, &sm.full[s]); }
+  __device__ void next() { if (++s == slots) { s = 0; ph ^= 1; } }
 };
 __device__ __forceinline__ void norm_ring_init(NormSmem& sm, int slots, int warps) {
   if (threadIdx.x == 0) {
@@ -163,8 +161,9 @@ __device__ __forceinline__ void load_weight(const void* w, size_t v, bool in, fl
   }
 }
 
-// SRC 0: no y (r' = res_scale * r), 1: y given, 2: y combined from the expert buffers.  The last warp is the producer.
-template <typename T, int V, int SRC, int MaxG, int Ctas>
+// SRC 0: no y (r' = res_scale * r), 1: y given, 2: y combined from the expert buffers.  Full: the threads' vectors are exactly
+// the row.  The last warp is the producer.  A ring slot holds a token's rows, or one row each where their number varies (SRC 2).
+template <typename T, int V, int SRC, bool Full, int MaxG, int Ctas>
 __global__ void __launch_bounds__(MaxG + 32, Ctas)
 norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_idx, const int32_t* __restrict__ slot_idx,
                 const float* __restrict__ gate_w, int E, int k, int C, const T* residual, T* __restrict__ y_out, T* r_out,
@@ -177,7 +176,8 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
   norm_ring_init(sm, slots, G >> 5);
   if (threadIdx.x >= G) {
     // ---- producer: residual row first, then y or the rows of the token's experts in ascending order -------------------
-    NormFeed feed(sm, norm_ring, row_bytes, slots);
+    constexpr uint32_t kRows = SRC == 1 ? 2 : 1;
+    NormFeed feed(sm, norm_ring, row_bytes * kRows, slots);
     int e = 0, sl = 0; float w = 0.f;
     auto pairs_of = [&](int tok) {
       if (SRC == 2 && lane < k && tok < a.T) {
@@ -203,13 +203,15 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
         pairs_of(tok + gridDim.x);                                 // the next token's, while this one's rows are on the way
       }
       if (lane == 0) {
-        feed.row(residual + (size_t)tok * a.d);
-        if (SRC == 1 && feed.room()) feed.row(y_in + (size_t)tok * a.d);
+        feed.expect(row_bytes * kRows);
+        feed.row(0, residual + (size_t)tok * a.d, row_bytes);
+        if (SRC == 1) feed.row(row_bytes, y_in + (size_t)tok * a.d, row_bytes);
+        feed.next();
       }
       if (SRC == 2)
         for (unsigned m = mask; m; m &= m - 1) {
           const unsigned long long p = __shfl_sync(0xffffffffu, (unsigned long long)at, __ffs(m) - 1);
-          if (lane == 0 && feed.room()) feed.row((const void*)p);
+          if (lane == 0 && feed.room()) { feed.expect(row_bytes); feed.row(0, (const void*)p, row_bytes); feed.next(); }
         }
       if (!__shfl_sync(0xffffffffu, feed.ok, 0)) break;
     }
@@ -218,31 +220,36 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
   }
   constexpr int P = N / 2;
   const uint4 zero = make_uint4(0, 0, 0, 0);
+  auto mine = [&](int v) { return Full || v < a.nvec; };
   float2 wpre[V][P], gw[V][P];                          // gw: after-norm weight times gate, per gate row
   auto gate_weights = [&](int g) {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const int v = threadIdx.x + j * G;
       float2 x[P];
-      load_weight<T>(a.w_post, v, v < a.nvec, a.w_offset, gw[j]);
-      load_weight<T>(a.gate, (size_t)g * a.nvec + v, v < a.nvec, 0.f, x);
+      load_weight<T>(a.w_post, v, mine(v), a.w_offset, gw[j]);
+      load_weight<T>(a.gate, (size_t)g * a.nvec + v, mine(v), 0.f, x);
 #pragma unroll
       for (int i = 0; i < P; ++i) gw[j][i] = mul2(gw[j][i], x[i]);
     }
   };
 #pragma unroll
-  for (int j = 0; j < V; ++j) load_weight<T>(a.w_pre, threadIdx.x + j * G, threadIdx.x + j * G < a.nvec, a.w_offset, wpre[j]);
-  NormGroup group(sm, norm_ring, row_bytes, slots, G);
+  for (int j = 0; j < V; ++j) load_weight<T>(a.w_pre, threadIdx.x + j * G, mine(threadIdx.x + j * G), a.w_offset, wpre[j]);
+  NormGroup group(sm, norm_ring, SRC == 1 ? 2 * row_bytes : row_bytes, slots, G);
   const float inv_d = 1.f / (float)a.d;
   const float2 scale = both(a.res_scale);
-  int gate_row = -1;
+  long long gate_end = 0;                               // first token behind the present gate row
   for (int tok = blockIdx.x; tok < a.T; tok += gridDim.x) {
     const size_t row = (size_t)tok * a.d;
     uint4 rv[V], yv[V];
     {
-      const uint4* p = group.row();
+      const uint4* p = group.take();
 #pragma unroll
-      for (int j = 0; j < V; ++j) { const int v = threadIdx.x + j * G; rv[j] = v < a.nvec ? p[v] : zero; }
+      for (int j = 0; j < V; ++j) {
+        const int v = threadIdx.x + j * G;
+        rv[j] = mine(v) ? p[v] : zero;
+        if (SRC == 1) yv[j] = mine(v) ? p[a.nvec + v] : zero;
+      }
     }
     if (SRC == 2) {
       const int n = sm.count[group.s];
@@ -258,12 +265,12 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
 #pragma unroll
       for (int c = 0; c < kMaxK; ++c)
         if (c < n) {
-          const uint4* p = group.row();
+          const uint4* p = group.take();
 #pragma unroll
           for (int j = 0; j < V; ++j) {
             const int v = threadIdx.x + j * G;
             float2 x[P];
-            unpack2<T>(v < a.nvec ? p[v] : zero, x);
+            unpack2<T>(mine(v) ? p[v] : zero, x);
 #pragma unroll
             for (int i = 0; i < P; ++i) acc[j][i] = fma2(both(wgt[c]), x[i], acc[j][i]);
           }
@@ -273,20 +280,15 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
       for (int j = 0; j < V; ++j) {
         const int v = threadIdx.x + j * G;
         yv[j] = pack2<T>(acc[j]);
-        if (y_out && v < a.nvec && group.ok) *reinterpret_cast<uint4*>(y_out + row + (size_t)v * N) = yv[j];
+        if (y_out && mine(v) && group.ok) *reinterpret_cast<uint4*>(y_out + row + (size_t)v * N) = yv[j];
       }
     } else {
       group.release();
-      if (SRC == 1) {
-        const uint4* p = group.row();
-#pragma unroll
-        for (int j = 0; j < V; ++j) { const int v = threadIdx.x + j * G; yv[j] = v < a.nvec ? p[v] : zero; }
-        group.release();
-      }
     }
-    if (SRC) {
+    if (SRC && tok >= gate_end) {
       const int g = a.gate ? tok / a.rows_per_gate : 0;
-      if (g != gate_row) { gate_row = g; gate_weights(g); }
+      gate_end = a.gate ? ((long long)g + 1) * a.rows_per_gate : a.T;
+      gate_weights(g);
     }
     float inv_y = 1.f;
     if (SRC && a.w_post) {
@@ -313,7 +315,7 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
         if (SRC) r[i] = fma2(mul2(y[i], both(inv_y)), gw[j][i], r[i]);
       }
       rv[j] = pack2<T>(r);
-      if (v < a.nvec) {
+      if (mine(v)) {
         if (r_out && group.ok) *reinterpret_cast<uint4*>(r_out + row + (size_t)v * N) = rv[j];
         unpack2<T>(rv[j], r);
 #pragma unroll
@@ -329,7 +331,7 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
         unpack2<T>(rv[j], r);
 #pragma unroll
         for (int i = 0; i < P; ++i) r[i] = mul2(mul2(r[i], inv), wpre[j][i]);
-        if (v < a.nvec && group.ok) *reinterpret_cast<uint4*>(h + row + (size_t)v * N) = pack2<T>(r);
+        if (mine(v) && group.ok) *reinterpret_cast<uint4*>(h + row + (size_t)v * N) = pack2<T>(r);
       }
     }
   }
@@ -348,7 +350,7 @@ __device__ __forceinline__ void unit_range(const NormUnits& u, const NormArgs& a
   t0 = (int)min(start, (long long)a.T); t1 = (int)end;
 }
 
-template <typename T, int V, int MaxG, int Ctas>
+template <typename T, int V, bool Full, int MaxG, int Ctas>
 __global__ void __launch_bounds__(MaxG + 32, Ctas)
 norm_bwd_kernel(const T* dr_out, const T* dh, const T* y, const T* r_out, T* __restrict__ dy, T* dr,
                 float* __restrict__ part_post, float* __restrict__ part_pre, float* __restrict__ part_gate, NormUnits u, NormArgs a,
@@ -362,17 +364,21 @@ norm_bwd_kernel(const T* dr_out, const T* dh, const T* y, const T* r_out, T* __r
   const float inv_d = 1.f / (float)a.d;
   norm_ring_init(sm, slots, G >> 5);
   const bool dh_given = dh != nullptr, y_given = y != nullptr, dro_given = dr_out != nullptr;
+  // a slot holds the token's rows that are given: r', dh, y, dr'
+  const uint32_t at_y = dh_given ? 2 * a.nvec : 0, at_o = at_y + (y_given ? a.nvec : 0), rows = (dh_given ? 2 : 0) + (y_given ? 1 : 0) + (dro_given ? 1 : 0);
   int grow, t0, t1;
   if (threadIdx.x >= G) {
     if (threadIdx.x == G) {
-      NormFeed feed(sm, norm_ring, row_bytes, slots);
+      NormFeed feed(sm, norm_ring, rows * row_bytes, slots);
       for (int unit = blockIdx.x; unit < u.n_units && feed.ok; unit += gridDim.x) {
         unit_range(u, a, unit, grow, t0, t1);
-        for (int tok = t0; tok < t1 && feed.ok; ++tok) {
+        for (int tok = t0; rows && tok < t1 && feed.room(); ++tok) {
           const size_t row = (size_t)tok * a.d;
-          if (dh) { if (feed.room()) feed.row(r_out + row); if (feed.room()) feed.row(dh + row); }
-          if (y && feed.room()) feed.row(y + row);
-          if (dr_out && feed.room()) feed.row(dr_out + row);
+          feed.expect(rows * row_bytes);
+          if (dh_given) { feed.row(0, r_out + row, row_bytes); feed.row(row_bytes, dh + row, row_bytes); }
+          if (y_given) feed.row(at_y * 16, y + row, row_bytes);
+          if (dro_given) feed.row(at_o * 16, dr_out + row, row_bytes);
+          feed.next();
         }
       }
       norm_ring_end(feed.ok, error_flag);
@@ -380,13 +386,14 @@ norm_bwd_kernel(const T* dr_out, const T* dh, const T* y, const T* r_out, T* __r
     return;
   }
   constexpr int P = N / 2;
-  NormGroup group(sm, norm_ring, row_bytes, slots, G);
+  NormGroup group(sm, norm_ring, rows * row_bytes, slots, G);
+  auto mine = [&](int v) { return Full || v < a.nvec; };
   // Per column only two sums run along the tokens: S = sum dr y / rms(y) (within a gate row: dgate = w_post S, and gate S goes
   // to dw_post when the unit ends) and dw_pre.
   float2 wpre[V][P], gw[V][P], acc[V][P], apre[V][P], apost[V][P];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    load_weight<T>(a.w_pre, threadIdx.x + j * G, threadIdx.x + j * G < a.nvec, a.w_offset, wpre[j]);
+    load_weight<T>(a.w_pre, threadIdx.x + j * G, mine(threadIdx.x + j * G), a.w_offset, wpre[j]);
 #pragma unroll
     for (int i = 0; i < P; ++i) apost[j][i] = apre[j][i] = both(0.f);
   }
@@ -397,28 +404,28 @@ norm_bwd_kernel(const T* dr_out, const T* dh, const T* y, const T* r_out, T* __r
     for (int j = 0; j < V; ++j) {
       const int v = threadIdx.x + j * G;
       float2 x[P];
-      load_weight<T>(a.w_post, v, v < a.nvec, a.w_offset, gw[j]);
-      load_weight<T>(a.gate, (size_t)grow * a.nvec + v, v < a.nvec, 0.f, x);
+      load_weight<T>(a.w_post, v, mine(v), a.w_offset, gw[j]);
+      load_weight<T>(a.gate, (size_t)grow * a.nvec + v, mine(v), 0.f, x);
 #pragma unroll
       for (int i = 0; i < P; ++i) { gw[j][i] = mul2(gw[j][i], x[i]); acc[j][i] = both(0.f); }
     }
     for (int tok = t0; tok < t1; ++tok) {
       const size_t row = (size_t)tok * a.d;
       float2 o[V][P], g[V][P], r[V][P], y[V][P];
-      auto take = [&](float2 (&to)[V][P], bool given) {
-        if (given) {
-          const uint4* p = group.row();
+      auto load = [&](float2 (&to)[V][P], const uint4* p, bool given) {
 #pragma unroll
-          for (int j = 0; j < V; ++j) { const int v = threadIdx.x + j * G; unpack2<T>(v < a.nvec ? p[v] : zero, to[j]); }
-          group.release();
-        } else {
-#pragma unroll
-          for (int j = 0; j < V; ++j)
-#pragma unroll
-            for (int i = 0; i < P; ++i) to[j][i] = both(0.f);
+        for (int j = 0; j < V; ++j) {
+          const int v = threadIdx.x + j * G;
+          unpack2<T>(given && mine(v) ? p[v] : zero, to[j]);
         }
       };
-      take(r, dh_given); take(g, dh_given); take(y, y_given); take(o, dro_given);
+      if (rows) {
+        const uint4* p = group.take();
+        load(r, p, dh_given); load(g, p + a.nvec, dh_given); load(y, p + at_y, y_given); load(o, p + at_o, dro_given);
+        group.release();
+      } else {
+        load(r, nullptr, false); load(g, nullptr, false); load(y, nullptr, false); load(o, nullptr, false);
+      }
       float2 sr = both(0.f), sg = both(0.f), sy = both(0.f);      // sum r^2, sum dh w r, sum y^2
       float2 pre[V][P];
 #pragma unroll
@@ -447,7 +454,7 @@ norm_bwd_kernel(const T* dr_out, const T* dh, const T* y, const T* r_out, T* __r
           sb = fma2(pre[j][i], y[j][i], sb);
           o[j][i] = mul2(scale, t);
         }
-        if (v < a.nvec && group.ok) *reinterpret_cast<uint4*>(dr + row + (size_t)v * N) = pack2<T>(o[j]);
+        if (mine(v) && group.ok) *reinterpret_cast<uint4*>(dr + row + (size_t)v * N) = pack2<T>(o[j]);
       }
       if (y_given) {
         float2 c_y = both(0.f);
@@ -457,7 +464,7 @@ norm_bwd_kernel(const T* dr_out, const T* dh, const T* y, const T* r_out, T* __r
           const int v = threadIdx.x + j * G;
 #pragma unroll
           for (int i = 0; i < P; ++i) pre[j][i] = fma2(y[j][i], c_y, mul2(pre[j][i], iy));
-          if (v < a.nvec && group.ok) *reinterpret_cast<uint4*>(dy + row + (size_t)v * N) = pack2<T>(pre[j]);
+          if (mine(v) && group.ok) *reinterpret_cast<uint4*>(dy + row + (size_t)v * N) = pack2<T>(pre[j]);
         }
       }
     }
@@ -465,10 +472,10 @@ norm_bwd_kernel(const T* dr_out, const T* dh, const T* y, const T* r_out, T* __r
     for (int j = 0; j < V; ++j) {
       const int v = threadIdx.x + j * G;
       float2 x[P];
-      load_weight<T>(a.gate, (size_t)grow * a.nvec + v, v < a.nvec, 0.f, x);
+      load_weight<T>(a.gate, (size_t)grow * a.nvec + v, mine(v), 0.f, x);
 #pragma unroll
       for (int i = 0; i < P; ++i) apost[j][i] = fma2(acc[j][i], x[i], apost[j][i]);
-      if (part_gate && v < a.nvec) {
+      if (part_gate && mine(v)) {
         load_weight<T>(a.w_post, v, true, a.w_offset, x);
 #pragma unroll
         for (int i = 0; i < P; ++i) *reinterpret_cast<float2*>(part_gate + (size_t)unit * a.d + (size_t)v * N + 2 * i) = mul2(acc[j][i], x[i]);
@@ -478,7 +485,7 @@ norm_bwd_kernel(const T* dr_out, const T* dh, const T* y, const T* r_out, T* __r
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     const int v = threadIdx.x + j * G;
-    if (v < a.nvec)
+    if (mine(v))
 #pragma unroll
       for (int i = 0; i < P; ++i) {
         const size_t at = (size_t)blockIdx.x * a.d + (size_t)v * N + 2 * i;
