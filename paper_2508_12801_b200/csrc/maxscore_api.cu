@@ -1175,14 +1175,18 @@ NormArgs norm_args(const maxscore_ctx* c, const maxscore_norm* n) {
 // How a row of nvec 16-byte vectors is worked on: V vectors a thread, G threads, CTAs of an SM, and the ring of slots (of
 // `rows` row buffers each) that a CTA's share of shared memory holds.
 struct NormShape { int V, G, ctas, slots; size_t smem; bool full; };
-NormShape norm_shape(int nvec, bool bwd, int rows) {
+NormShape norm_shape(int nvec, bool bwd, bool gathers, int rows) {
   NormShape s{};
   s.V = bwd ? (nvec <= 512 ? 1 : nvec <= 1024 ? 2 : 4) : nvec <= 1024 ? 2 : 4;
   s.G = ((nvec + s.V - 1) / s.V + 31) / 32 * 32;
   s.ctas = s.V == 1 || !bwd ? (s.G <= 64 ? 8 : s.G <= 128 ? 4 : s.G <= 256 ? 2 : 1) : 1;
   s.full = nvec == s.V * s.G;
-  const size_t slot = (size_t)nvec * 16 * rows, budget = kNormRing / s.ctas - sizeof(NormSmem);
-  s.slots = (int)std::min<size_t>(kNormSlots, budget / slot);
+  // How much to have in flight matters more than how much fits: with 210 KB of rows on their way per SM reads and writes get in
+  // each other's way (combine and norms at T 65536, d 4096, k 8: 1 018 us; 105 KB 926 us, 70 KB 977 us, 52 KB 1 049 us; without
+  // combine 387, 379, 355, 378 us).  Two slots at least, or nothing runs ahead.
+  const size_t slot = (size_t)nvec * 16 * rows, share = kNormRing / s.ctas - sizeof(NormSmem);
+  const size_t wanted = (size_t)kNormRing / (gathers ? 2 : 3) / s.ctas / slot;
+  s.slots = (int)std::min<size_t>({kNormSlots, share / slot, std::max<size_t>(2, wanted)});
   s.smem = s.slots * slot;
   return s;
 }
@@ -1193,7 +1197,7 @@ maxscore_status launch_norm_fwd(maxscore_ctx* c, const void* y_in, const void* s
                                 cudaStream_t st) {
   const maxscore_params& p = c->p;
   const NormArgs a = norm_args(c, n);
-  const NormShape f = norm_shape(a.nvec, false, SRC == 1 ? 2 : 1);
+  const NormShape f = norm_shape(a.nvec, false, SRC == 2, SRC == 1 ? 2 : 1);
   const int grid = std::min(p.T, c->sm_count * f.ctas);
   auto go = [&](auto kernel) {
     kernel<<<grid, f.G + 32, f.smem, st>>>((const T*)y_in, (const T*)src, expert_idx, slot_idx, gate_w, p.E, p.k, c->C, (const T*)residual,
@@ -1219,7 +1223,7 @@ maxscore_status launch_norm_bwd(maxscore_ctx* c, const void* dr_out, const void*
                                 cudaStream_t st) {
   const maxscore_params& p = c->p;
   const NormArgs a = norm_args(c, n);
-  const NormShape f = norm_shape(a.nvec, true, std::max(1, (dh ? 2 : 0) + (y ? 1 : 0) + (dr_out ? 1 : 0)));
+  const NormShape f = norm_shape(a.nvec, true, false, std::max(1, (dh ? 2 : 0) + (y ? 1 : 0) + (dr_out ? 1 : 0)));
   const int parts = std::min(p.T, kNormParts);                       // rows of each partial matrix in the workspace
   const int ctas = std::min(parts, c->sm_count * f.ctas);
   const int gate_rows = (p.T + a.rows_per_gate - 1) / a.rows_per_gate;

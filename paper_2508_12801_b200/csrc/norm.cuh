@@ -280,7 +280,7 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
       for (int j = 0; j < V; ++j) {
         const int v = threadIdx.x + j * G;
         yv[j] = pack2<T>(acc[j]);
-        if (y_out && mine(v) && group.ok) *reinterpret_cast<uint4*>(y_out + row + (size_t)v * N) = yv[j];
+        if (y_out && mine(v) && group.ok) __stcs(reinterpret_cast<uint4*>(y_out + row + (size_t)v * N), yv[j]);
       }
     } else {
       group.release();
@@ -316,7 +316,7 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
       }
       rv[j] = pack2<T>(r);
       if (mine(v)) {
-        if (r_out && group.ok) *reinterpret_cast<uint4*>(r_out + row + (size_t)v * N) = rv[j];
+        if (r_out && group.ok) __stcs(reinterpret_cast<uint4*>(r_out + row + (size_t)v * N), rv[j]);
         unpack2<T>(rv[j], r);
 #pragma unroll
         for (int i = 0; i < P; ++i) s = fma2(r[i], r[i], s);
@@ -331,7 +331,7 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
         unpack2<T>(rv[j], r);
 #pragma unroll
         for (int i = 0; i < P; ++i) r[i] = mul2(mul2(r[i], inv), wpre[j][i]);
-        if (mine(v) && group.ok) *reinterpret_cast<uint4*>(h + row + (size_t)v * N) = pack2<T>(r);
+        if (mine(v) && group.ok) __stcs(reinterpret_cast<uint4*>(h + row + (size_t)v * N), pack2<T>(r));
       }
     }
   }
@@ -454,7 +454,7 @@ norm_bwd_kernel(const T* dr_out, const T* dh, const T* y, const T* r_out, T* __r
           sb = fma2(pre[j][i], y[j][i], sb);
           o[j][i] = mul2(scale, t);
         }
-        if (mine(v) && group.ok) *reinterpret_cast<uint4*>(dr + row + (size_t)v * N) = pack2<T>(o[j]);
+        if (mine(v) && group.ok) __stcs(reinterpret_cast<uint4*>(dr + row + (size_t)v * N), pack2<T>(o[j]));
       }
       if (y_given) {
         float2 c_y = both(0.f);
@@ -464,7 +464,7 @@ norm_bwd_kernel(const T* dr_out, const T* dh, const T* y, const T* r_out, T* __r
           const int v = threadIdx.x + j * G;
 #pragma unroll
           for (int i = 0; i < P; ++i) pre[j][i] = fma2(y[j][i], c_y, mul2(pre[j][i], iy));
-          if (mine(v) && group.ok) *reinterpret_cast<uint4*>(dy + row + (size_t)v * N) = pack2<T>(pre[j]);
+          if (mine(v) && group.ok) __stcs(reinterpret_cast<uint4*>(dy + row + (size_t)v * N), pack2<T>(pre[j]));
         }
       }
     }
