@@ -76,6 +76,8 @@ def _load():
 
 _lib = _load()
 _vp, _i32 = C.c_void_p, C.c_int32
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 _lib.maxscore_expert_gemm.argtypes = [_vp] * 5 + [_i32] * 3 + [_vp]
 _lib.maxscore_expert_gemm_dw.argtypes = [_vp] * 5 + [_i32] * 4 + [_vp]
 _lib.maxscore_expert_glu.argtypes = [_vp] * 6 + [_i32] * 3 + [_vp]
@@ -258,7 +260,7 @@ def _need(ctx, name, t, dtype, numel, optional=False):
         if optional:
             return None
         raise ValueError(f"{name}: a tensor is needed")
-    if t.dtype is not dtype or t.numel() != numel or not t.is_contiguous() or t.get_device() != ctx.device_index:
+    if t.dtype is not dtype or t.numel() != numel or t.get_device() != ctx.device_index or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous {dtype} tensor of {numel} elements on {ctx.device} is needed, got "
                          f"{tuple(t.shape)} {t.dtype} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
     return t.data_ptr()
@@ -266,12 +268,15 @@ def _need(ctx, name, t, dtype, numel, optional=False):
 
 def _call(ctx, where, fn, *args, stream=None):
     """One C call on the context's device: on `stream`, or on that device's current stream."""
-    if torch.cuda.current_device() != ctx.device_index:
-        with torch.cuda.device(ctx.device_index):
+    dev = ctx.device_index
+    if _current_device() != dev:
+        with torch.cuda.device(dev):
             return _call(ctx, where, fn, *args, stream=stream)
     if stream is None:
-        stream = torch.cuda.current_stream(ctx.device_index)
-    status = fn(ctx.handle, *args, stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
+        stream = _current_raw_stream(dev)     # torch.cuda.current_stream(dev).cuda_stream without making the object
+    elif hasattr(stream, "cuda_stream"):
+        stream = stream.cuda_stream
+    status = fn(ctx.handle, *args, stream)
     if status:
         _check(status, where)
 

@@ -69,28 +69,26 @@ __device__ void expert_zero_behind_rows(const ExpertArgs& a, const int* rows, ch
 }
 
 // ---- FMA tiles -----------------------------------------------------------------------------------------------------
-// A CTA of 256 threads owns a BM x BN tile, a thread TM x TN of it in two halves along each side (so that shared-memory
-// reads are conflict-free and a thread of the gated product holds the gate and the up value of the same column).  The
-// next 16-deep slice is in registers while the current one is multiplied.
-constexpr int kFmaBK = 16;
+// A CTA of 256 threads owns a BM x BN tile, a thread TM x TN of it in groups of four rows and four columns (one 16-byte
+// shared-memory read each, conflict-free; what bounds these tiles is those reads).  In the gated product a thread's columns are
+// half gate and half up, so that it holds both values of a column.  Products are packed two columns at a time, and the next
+// BK-deep slice is in registers while the current one is multiplied.
 __device__ __forceinline__ float4 load4(const float* p) { return __ldg(reinterpret_cast<const float4*>(p)); }
-__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
-  const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
-  return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16),
-                     __uint_as_float(v.y & 0xffff0000u));
-}
-__device__ __forceinline__ void put(float* p, float v) { *p = v; }
-__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }
 
-template <typename T, int BM, int BN, int EPI, bool A_MN, bool B_MN>
-__global__ void __launch_bounds__(256)
-expert_fma_kernel(const T* __restrict__ A, const T* __restrict__ B, const T* __restrict__ pre_in, void* __restrict__ out_raw,
-                  T* __restrict__ pre_out, ExpertArgs a) {
-  T* out = reinterpret_cast<T*>(out_raw);
-  constexpr int TM = BM / 16, TN = BN / 16, HM = TM / 2, HN = TN / 2;
-  constexpr int LA = BM * kFmaBK / 4 / 256, LB = BN * kFmaBK / 4 / 256;   // float4 loads per thread and slice
+template <int BM, int BN, int BK, int EPI, bool A_MN, bool B_MN>
+__global__ void __launch_bounds__(256, BM == 128 ? 2 : 4)
+expert_fma_kernel(const float* __restrict__ A, const float* __restrict__ B, const float* __restrict__ pre_in,
+                  float* __restrict__ out, float* __restrict__ pre_out, ExpertArgs a) {
+  constexpr int TM = BM / 16, TN = BN / 16;
+  constexpr int GM = TM < 4 ? TM : 4, GN = EPI == kEpiGlu ? TN / 2 : TN < 4 ? TN : 4;      // rows and columns of a group
+  constexpr int HN = TN / 2;
+  static_assert(GN % 2 == 0, "columns are packed in pairs");
+  // where a thread's i-th row / j-th column lies in the tile: groups are spread over the tile's halves
+  auto row_of = [](int i, int ty) { return i / GM * (BM / (TM / GM)) + ty * GM + i % GM; };
+  auto col_of = [](int j, int tx) { return j / GN * (BN / (TN / GN)) + tx * GN + j % GN; };
+  constexpr int LA = BM * BK / 4 / 256, LB = BN * BK / 4 / 256;   // float4 loads per thread and slice
   static_assert(LA >= 1 && LB >= 1, "tile too small for 256 threads");
-  __shared__ __align__(16) float sa[2][kFmaBK][BM + 4], sb[2][kFmaBK][BN + 4];
+  __shared__ __align__(16) float sa[2][BK][BM + 4], sb[2][BK][BN + 4];
   __shared__ int srows[kMaxE];
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   if (tid < a.E) srows[tid] = expert_rows(a, tid);
@@ -104,8 +102,8 @@ expert_fma_kernel(const T* __restrict__ A, const T* __restrict__ B, const T* __r
     const int ntm = EPI == kEpiDw ? ntm_dw : (rows + BM - 1) / BM;
     const int K = EPI == kEpiDw ? rows : a.K, M = EPI == kEpiDw ? a.M : rows;
     const long long n_tiles = (long long)ntm * ntn;
-    const T* Ae = A + (EPI == kEpiDw ? (size_t)e * a.C * a.M : (size_t)e * a.C * a.K);
-    const T* Be = B + (EPI == kEpiDw ? (size_t)e * a.C * a.N : (size_t)e * ldb_cols * a.K);
+    const float* Ae = A + (EPI == kEpiDw ? (size_t)e * a.C * a.M : (size_t)e * a.C * a.K);
+    const float* Be = B + (EPI == kEpiDw ? (size_t)e * a.C * a.N : (size_t)e * ldb_cols * a.K);
     for (; tile < first + n_tiles; tile += gridDim.x) {
       const int m0 = (int)((tile - first) / ntn) * BM, n0 = (int)((tile - first) % ntn) * BNU;
       float4 ra[LA], rb[LB];
@@ -113,15 +111,15 @@ expert_fma_kernel(const T* __restrict__ A, const T* __restrict__ B, const T* __r
 #pragma unroll
         for (int i = 0; i < LA; ++i) {
           const int q = tid + i * 256;
-          const int m = m0 + (A_MN ? (q % (BM / 4)) * 4 : q / 4), k = k0 + (A_MN ? q / (BM / 4) : (q % 4) * 4);
+          const int m = m0 + (A_MN ? (q % (BM / 4)) * 4 : q / (BK / 4)), k = k0 + (A_MN ? q / (BM / 4) : (q % (BK / 4)) * 4);
           ra[i] = (m < M && k < K) ? load4(A_MN ? Ae + (size_t)k * a.M + m : Ae + (size_t)m * a.K + k)
                                    : make_float4(0.f, 0.f, 0.f, 0.f);
         }
 #pragma unroll
         for (int i = 0; i < LB; ++i) {
           const int q = tid + i * 256;
-          int c = B_MN ? (q % (BN / 4)) * 4 : q / 4;
-          const int k = k0 + (B_MN ? q / (BN / 4) : (q % 4) * 4);
+          const int c = B_MN ? (q % (BN / 4)) * 4 : q / (BK / 4);
+          const int k = k0 + (B_MN ? q / (BN / 4) : (q % (BK / 4)) * 4);
           int n = n0 + c; bool in = n < a.N;
           if (EPI == kEpiGlu && c >= BNU) { n = n0 + c - BNU; in = n < a.N; n += a.N; }
           rb[i] = (in && k < K) ? load4(B_MN ? Be + (size_t)k * ldb_cols + n : Be + (size_t)n * a.K + k)
@@ -133,43 +131,45 @@ expert_fma_kernel(const T* __restrict__ A, const T* __restrict__ B, const T* __r
         for (int i = 0; i < LA; ++i) {
           const int q = tid + i * 256;
           if (A_MN) *reinterpret_cast<float4*>(&sa[s][q / (BM / 4)][(q % (BM / 4)) * 4]) = ra[i];
-          else { const int k = (q % 4) * 4, m = q / 4; sa[s][k][m] = ra[i].x; sa[s][k + 1][m] = ra[i].y; sa[s][k + 2][m] = ra[i].z; sa[s][k + 3][m] = ra[i].w; }
+          else { const int k = (q % (BK / 4)) * 4, m = q / (BK / 4); sa[s][k][m] = ra[i].x; sa[s][k + 1][m] = ra[i].y; sa[s][k + 2][m] = ra[i].z; sa[s][k + 3][m] = ra[i].w; }
         }
 #pragma unroll
         for (int i = 0; i < LB; ++i) {
           const int q = tid + i * 256;
           if (B_MN) *reinterpret_cast<float4*>(&sb[s][q / (BN / 4)][(q % (BN / 4)) * 4]) = rb[i];
-          else { const int k = (q % 4) * 4, n = q / 4; sb[s][k][n] = rb[i].x; sb[s][k + 1][n] = rb[i].y; sb[s][k + 2][n] = rb[i].z; sb[s][k + 3][n] = rb[i].w; }
+          else { const int k = (q % (BK / 4)) * 4, n = q / (BK / 4); sb[s][k][n] = rb[i].x; sb[s][k + 1][n] = rb[i].y; sb[s][k + 2][n] = rb[i].z; sb[s][k + 3][n] = rb[i].w; }
         }
       };
-      float acc[TM][TN];
+      float2 acc[TM][TN / 2];
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = 0.f;
-      const int slices = (K + kFmaBK - 1) / kFmaBK;
+        for (int j = 0; j < TN / 2; ++j) acc[i][j] = both(0.f);
+      const int slices = (K + BK - 1) / BK;
       if (slices > 0) { load(0); stash(0); }
       __syncthreads();
       for (int s = 0; s < slices; ++s) {
-        if (s + 1 < slices) load((s + 1) * kFmaBK);
+        if (s + 1 < slices) load((s + 1) * BK);
 #pragma unroll
-        for (int k = 0; k < kFmaBK; ++k) {
-          float x[TM], w[TN];
+        for (int k = 0; k < BK; ++k) {
+          float x[TM];
+          float2 w[TN / 2];
 #pragma unroll
-          for (int i = 0; i < HM; ++i) { x[i] = sa[s & 1][k][ty * HM + i]; x[HM + i] = sa[s & 1][k][BM / 2 + ty * HM + i]; }
+          for (int i = 0; i < TM; ++i) x[i] = sa[s & 1][k][row_of(i, ty)];
 #pragma unroll
-          for (int j = 0; j < HN; ++j) { w[j] = sb[s & 1][k][tx * HN + j]; w[HN + j] = sb[s & 1][k][BN / 2 + tx * HN + j]; }
+          for (int j = 0; j < TN / 2; ++j) w[j] = *reinterpret_cast<const float2*>(&sb[s & 1][k][col_of(2 * j, tx)]);
 #pragma unroll
           for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = fmaf(x[i], w[j], acc[i][j]);
+            for (int j = 0; j < TN / 2; ++j) acc[i][j] = fma2(both(x[i]), w[j], acc[i][j]);
         }
         if (s + 1 < slices) stash((s + 1) & 1);
         __syncthreads();
       }
+      auto at = [](const float2 (&r)[TN / 2], int j) { return j & 1 ? r[j >> 1].y : r[j >> 1].x; };
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
-        const int m = m0 + (i < HM ? ty * HM + i : BM / 2 + ty * HM + i - HM);
+        const int m = m0 + row_of(i, ty);
         if (m >= M) continue;
         if constexpr (EPI == kEpiGlu) {
 #pragma unroll
@@ -177,24 +177,26 @@ expert_fma_kernel(const T* __restrict__ A, const T* __restrict__ B, const T* __r
             const int n = n0 + tx * HN + j;
             if (n >= a.N) continue;
             const size_t row = (size_t)e * a.C + m;
-            if (pre_out) { put(pre_out + row * 2 * a.N + n, acc[i][j]); put(pre_out + row * 2 * a.N + a.N + n, acc[i][HN + j]); }
-            put(out + row * a.N + n, silu_mul<false>(acc[i][j], acc[i][HN + j]));
+            const float g = at(acc[i], j), u = at(acc[i], HN + j);
+            if (pre_out) { pre_out[row * 2 * a.N + n] = g; pre_out[row * 2 * a.N + a.N + n] = u; }
+            out[row * a.N + n] = silu_mul<false>(g, u);
           }
         } else {
 #pragma unroll
           for (int j = 0; j < TN; ++j) {
-            const int n = n0 + (j < HN ? tx * HN + j : BN / 2 + tx * HN + j - HN);
+            const int n = n0 + col_of(j, tx);
+            const float v = at(acc[i], j);
             if (n >= a.N) continue;
             if constexpr (EPI == kEpiDw) {
-              float* o = reinterpret_cast<float*>(out_raw) + ((size_t)e * a.M + m) * a.N + n;
-              *o = a.accumulate ? *o + acc[i][j] : acc[i][j];
+              float* o = out + ((size_t)e * a.M + m) * a.N + n;
+              *o = a.accumulate ? *o + v : v;
             } else if constexpr (EPI == kEpiDact) {
               const size_t row = ((size_t)e * a.C + m) * 2 * a.N;
               float dg, du;
-              dact<false>(acc[i][j], to_f(pre_in[row + n]), to_f(pre_in[row + a.N + n]), dg, du);
-              put(out + row + n, dg); put(out + row + a.N + n, du);
+              dact<false>(v, pre_in[row + n], pre_in[row + a.N + n], dg, du);
+              out[row + n] = dg; out[row + a.N + n] = du;
             } else {
-              put(out + ((size_t)e * a.C + m) * a.N + n, acc[i][j]);
+              out[((size_t)e * a.C + m) * a.N + n] = v;
             }
           }
         }
@@ -204,8 +206,8 @@ expert_fma_kernel(const T* __restrict__ A, const T* __restrict__ B, const T* __r
   }
   if constexpr (EPI != kEpiDw) {
     const int worker = blockIdx.x * 256 + tid, workers = gridDim.x * 256;
-    expert_zero_behind(a, srows, (char*)out, sizeof(T) * (size_t)(EPI == kEpiDact ? 2 * a.N : a.N), 1, worker, workers);
-    if (EPI == kEpiGlu && pre_out) expert_zero_behind(a, srows, (char*)pre_out, sizeof(T) * 2 * (size_t)a.N, 1, worker, workers);
+    expert_zero_behind(a, srows, (char*)out, sizeof(float) * (size_t)(EPI == kEpiDact ? 2 * a.N : a.N), 1, worker, workers);
+    if (EPI == kEpiGlu && pre_out) expert_zero_behind(a, srows, (char*)pre_out, sizeof(float) * 2 * (size_t)a.N, 1, worker, workers);
   }
 }
 

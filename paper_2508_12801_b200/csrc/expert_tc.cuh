@@ -427,7 +427,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
         }
         if constexpr (kDw) {
 #pragma unroll 1
-          for (int c0 = 0; c0 < 128; c0 += 32) {
+          for (int c0 = 0; c0 < kCols; c0 += 32) {
             uint32_t u[2][16];
             if (nkb > 0) {
               tmem_ld16_issue(acc + c0, u[0]); tmem_ld16_issue(acc + c0 + 16, u[1]);
@@ -444,7 +444,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
           }
         } else if constexpr (EPI == kEpiPlain) {
 #pragma unroll 1
-          for (int c0 = 0; c0 < 128; c0 += 64) {
+          for (int c0 = 0; c0 < kCols; c0 += 64) {
             uint32_t u[4][16];
 #pragma unroll
             for (int i = 0; i < 4; ++i) tmem_ld16_issue(acc + c0 + 16 * i, u[i]);

@@ -1033,17 +1033,19 @@ maxscore_status check_expert(const maxscore_ctx* c, std::initializer_list<const 
   return MAXSCORE_OK;
 }
 
-template <typename T, int EPI, bool A_MN, bool B_MN>
+template <int EPI, bool A_MN, bool B_MN>
 maxscore_status launch_fma(maxscore_ctx* c, const void* A, const void* B, const void* pre_in, void* out, void* pre_out,
                            const ExpertArgs& a, cudaStream_t st) {
-  // 128 x 128 tiles once the batch could fill the SMs with them, 64 x 64 below
-  const long long rows = (long long)c->p.T * c->p.k;
-  const long long big = EPI == kEpiDw ? (long long)a.E * ((a.M + 127) / 128) * ((a.N + 127) / 128)
-                                      : (rows + 127) / 128 * ((a.N * (EPI == kEpiGlu ? 2 : 1) + 127) / 128);
-  if (big >= 2 * c->sm_count)
-    expert_fma_kernel<T, 128, 128, EPI, A_MN, B_MN><<<c->sm_count * 2, 256, 0, st>>>((const T*)A, (const T*)B, (const T*)pre_in, out, (T*)pre_out, a);
-  else
-    expert_fma_kernel<T, 64, 64, EPI, A_MN, B_MN><<<c->sm_count * 4, 256, 0, st>>>((const T*)A, (const T*)B, (const T*)pre_in, out, (T*)pre_out, a);
+  // 128 x 128 tiles where they give every SM two of them, else 64 x 64
+  const long long rows = (long long)c->p.T * c->p.k, cols = (long long)a.N * (EPI == kEpiGlu ? 2 : 1);
+  auto tiles = [&](int m, int n) {
+    return (EPI == kEpiDw ? (long long)a.E * ((a.M + m - 1) / m) : (rows + m - 1) / m) * ((cols + n - 1) / n);
+  };
+  auto go = [&](auto kernel, int per_sm) {
+    kernel<<<c->sm_count * per_sm, 256, 0, st>>>((const float*)A, (const float*)B, (const float*)pre_in, (float*)out, (float*)pre_out, a);
+  };
+  if (tiles(128, 128) >= 2 * c->sm_count) go(expert_fma_kernel<128, 128, 16, EPI, A_MN, B_MN>, 2);
+  else go(expert_fma_kernel<64, 64, 16, EPI, A_MN, B_MN>, 4);
   MS_LAUNCH_CHECK("expert_fma_kernel");
   c->launches += 1;
   return MAXSCORE_OK;
@@ -1141,9 +1143,9 @@ maxscore_status launch_expert(maxscore_ctx* c, const void* A, const void* B, con
     else return b_mn ? launch_tc<EPI, true>(c, A, B, pre_in, out, pre_out, a, st)
                      : launch_tc<EPI, false>(c, A, B, pre_in, out, pre_out, a, st);
   }
-  if constexpr (EPI == kEpiDw) return launch_fma<float, EPI, true, true>(c, A, B, pre_in, out, pre_out, a, st);
-  else return b_mn ? launch_fma<float, EPI, false, true>(c, A, B, pre_in, out, pre_out, a, st)
-                   : launch_fma<float, EPI, false, false>(c, A, B, pre_in, out, pre_out, a, st);
+  if constexpr (EPI == kEpiDw) return launch_fma<EPI, true, true>(c, A, B, pre_in, out, pre_out, a, st);
+  else return b_mn ? launch_fma<EPI, false, true>(c, A, B, pre_in, out, pre_out, a, st)
+                   : launch_fma<EPI, false, false>(c, A, B, pre_in, out, pre_out, a, st);
 }
 
 ExpertArgs expert_args(const maxscore_ctx* c, const int32_t* load, int M, int N, int K, int accumulate = 0) {

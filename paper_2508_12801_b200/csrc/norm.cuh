@@ -112,20 +112,6 @@ __device__ __forceinline__ void norm_ring_end(bool ok, unsigned* error_flag) {
 // ---- pairs of floats: one instruction for two values ----------------------------------------------------------------
 // The kernels are short of instruction slots before they are short of bandwidth (a token passes 8 to 48 bytes an element
 // through some twenty operations each), so the arithmetic is done on packed pairs.
-typedef unsigned long long u64;
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-  u64 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<u64&>(a)), "l"(reinterpret_cast<u64&>(b)));
-  return reinterpret_cast<float2&>(r);
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  u64 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<u64&>(a)), "l"(reinterpret_cast<u64&>(b)));
-  return reinterpret_cast<float2&>(r);
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  u64 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(reinterpret_cast<u64&>(a)), "l"(reinterpret_cast<u64&>(b)), "l"(reinterpret_cast<u64&>(c)));
-  return reinterpret_cast<float2&>(r);
-}
-__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 template <typename T> __device__ __forceinline__ void unpack2(const uint4& v, float2 (&f)[Vec16<T>::N / 2]);
 template <> __device__ __forceinline__ void unpack2<float>(const uint4& v, float2 (&f)[2]) {
   f[0] = make_float2(__uint_as_float(v.x), __uint_as_float(v.y)); f[1] = make_float2(__uint_as_float(v.z), __uint_as_float(v.w));
