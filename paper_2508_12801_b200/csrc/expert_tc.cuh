@@ -163,8 +163,8 @@ __device__ __forceinline__ void expert_prefix(const ExpertArgs& a, int* rows, in
 
 // EPI as in expert.cuh.  B_MN: B is stored with its columns contiguous.  dW: both operands run along the rows.
 // Maps: tA; tB0 / tB1 = B of the leading / the other CTA (gate and up columns in the gated form, else the same).
-// tO0: y or h; tO1 / tO2: g / u kept (gated).  out: y, h, dpre or dW; pre_out: [g | u] kept or null; pre_in: [g | u] (backward).
-template <int EPI, bool B_MN, int W>
+// Add: dW is added to.  tO0: y or h; tO1 / tO2: g / u kept (gated).  out: y, h, dpre or dW; pre_out: [g | u] kept or null; pre_in: [g | u] (backward).
+template <int EPI, bool B_MN, int W, bool Add = false>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(x_threads(EPI))
 expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUtensorMap tB0, const __grid_constant__ CUtensorMap tB1,
                  const __grid_constant__ CUtensorMap tO0, const __grid_constant__ CUtensorMap tO1, const __grid_constant__ CUtensorMap tO2,
@@ -350,28 +350,29 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
     constexpr int kRow = EPI == kEpiDact ? 64 : 128, kPer = kRow / 16, kRows = 32 / kPer;      // bytes of a box row; chunks; rows a warp moves at once
     auto swz = [](int r) { return kRow == 128 ? r & 7 : (r >> 1) & 3; };
     auto to_box = [&](unsigned char* box, int i, uint4 v) { *reinterpret_cast<uint4*>(box + lane * kRow + ((i ^ swz(lane)) << 4)) = v; };
-    // box -> memory: rows and bytes beyond the tensor are left out; add: fp32 sums instead of stores
-    auto box_out = [&](const unsigned char* box, char* dst, size_t stride, int rows, int bytes, bool add) {
-      __syncwarp();
-      const int c = lane % kPer;
+    // box -> memory: rows and bytes beyond the tensor are left out; Add: fp32 sums instead of stores.  (Kept small, and the sums
+    // a form of the kernel of their own: the MMA warp's loop shares the instruction cache with this.  dW at E 64, C 1024,
+    // 2048 x 2048: 480 us; 537 us with a branch on adding.)
+    auto box_out = [&](const unsigned char* box, char* dst, size_t stride, int rows, int bytes) {
+      const int c = (int)((unsigned)lane % kPer), r0 = (int)((unsigned)lane / kPer);
+      if (c * 16 >= bytes) rows = 0;
+      dst += r0 * stride + c * 16;
       float4 old[kPer];
-      if (kDw && add) {
+      if constexpr (Add) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          const int r = i * kRows + lane / kPer;
-          if (r < rows && c * 16 < bytes) old[i] = *reinterpret_cast<const float4*>(dst + r * stride + c * 16);
-        }
+        for (int i = 0; i < kPer; ++i)
+          if (i * kRows + r0 < rows) old[i] = *reinterpret_cast<const float4*>(dst + i * kRows * stride);
       }
+      __syncwarp();
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        const int r = i * kRows + lane / kPer;
+        const int r = i * kRows + r0;
         uint4 v = *reinterpret_cast<const uint4*>(box + r * kRow + ((c ^ swz(r)) << 4));
-        if (r < rows && c * 16 < bytes) {
-          if (kDw && add)
-            v = make_uint4(__float_as_uint(old[i].x + __uint_as_float(v.x)), __float_as_uint(old[i].y + __uint_as_float(v.y)),
-                           __float_as_uint(old[i].z + __uint_as_float(v.z)), __float_as_uint(old[i].w + __uint_as_float(v.w)));
-          *reinterpret_cast<uint4*>(dst + r * stride + c * 16) = v;
-        }
+        if constexpr (Add)
+          v = make_uint4(__float_as_uint(old[i].x + __uint_as_float(v.x)), __float_as_uint(old[i].y + __uint_as_float(v.y)),
+                         __float_as_uint(old[i].z + __uint_as_float(v.z)), __float_as_uint(old[i].w + __uint_as_float(v.w)));
+        if (r < rows) *reinterpret_cast<uint4*>(dst) = v;
+        dst += kRows * stride;
       }
       __syncwarp();
     };
@@ -436,11 +437,11 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
 #pragma unroll
               for (int i = 0; i < 16; ++i) u[0][i] = u[1][i] = 0;
             }
-            if (nkb == 0 && a.accumulate) continue;                    // an expert without rows adds nothing
+            if (Add && nkb == 0) continue;                             // an expert without rows adds nothing
 #pragma unroll
             for (int i = 0; i < 8; ++i)
               to_box(stage, i, make_uint4(u[i >> 2][(i & 3) * 4], u[i >> 2][(i & 3) * 4 + 1], u[i >> 2][(i & 3) * 4 + 2], u[i >> 2][(i & 3) * 4 + 3]));
-            box_out(stage, out + (row0 * a.N + col0 + c0) * 4, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 4, a.accumulate != 0);
+            box_out(stage, out + (row0 * a.N + col0 + c0) * 4, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 4);
           }
         } else if constexpr (EPI == kEpiPlain) {
 #pragma unroll 1
@@ -521,8 +522,8 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
               *pu = make_uint4(wu[0], wu[1], wu[2], wu[3]);
             }
             char* dst = out + (row0 * 2 * a.N + col0 + c0) * 2;
-            box_out(stage, dst, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 2, false);
-            box_out(stage + 32 * kRow, dst + (size_t)a.N * 2, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 2, false);
+            box_out(stage, dst, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 2);
+            box_out(stage + 32 * kRow, dst + (size_t)a.N * 2, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 2);
           }
         }
         if (nkb > 0) {
