@@ -103,6 +103,12 @@ struct XSmem {
   int rows[kMaxE], first[kMaxE + 1];     // rows in use; tiles before each expert
 };
 
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&u)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]) : "r"(taddr));
+  tmem_ld_wait();
+}
+
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<uint32_t*>(&h);
@@ -350,6 +356,13 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
     constexpr int kRow = EPI == kEpiDact ? 64 : 128, kPer = kRow / 16, kRows = 32 / kPer;      // bytes of a box row; chunks; rows a warp moves at once
     auto swz = [](int r) { return kRow == 128 ? r & 7 : (r >> 1) & 3; };
     auto to_box = [&](unsigned char* box, int i, uint4 v) { *reinterpret_cast<uint4*>(box + lane * kRow + ((i ^ swz(lane)) << 4)) = v; };
+    auto put16 = [&](unsigned char* box, int i, const uint32_t (&u)[16], bool keep) {      // the i-th 16 values of the row, as bf16
+      uint32_t w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = keep ? pack_bf16(__uint_as_float(u[2 * j]), __uint_as_float(u[2 * j + 1])) : 0u;
+      to_box(box, 2 * i, make_uint4(w[0], w[1], w[2], w[3]));
+      to_box(box, 2 * i + 1, make_uint4(w[4], w[5], w[6], w[7]));
+    };
     // box -> memory: rows and bytes beyond the tensor are left out; Add: fp32 sums instead of stores.  (Kept small, and the sums
     // a form of the kernel of their own: the MMA warp's loop shares the instruction cache with this.  dW at E 64, C 1024,
     // 2048 x 2048: 480 us; 537 us with a branch on adding.)
@@ -452,74 +465,52 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
             tmem_ld_wait();
             unsigned char* to = next_box();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              uint32_t w[4];
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const int at = (i & 1) * 8 + 2 * j;
-                w[j] = keep_row ? pack_bf16(__uint_as_float(u[i >> 1][at]), __uint_as_float(u[i >> 1][at + 1])) : 0u;
-              }
-              to_box(to, i, make_uint4(w[0], w[1], w[2], w[3]));
-            }
+            for (int i = 0; i < 4; ++i) put16(to, i, u[i], keep_row);
             box_store(&tO0, col0 + c0, y0, x.e, rows > 0 && col0 + c0 < a.N);
           }
         } else if constexpr (EPI == kEpiGlu) {
-          uint32_t hw[32], gw[32], uw[32];
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            uint32_t g[2][16], u[2][16];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              tmem_ld16_issue(acc + half * 32 + 16 * i, g[i]);
-              tmem_ld16_issue(acc + 128 + half * 32 + 16 * i, u[i]);
-            }
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float g0 = __uint_as_float(g[i >> 3][(i & 7) * 2]), g1 = __uint_as_float(g[i >> 3][(i & 7) * 2 + 1]);
-              const float u0 = __uint_as_float(u[i >> 3][(i & 7) * 2]), u1 = __uint_as_float(u[i >> 3][(i & 7) * 2 + 1]);
-              hw[half * 16 + i] = keep_row ? pack_bf16(silu_mul<true>(g0, u0), silu_mul<true>(g1, u1)) : 0u;
-              gw[half * 16 + i] = keep_row ? pack_bf16(g0, g1) : 0u;
-              uw[half * 16 + i] = keep_row ? pack_bf16(u0, u1) : 0u;
-            }
-          }
-          auto emit = [&](const CUtensorMap* tm, const uint32_t (&w)[32]) {
+          // h, then g and u if they are kept: the accumulator is read again for each rather than held in registers
+#pragma unroll 1
+          for (int what = 0; what < (pre_out ? 3 : 1); ++what) {
             unsigned char* to = next_box();
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+              uint32_t g[16], u[16];
+              tmem_ld16_issue(acc + 16 * i + (what == 2 ? 128 : 0), g);
+              if (what == 0) tmem_ld16_issue(acc + 128 + 16 * i, u);
+              tmem_ld_wait();
+              if (what == 0) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) to_box(to, i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
-            box_store(tm, col0, y0, x.e, rows > 0 && col0 < a.N);
-          };
-          emit(&tO0, hw);
-          if (pre_out) { emit(&tO1, gw); emit(&tO2, uw); }
+                for (int j = 0; j < 16; ++j) g[j] = __float_as_uint(silu_mul<true>(__uint_as_float(g[j]), __uint_as_float(u[j])));
+              }
+              put16(to, i, g, keep_row);
+            }
+            box_store(what == 0 ? &tO0 : what == 1 ? &tO1 : &tO2, col0, y0, x.e, rows > 0 && col0 < a.N);
+          }
         } else {
           // dh in the accumulator; g and u sit in a pair of boxes, which dg and du then leave from
 #pragma unroll 1
           for (int c0 = 0; c0 < kCols; c0 += 32) {
             if (c0) fetch(row0, rows, col0 + c0);                      // the first one was asked for ahead of the accumulator
-            uint32_t u[2][16];
-            tmem_ld16_issue(acc + c0, u[0]); tmem_ld16_issue(acc + c0 + 16, u[1]);
-            tmem_ld_wait();
             asm volatile("cp.async.wait_group 0;" ::: "memory");
             __syncwarp();
             unsigned char* row = stage + lane * kRow;
-#pragma unroll
+#pragma unroll 1
             for (int i = 0; i < 4; ++i) {
+              uint32_t u[8];
+              tmem_ld8(acc + c0 + 8 * i, u);
               uint4* pg = reinterpret_cast<uint4*>(row + ((i ^ swz(lane)) << 4));
               uint4* pu = reinterpret_cast<uint4*>(row + 32 * kRow + ((i ^ swz(lane)) << 4));
               float g[8], up[8];
               Vec16<__nv_bfloat16>::unpack(*pg, g); Vec16<__nv_bfloat16>::unpack(*pu, up);
-              uint32_t wg[4], wu[4];
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                float d0, d1, e0, e1;
-                const int at = (i & 1) * 8 + 2 * j;
-                dact<true>(__uint_as_float(u[i >> 1][at]), g[2 * j], up[2 * j], d0, e0);
-                dact<true>(__uint_as_float(u[i >> 1][at + 1]), g[2 * j + 1], up[2 * j + 1], d1, e1);
-                wg[j] = keep_row ? pack_bf16(d0, d1) : 0u;
-                wu[j] = keep_row ? pack_bf16(e0, e1) : 0u;
+              for (int j = 0; j < 8; ++j) {
+                float dg, du;
+                dact<true>(__uint_as_float(u[j]), g[j], up[j], dg, du);
+                g[j] = keep_row ? dg : 0.f; up[j] = keep_row ? du : 0.f;
               }
-              *pg = make_uint4(wg[0], wg[1], wg[2], wg[3]);
-              *pu = make_uint4(wu[0], wu[1], wu[2], wu[3]);
+              Vec16<__nv_bfloat16>::store(reinterpret_cast<__nv_bfloat16*>(pg), g);
+              Vec16<__nv_bfloat16>::store(reinterpret_cast<__nv_bfloat16*>(pu), up);
             }
             char* dst = out + (row0 * 2 * a.N + col0 + c0) * 2;
             box_out(stage, dst, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 2);
