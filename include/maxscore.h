@@ -23,7 +23,8 @@
  *   - Every wait inside a kernel is bounded.  A wait that runs out raises the context's internal-error
  *     flag and the kernel returns with its output incomplete.  maxscore_route_fwd and maxscore_assign
  *     report the flag as MAXSCORE_STAT_INTERNAL in stats.status and clear it; after the calls that write
- *     no stats (maxscore_gate, maxscore_gate_bwd, maxscore_route_bwd) read it with maxscore_check_internal.
+ *     no stats (maxscore_gate, maxscore_gate_bwd, maxscore_route_bwd, the experts and the norms) read it with
+ *     maxscore_check_internal.
  *   - expert_idx[i, :] is ascending.  slot_idx[i, c] is the rank of token i among the tokens of expert
  *     expert_idx[i, c], in ascending token order.  Unused slots of slot_token hold -1.
  *   - If the solver runs out of its budget (MAXSCORE_STAT_NOT_CONVERGED; never seen with the default
@@ -267,7 +268,7 @@ maxscore_status maxscore_gate_bwd(maxscore_ctx* ctx, const void* hidden, const v
  *   w_layout 0: weights are [E, d_in, d_out] as w_gate in Eq. 2;  1: [E, d_out, d_in].
  *   Widths (d_in, d_out, d_ff) need not be d_model; a multiple of 8 for bf16 I/O and of 4 for fp32, as d_model.
  * Products are accumulated in fp32 and rounded once.  Outputs must not overlap inputs.  Reproducible bit for bit.
- * After the bf16 calls maxscore_check_internal tells whether a bounded wait gave up, as for maxscore_gate.
+ * After these calls maxscore_check_internal tells whether a bounded wait gave up, as for maxscore_gate.
  * Errors: NULL (unless said otherwise) or misaligned pointers, an output that is an input's own buffer, non-positive
  * widths, w_layout not 0 or 1 -> MAXSCORE_ERR_INVALID_ARG; widths that are no such multiple -> MAXSCORE_ERR_UNSUPPORTED. */
 
@@ -305,9 +306,12 @@ maxscore_status maxscore_expert_glu_bwd(maxscore_ctx* ctx, const void* dy, const
  *   n_i  = y_i / rms(y_i) * (w_offset + w_post)                 w_post NULL: n = y
  *   r'_i = res_scale * residual_i + gate[i / rows_per_gate] * n_i    gate NULL: n is added as it is
  *   h_i  = r'_i / rms(r'_i) * (w_offset + w_pre)                w_pre NULL: no h
- * with rms(v)^2 = mean(v^2) + eps.  y and r' are rounded to io_dtype and each norm takes the rounded row, so that the
- * backward call, which is handed those rows, works from the same numbers.  Sums are fp32.
+ * with rms(v)^2 = mean(v^2) + eps.  A row passes through the steps in fp32; y, r' and h are each rounded to io_dtype once,
+ * when they are stored.  The backward call works from the stored rows.
  *   w_post, w_pre [d_model], gate [ceil(T / rows_per_gate), d_model]: DEVICE memory, io_dtype, 16-byte aligned.
+ * After these calls maxscore_check_internal tells whether a bounded wait gave up.
+ * Errors: a NULL that is not allowed below, a misaligned pointer, eps or rows_per_gate out of range, an output that is
+ * another argument's buffer (but for the two pairs named below) -> MAXSCORE_ERR_INVALID_ARG.
  * Limits: d_model <= 16384 for bf16 I/O, 8192 for fp32 (MAXSCORE_ERR_UNSUPPORTED). */
 typedef struct {
   const void* w_post;    /* after-norm weight or NULL                                              */
@@ -322,7 +326,7 @@ typedef struct {
 /* maxscore_combine followed by the steps above, without the round trip of y through memory.
  *   src, expert_idx, slot_idx, gate_w as in maxscore_combine (gate_w NULL = unit weights)
  *   residual [T, d_model] in; y [T, d_model] out or NULL (what maxscore_combine would have written, bit for bit; the
- *   backward call needs it); r_out [T, d_model] out (may be residual's buffer); h [T, d_model] out, NULL iff w_pre is. */
+ *   backward call needs it; the norm takes it before its rounding); r_out [T, d_model] out (may be residual's buffer); h [T, d_model] out, NULL iff w_pre is. */
 maxscore_status maxscore_combine_norm(maxscore_ctx* ctx, const void* src, const int32_t* expert_idx, const int32_t* slot_idx,
                                       const float* gate_w, const void* residual, const maxscore_norm* norm, void* y,
                                       void* r_out, void* h, void* cuda_stream);

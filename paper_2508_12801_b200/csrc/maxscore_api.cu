@@ -9,6 +9,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <atomic>
 #include <initializer_list>
 #include <new>
 #include <type_traits>
@@ -517,7 +518,8 @@ maxscore_status maxscore_create(maxscore_ctx** out, const maxscore_params* param
   MS_CUDA(cudaFuncSetAttribute(gate_bwd_dh_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDhSmemMax));
   MS_CUDA(cudaFuncSetAttribute(gate_bwd_dw_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDwSmemMax));
   MS_CUDA(cudaFuncSetAttribute(dispatch_tma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kTmaWarps * kTmaStages * kTmaChunk));
-  {
+  static std::atomic<uint64_t> ready{0};                 // devices on which the kernels below have their shared memory
+  if (dev >= 64 || !(ready.load(std::memory_order_acquire) >> dev & 1)) {
     cudaError_t e_ = cudaSuccess;
     auto room = [&](auto kernel, int bytes) { if (e_ == cudaSuccess) e_ = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
     room(expert_tc_kernel<kEpiPlain, false, 1>, x_smem(kEpiPlain, 1)); room(expert_tc_kernel<kEpiPlain, false, 2>, x_smem(kEpiPlain, 2));
@@ -530,6 +532,7 @@ maxscore_status maxscore_create(maxscore_ctx** out, const maxscore_params* param
     room(expert_few_kernel<kEpiGlu, false>, few_smem(kEpiGlu, kFewRows)); room(expert_few_kernel<kEpiGlu, true>, few_smem(kEpiGlu, kFewRows));
     norm_room<float, true>(room); norm_room<float, false>(room); norm_room<__nv_bfloat16, true>(room); norm_room<__nv_bfloat16, false>(room);
     if (e_ != cudaSuccess) return cuda_fail(e_, "cudaFuncSetAttribute(expert and norm kernels)");
+    if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
   }
   int coop = 0, sweep_occ = 0;
   MS_CUDA(cudaDeviceGetAttribute(&coop, cudaDevAttrCooperativeLaunch, dev));

@@ -1,12 +1,12 @@
 // Norms before and after a block, fused with its gate and the scaled residual; optionally with combine in front.
 //
-//   y_i  = combine of the token's expert rows (Eq. 1), or given           rounded to the I/O type
+//   y_i  = combine of the token's expert rows (Eq. 1), or given
 //   n_i  = y_i / rms(y_i) * (offset + w_post)                             rms(v)^2 = mean(v^2) + eps
-//   r'_i = res_scale * r_i + gate_(i / rows_per_gate) * n_i               rounded to the I/O type
+//   r'_i = res_scale * r_i + gate_(i / rows_per_gate) * n_i
 //   h_i  = r'_i / rms(r'_i) * (offset + w_pre)
 //
-// Both norms take the rounded value that is also returned, so that the backward pass, which is handed those, forms the
-// same statistics again instead of having them stored.  Sums are fp32.
+// A row passes through in fp32: y, r' and h are each rounded once, when they are stored, and the steps behind take the values
+// before that.  The backward pass forms the statistics again from the stored rows instead of having them stored too.
 //
 // All of it is bound by HBM.  A producer warp streams the rows of the coming tokens into a ring of row buffers in shared
 // memory (bulk copies on mbarriers), so the loads never wait for the two reductions a token goes through; a group of G
@@ -227,14 +227,14 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
   long long gate_end = 0;                               // first token behind the present gate row
   for (int tok = blockIdx.x; tok < a.T; tok += gridDim.x) {
     const size_t row = (size_t)tok * a.d;
-    uint4 rv[V], yv[V];
+    float2 r[V][P], y[V][P];
     {
       const uint4* p = group.take();
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const int v = threadIdx.x + j * G;
-        rv[j] = mine(v) ? p[v] : zero;
-        if (SRC == 1) yv[j] = mine(v) ? p[a.nvec + v] : zero;
+        unpack2<T>(mine(v) ? p[v] : zero, r[j]);
+        if (SRC == 1) unpack2<T>(mine(v) ? p[a.nvec + v] : zero, y[j]);
       }
     }
     if (SRC == 2) {
@@ -243,11 +243,10 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
 #pragma unroll
       for (int c = 0; c < kMaxK; ++c) wgt[c] = sm.weight[group.s][c];
       group.release();
-      float2 acc[V][P];
 #pragma unroll
       for (int j = 0; j < V; ++j)
 #pragma unroll
-        for (int i = 0; i < P; ++i) acc[j][i] = both(0.f);
+        for (int i = 0; i < P; ++i) y[j][i] = both(0.f);
 #pragma unroll
       for (int c = 0; c < kMaxK; ++c)
         if (c < n) {
@@ -258,15 +257,14 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
             float2 x[P];
             unpack2<T>(mine(v) ? p[v] : zero, x);
 #pragma unroll
-            for (int i = 0; i < P; ++i) acc[j][i] = fma2(both(wgt[c]), x[i], acc[j][i]);
+            for (int i = 0; i < P; ++i) y[j][i] = fma2(both(wgt[c]), x[i], y[j][i]);
           }
           group.release();
         }
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const int v = threadIdx.x + j * G;
-        yv[j] = pack2<T>(acc[j]);
-        if (y_out && mine(v) && group.ok) __stcs(reinterpret_cast<uint4*>(y_out + row + (size_t)v * N), yv[j]);
+        if (y_out && mine(v) && group.ok) __stcs(reinterpret_cast<uint4*>(y_out + row + (size_t)v * N), pack2<T>(y[j]));
       }
     } else {
       group.release();
@@ -280,44 +278,31 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
     if (SRC && a.w_post) {
       float2 s = both(0.f);
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        float2 y[P];
-        unpack2<T>(yv[j], y);
+      for (int j = 0; j < V; ++j)
 #pragma unroll
-        for (int i = 0; i < P; ++i) s = fma2(y[i], y[i], s);
-      }
+        for (int i = 0; i < P; ++i) s = fma2(y[j][i], y[j][i], s);
       inv_y = rsqrtf(group.sum(s.x + s.y) * inv_d + a.eps);
     }
     float2 s = both(0.f);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const int v = threadIdx.x + j * G;
-      float2 r[P], y[P];
-      unpack2<T>(rv[j], r);
-      if (SRC) unpack2<T>(yv[j], y);
 #pragma unroll
       for (int i = 0; i < P; ++i) {
-        r[i] = mul2(scale, r[i]);
-        if (SRC) r[i] = fma2(mul2(y[i], both(inv_y)), gw[j][i], r[i]);
+        r[j][i] = mul2(scale, r[j][i]);
+        if (SRC) r[j][i] = fma2(mul2(y[j][i], both(inv_y)), gw[j][i], r[j][i]);
+        s = fma2(r[j][i], r[j][i], s);
       }
-      rv[j] = pack2<T>(r);
-      if (mine(v)) {
-        if (r_out && group.ok) __stcs(reinterpret_cast<uint4*>(r_out + row + (size_t)v * N), rv[j]);
-        unpack2<T>(rv[j], r);
-#pragma unroll
-        for (int i = 0; i < P; ++i) s = fma2(r[i], r[i], s);
-      }
+      if (r_out && mine(v) && group.ok) __stcs(reinterpret_cast<uint4*>(r_out + row + (size_t)v * N), pack2<T>(r[j]));
     }
     if (h) {
       const float2 inv = both(rsqrtf(group.sum(s.x + s.y) * inv_d + a.eps));
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const int v = threadIdx.x + j * G;
-        float2 r[P];
-        unpack2<T>(rv[j], r);
 #pragma unroll
-        for (int i = 0; i < P; ++i) r[i] = mul2(mul2(r[i], inv), wpre[j][i]);
-        if (mine(v) && group.ok) __stcs(reinterpret_cast<uint4*>(h + row + (size_t)v * N), pack2<T>(r));
+        for (int i = 0; i < P; ++i) r[j][i] = mul2(mul2(r[j][i], inv), wpre[j][i]);
+        if (mine(v) && group.ok) __stcs(reinterpret_cast<uint4*>(h + row + (size_t)v * N), pack2<T>(r[j]));
       }
     }
   }
