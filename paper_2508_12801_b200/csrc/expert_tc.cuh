@@ -83,6 +83,10 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {     // arrives
 
 // ---- the kernel ----------------------------------------------------------------------------------------------------
 constexpr int kXTile = 256, kXBK = 64;
+// The tensor pipe cuts the accumulator off at 24 bits with every MMA instead of rounding it, so a long coherent sum shrinks by
+// about 1.1e-9 of itself a row.  dW folds its accumulator into the fp32 result in memory, with rounding, every 4096 rows: its
+// error stays below 5e-6 of the sum (8e-5 over 66 000 rows without).  Capacities up to that need no fold.
+constexpr int kXFoldRows = 4096, kXFoldKb = kXFoldRows / kXBK;
 // W: column tiles of a pair at a time (1: 256 x 256, two accumulators in turn; 2: 256 x 512)
 __host__ __device__ constexpr int x_stage_bytes(int w) { return 16384 * (1 + w); }
 // Epilogue warps: two for each of the four TMEM lane quarters; four in the backward of the activation, whose epilogue (two
@@ -169,13 +173,13 @@ __device__ __forceinline__ void expert_prefix(const ExpertArgs& a, int* rows, in
 
 // EPI as in expert.cuh.  B_MN: B is stored with its columns contiguous.  dW: both operands run along the rows.
 // Maps: tA; tB0 / tB1 = B of the leading / the other CTA (gate and up columns in the gated form, else the same).
-// Add: dW is added to.  tO0: y or h; tO1 / tO2: g / u kept (gated).  out: y, h, dpre or dW; pre_out: [g | u] kept or null; pre_in: [g | u] (backward).
+// Add: dW is added to, or its rows may be more than one sum takes.  tO0: y or h; tO1 / tO2: g / u kept (gated).  out: y, h, dpre or dW; pre_out: [g | u] kept or null; pre_in: [g | u] (backward).
 template <int EPI, bool B_MN, int W, bool Add = false>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(x_threads(EPI))
 expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUtensorMap tB0, const __grid_constant__ CUtensorMap tB1,
                  const __grid_constant__ CUtensorMap tO0, const __grid_constant__ CUtensorMap tO1, const __grid_constant__ CUtensorMap tO2,
                  char* __restrict__ out, char* __restrict__ pre_out, const char* __restrict__ pre_in, ExpertArgs a, unsigned* error_flag) {
-  constexpr bool kDw = EPI == kEpiDw, kA_MN = kDw;
+  constexpr bool kDw = EPI == kEpiDw, kA_MN = kDw, kFold = kDw && Add;
   constexpr int kEpiWarps = x_epi_warps(EPI);
   constexpr int kStages = x_stages(EPI, W), kStageBytes = x_stage_bytes(W);
   constexpr int kTileN = EPI == kEpiGlu ? 128 : kXTile;               // output columns of a tile
@@ -302,15 +306,17 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       // With two column tiles the first and the last slices are multiplied group-wise, the first column tile ahead of the
       // second: its accumulator is complete (and free again) that much earlier, which is what hides the epilogues.
       const int group = x.subs == 2 ? kStages : 1;
+      int begin = 0, end = kFold ? min(nkb, kXFoldKb) : nkb;           // slices of the present sum
       for (int kb = 0; kb < nkb && ok;) {
-        const int n = (kb == 0 || nkb - kb <= group) ? min(group, nkb - kb) : 1;
+        if (kFold && kb == end) { begin = end; end = min(nkb, end + kXFoldKb); }
+        const int n = (kb == begin || end - kb <= group) ? min(group, end - kb) : 1;
         int s = s0;
 #pragma unroll
         for (int h = 0; h < W; ++h) {
           if (h >= x.subs) break;
           const uint32_t buf = W == 2 ? h : turn & 1;
           const uint32_t acc = tmem + buf * 256;
-          if (kb == 0) { ok = ok && mbar_wait_bounded(&sm.acc_empty[buf], (acc_ph >> buf) & 1); acc_ph ^= 1u << buf; }
+          if (kb == begin) { ok = ok && mbar_wait_bounded(&sm.acc_empty[buf], (acc_ph >> buf) & 1); acc_ph ^= 1u << buf; }
           s = s0;
           uint32_t ph = full_ph;
           for (int j = 0; j < n; ++j) {
@@ -320,12 +326,12 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
             const uint64_t ad = adesc0 + (uint64_t)(s * (kStageBytes / 16)), bd = bdesc0 + (uint64_t)(s * (kStageBytes / 16) + h * 1024);
             const int left = K - (kb + j) * kXBK;
             if (elect_one()) {
-              umma_bf16_pair(acc, ad, bd, idesc, kb + j > 0 ? 1u : 0u);
+              umma_bf16_pair(acc, ad, bd, idesc, kb + j > begin ? 1u : 0u);
               if (left > 16) umma_bf16_pair(acc, ad + kAStep, bd + kBStep, idesc, 1u);
               if (left > 32) umma_bf16_pair(acc, ad + 2 * kAStep, bd + 2 * kBStep, idesc, 1u);
               if (left > 48) umma_bf16_pair(acc, ad + 3 * kAStep, bd + 3 * kBStep, idesc, 1u);
               if (h == x.subs - 1) umma_commit_pair(&sm.empty[s]);
-              if (kb + j == nkb - 1) umma_commit_pair(&sm.acc_full[buf]);
+              if (kb + j == end - 1) umma_commit_pair(&sm.acc_full[buf]);
             }
             __syncwarp();
             if (++s == kStages) { s = 0; ph ^= 1; }
@@ -363,10 +369,10 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       to_box(box, 2 * i, make_uint4(w[0], w[1], w[2], w[3]));
       to_box(box, 2 * i + 1, make_uint4(w[4], w[5], w[6], w[7]));
     };
-    // box -> memory: rows and bytes beyond the tensor are left out; Add: fp32 sums instead of stores.  (Kept small, and the sums
+    // box -> memory: rows and bytes beyond the tensor are left out; add: fp32 sums instead of stores.  (Kept small, and the sums
     // a form of the kernel of their own: the MMA warp's loop shares the instruction cache with this.  dW at E 64, C 1024,
     // 2048 x 2048: 480 us; 537 us with a branch on adding.)
-    auto box_out = [&](const unsigned char* box, char* dst, size_t stride, int rows, int bytes) {
+    auto box_out = [&](const unsigned char* box, char* dst, size_t stride, int rows, int bytes, bool add = false) {
       const int c = (int)((unsigned)lane % kPer), r0 = (int)((unsigned)lane / kPer);
       if (c * 16 >= bytes) rows = 0;
       dst += r0 * stride + c * 16;
@@ -374,7 +380,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       if constexpr (Add) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i)
-          if (i * kRows + r0 < rows) old[i] = *reinterpret_cast<const float4*>(dst + i * kRows * stride);
+          old[i] = add && i * kRows + r0 < rows ? *reinterpret_cast<const float4*>(dst + i * kRows * stride) : make_float4(0.f, 0.f, 0.f, 0.f);
       }
       __syncwarp();
 #pragma unroll
@@ -427,7 +433,10 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       const int y0 = x.m * kXTile + 128 * rank + 32 * q;              // first row of this warp
       const int rows = min(32, (kDw ? a.M : a.C) - y0);               // rows of the tensor; may be none
       const size_t row0 = (size_t)x.e * (kDw ? a.M : a.C) + y0;
-      for (int sub = 0; sub < x.subs && ok; ++sub) {
+      const int folds = kFold ? max(1, (nkb + kXFoldKb - 1) / kXFoldKb) : 1;
+      for (int fs = 0; fs < folds * x.subs && ok; ++fs) {
+        const int sub = kFold ? fs % x.subs : fs;
+        const bool add = kFold && (a.accumulate || fs >= x.subs);      // to what is there, or to the sums folded so far
         const int buf = W == 2 ? sub : turn & 1;
         constexpr int kTileCols = EPI == kEpiGlu ? 128 : kXTile, kCols = kTileCols / (kEpiWarps / 4);     // columns of this warp
         const int col0 = (x.n + sub) * kTileCols + part * kCols;
@@ -450,11 +459,11 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
 #pragma unroll
               for (int i = 0; i < 16; ++i) u[0][i] = u[1][i] = 0;
             }
-            if (Add && nkb == 0) continue;                             // an expert without rows adds nothing
+            if (Add && nkb == 0 && add) continue;                      // an expert without rows adds nothing
 #pragma unroll
             for (int i = 0; i < 8; ++i)
               to_box(stage, i, make_uint4(u[i >> 2][(i & 3) * 4], u[i >> 2][(i & 3) * 4 + 1], u[i >> 2][(i & 3) * 4 + 2], u[i >> 2][(i & 3) * 4 + 3]));
-            box_out(stage, out + (row0 * a.N + col0 + c0) * 4, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 4);
+            box_out(stage, out + (row0 * a.N + col0 + c0) * 4, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 4, add);
           }
         } else if constexpr (EPI == kEpiPlain) {
 #pragma unroll 1

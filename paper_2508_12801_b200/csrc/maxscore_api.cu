@@ -1098,7 +1098,7 @@ maxscore_status launch_tc(maxscore_ctx* c, const void* A, const void* B, const v
   // 256 x 256: y at C 4096, K 4096 1 248 / 1 234 TFLOP/s, at C 1024, K 2048 1 150 / 1 145, K 1024 1 041 / 1 055, K 512 853 / 904;
   // h 1 286 / 1 257 at K 4096, 1 125 / 1 178 at K 2048.  dW gains at every size (4096 x 2048 over 4096 rows: 1 187 / 1 000,
   // over 300 rows 434 / 388); the backward of the activation loses at every size (1 022 / 1 058 at K 4096, 561 / 705 at 1024).
-  if constexpr (kDw) { if (a.accumulate) go(expert_tc_kernel<EPI, B_MN, 2, true>, 2); else go(expert_tc_kernel<EPI, B_MN, 2>, 2); }
+  if constexpr (kDw) { if (a.accumulate || a.C > kXFoldRows) go(expert_tc_kernel<EPI, B_MN, 2, true>, 2); else go(expert_tc_kernel<EPI, B_MN, 2>, 2); }
   else if constexpr (EPI == kEpiDact) go(expert_tc_kernel<EPI, B_MN, 1>, 1);
   else if (a.K >= 4096 && tiles >= 4 * pairs) go(expert_tc_kernel<EPI, B_MN, 2>, 2);
   else go(expert_tc_kernel<EPI, B_MN, 1>, 1);
@@ -1260,7 +1260,7 @@ maxscore_status launch_norm_bwd(maxscore_ctx* c, const void* dr_out, const void*
   c->launches += 1;
   const bool reduce_gate = n->gate && u.per_gate > 1;
   if (n->w_post || n->w_pre || reduce_gate) {
-    norm_reduce_kernel<<<dim3((p.d_model + 31) / 32, 2 + (reduce_gate ? gate_rows : 0)), 256, 0, st>>>(
+    norm_reduce_kernel<<<dim3((p.d_model + 31) / 32, 2 + (reduce_gate ? gate_rows : 0)), kNormReduceWarps * 32, 0, st>>>(
         pp, pr, pg, dw_post, dw_pre, dgate, grid, u.per_gate, p.d_model);
     MS_LAUNCH_CHECK("norm_reduce_kernel");
     c->launches += 1;

@@ -468,11 +468,12 @@ norm_bwd_kernel(const T* dr_out, const T* dh, const T* y, const T* r_out, T* __r
 }
 
 // Column sums of up to 2 + gates partial matrices: blockIdx.y picks one (0: w_post, 1: w_pre, 2..: gate rows), a CTA 32
-// columns, its 8 warps every eighth row; added in a fixed order.
-__global__ void __launch_bounds__(256)
+// columns, its 32 warps every 32nd row; added in a fixed order.  All latency: the rows of a warp are on their way together.
+constexpr int kNormReduceWarps = 32;
+__global__ void __launch_bounds__(kNormReduceWarps * 32)
 norm_reduce_kernel(const float* __restrict__ part_post, const float* __restrict__ part_pre, const float* __restrict__ part_gate,
                    float* __restrict__ dw_post, float* __restrict__ dw_pre, float* __restrict__ dgate, int rows, int per_gate, int d) {
-  __shared__ float sm[8][33];
+  __shared__ float sm[kNormReduceWarps][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
   const int which = blockIdx.y;
   const float* p = which == 0 ? part_post : which == 1 ? part_pre : part_gate;
@@ -482,15 +483,15 @@ norm_reduce_kernel(const float* __restrict__ part_post, const float* __restrict_
   const int n = which < 2 ? rows : per_gate;
   float s = 0.f;
   if (col < d) {
-#pragma unroll 4
-    for (int r = warp; r < n; r += 8) s += p[(r0 + r) * d + col];
+#pragma unroll 8
+    for (int r = warp; r < n; r += kNormReduceWarps) s += p[(r0 + r) * d + col];
   }
   sm[warp][lane] = s;
   __syncthreads();
   if (warp == 0 && col < d) {
     float t = 0.f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) t += sm[w][lane];
+    for (int w = 0; w < kNormReduceWarps; ++w) t += sm[w][lane];
     o[(which < 2 ? 0 : (size_t)(which - 2) * d) + col] = t;
   }
 }

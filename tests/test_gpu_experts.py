@@ -327,3 +327,71 @@ def test_refusals(ms):
     assert lib.maxscore_expert_glu_bwd(ctx.handle, p(x), p(w), None, p(load), p(y), d_in, d_out, 0, st) == INVALID
     torch.cuda.synchronize()
     assert (y == 3.0).all()                     # nothing ran
+
+
+def test_offsets_beyond_32_bits(ms):
+    """An output of more than 2^31 elements: rows at both ends are right and the padding between is zero."""
+    E, C, d_in, d_out = 2, 66000, 64, 16384
+    dt = torch.bfloat16
+    ctx = make_ctx(ms, E, C, "bf16")
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.empty(E, C, d_in, dtype=dt, device=DEV).normal_(generator=g)
+    w = torch.empty(E, d_in, d_out, dtype=dt, device=DEV).normal_(generator=g)
+    load = torch.tensor([C - 300, C], dtype=torch.int32, device=DEV)
+    y = torch.full((E, C, d_out), float("nan"), dtype=dt, device=DEV)
+    ms.expert_gemm(ctx, x, w, load, y, d_in, d_out, 0)
+    for e, rows in ((0, [0, 1, C - 301]), (1, [0, C // 2, C - 257, C - 1])):
+        X, W = x[e, rows].double(), w[e].double()
+        ref, mag = X @ W, X.abs() @ W.abs()
+        assert ((y[e, rows].double() - ref).abs() <= ROUND["bf16"] * ref.abs() + ACC * mag).all()
+    assert (y[0, C - 300:] == 0).all() and not torch.isnan(y[1, ::997]).any()
+    dw = torch.empty(E, d_in, d_out, device=DEV)
+    ms.expert_gemm_dw(ctx, x, y, load, dw, d_in, d_out, 0)
+    ref = torch.einsum("si,sj->ij", x[1].double(), y[1, :, :64].double())
+    mag = torch.einsum("si,sj->ij", x[1].double().abs(), y[1, :, :64].double().abs())
+    assert ((dw[1, :, :64].double() - ref).abs() <= 1e-5 * mag).all()
+    assert ms.check_internal(ctx) == 0
+
+
+@pytest.mark.parametrize("C", [40, 300])
+def test_two_contexts_on_two_streams(ms, C):
+    """Calls of two contexts that may overlap on the GPU give what they give one after the other."""
+    E, d_in, d_out = 12, 512, 520
+    sets = []
+    for i in range(2):
+        load = loads(E, C, "rand", 20 + i)
+        d = Data("bf16", E, C, load, 30 + i)
+        x, _ = d.buffer(d_in)
+        dy, _ = d.buffer(d_out)
+        w, _ = d.weight(d_in, d_out, i)
+        sets.append((make_ctx(ms, E, C, "bf16"), x, dy, w, load.to(DEV), i))
+
+    def go(s, stream=None):
+        ctx, x, dy, w, load, layout = s
+        y = torch.empty(E, C, d_out, dtype=torch.bfloat16, device=DEV)
+        dw = torch.empty(w.shape, device=DEV)
+        torch.cuda.synchronize()
+        return y, dw, lambda: (ms.expert_gemm(ctx, x, w, load, y, d_in, d_out, layout, stream=stream),
+                               ms.expert_gemm_dw(ctx, x, dy, load, dw, d_in, d_out, layout, stream=stream))
+    alone = []
+    for s in sets:
+        y, dw, call = go(s)
+        call()
+        torch.cuda.synchronize()
+        alone.append((y, dw))
+    both = [go(s, torch.cuda.Stream()) for s in sets]
+    for _ in range(5):
+        for _, _, call in both:
+            call()
+    torch.cuda.synchronize()
+    for (y, dw), (y2, dw2, _) in zip(alone, both):
+        assert torch.equal(y, y2) and torch.equal(dw, dw2)
+
+
+def test_launches_are_counted(ms):
+    ctx = make_ctx(ms, 4, 8, "bf16")
+    bf = dict(dtype=torch.bfloat16, device=DEV)
+    x, w, y = torch.zeros(4, 8, 64, **bf), torch.zeros(4, 64, 32, **bf), torch.zeros(4, 8, 32, **bf)
+    n = ms.launch_count(ctx)
+    ms.expert_gemm(ctx, x, w, torch.ones(4, dtype=torch.int32, device=DEV), y, 64, 32, 0)
+    assert ms.launch_count(ctx) == n + 1

@@ -348,3 +348,55 @@ def test_refusals(ms):
     with pytest.raises(ms.MaxScoreError) as e:
         ms.block_norm(wide, None, t, n(w_pre=w), None, torch.empty_like(t))
     assert e.value.status == UNSUPPORTED
+
+
+def test_offsets_beyond_32_bits(ms):
+    """Rows behind 2^31 elements."""
+    T, d = 140000, 16384
+    c = Case(ms, T, d, "bf16", post=False, seed=12, E=2, k=1)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    res = torch.empty(T, d, dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    h = torch.empty_like(res)
+    ms.block_norm(c.ctx, None, res, c.norm, None, h)
+    for rows in ([0, 1, 2], [T - 3, T - 1], [131071, 131072, 131073]):
+        R = res[rows].double()
+        ref = R / c.rms(R) * c.w_pre.double()
+        c.close(h[rows], ref, ref.abs(), "h")
+    dh, dr, dw = res, torch.empty_like(res), torch.empty(d, device=DEV)
+    ms.block_norm_bwd(c.ctx, None, dh, None, h, c.norm, None, dr, None, None, dw)
+    R, H, w = h[T - 2:].double(), dh[T - 2:].double(), c.w_pre.double()
+    rms = c.rms(R)
+    v, u = H * w / rms, R / rms
+    c.close(dr[T - 2:], v - u * (v * u).mean(1, keepdim=True), v.abs() + u.abs() * (v * u).abs().mean(1, keepdim=True), "dr")
+
+
+def test_gate_rows_wider_than_the_batch_and_streams(ms):
+    c = Case(ms, 20, 264, "bf16", gates=1, seed=13)
+    y, res = c.rand(20, 264), c.rand(20, 264)
+    r1, h1, r2, h2 = (c.empty(20, 264) for _ in range(4))
+    ms.block_norm(c.ctx, y, res, c.norm, r1, h1)
+    wide = ms.make_norm(c.w_post, c.gate, c.w_pre, 10 ** 9, EPS, 0.0, 1.0)        # one gate row for many more tokens than there are
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    ms.block_norm(c.ctx, y, res, wide, r2, h2, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(r1, r2) and torch.equal(h1, h2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_captured_backward_replays(ms, dtype):
+    c = Case(ms, 300, 520, dtype, gates=3, seed=14)
+    y, r_out, dro, dh = (c.rand(300, 520) for _ in range(4))
+    want = run_backward(ms, c, dro, dh, y, r_out)
+    got = {k: torch.empty_like(v) for k, v in want.items()}
+    call = lambda: ms.block_norm_bwd(c.ctx, dro, dh, y, r_out, c.norm, *(got[k] for k in ("dy", "dr", "dw_post", "dgate", "dw_pre")))  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for t in got.values():
+        t.fill_(float("nan"))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(got[k], want[k]) for k in want)
