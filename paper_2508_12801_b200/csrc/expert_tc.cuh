@@ -236,7 +236,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
           if (it >= kStages) good = mbar_wait_bounded(&sm.empty[s], ph ^ 1);
           if (good) {
             // the leading CTA's barrier counts both CTAs' copies.  A remote arrival per slice instead (each CTA announcing its own
-            // half) held the whole pipeline at 0.74 us a slice: 755 TFLOP/s where this form gives 1 400.
+            // half) held the whole pipeline at 0.74 us a slice: 743 TFLOP/s where this form gave 1 372.
             if (masked) mbar_expect_tx(&sm.tail, bytes);
             else if (rank == 0) mbar_expect_tx(&sm.full[s], 2 * bytes);
             auto put = [&](uint32_t dst, const CUtensorMap* tm, int xx, int yy) {
