@@ -6,7 +6,7 @@
 // stages keeps about 190 KB of weights in flight on every SM.  One CTA per SM walks (expert with rows, 128 columns) items.
 //   warp 0: TMA loads;  warp 1: TMEM and MMAs;  warps 2-5: epilogue, a TMEM lane (= output column) per thread.
 // Measured (cold caches): E 64 with 2 rows each, 2048 -> 1024 gated 104 us, 5.1 TB/s; E 128 with 4 rows, 4096 -> 1024 346 us,
-// 6.2 TB/s; one token 15 us on the device (10 by its bytes).  At C 128 it still leads the 256-row tiles (112 against 128 us,
+// 6.2 TB/s; one token 15 us on the device (10 by its bytes).  At C 128 it still leads the 256-row tiles (112 against 135 us,
 // E 64, 2048 -> 2048): those would be half empty.
 // Gated form: 64 gate and 64 up columns share a tile; the up half passes through shared memory to the threads of the gate half.
 #pragma once

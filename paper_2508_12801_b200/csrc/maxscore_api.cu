@@ -9,7 +9,6 @@
 #include <string.h>
 
 #include <algorithm>
-#include <atomic>
 #include <initializer_list>
 #include <new>
 #include <type_traits>
@@ -176,9 +175,9 @@ void norm_fwd_room(F& room) {
 template <typename T, bool Full, typename F>
 void norm_room(F& room) {
   norm_fwd_room<T, 0, Full>(room); norm_fwd_room<T, 1, Full>(room); norm_fwd_room<T, 2, Full>(room);
-  room(norm_bwd_kernel<T, 4, Full, 512, 1>, kNormRing); room(norm_bwd_kernel<T, 2, Full, 512, 1>, kNormRing);
-  room(norm_bwd_kernel<T, 1, Full, 512, 1>, kNormRing); room(norm_bwd_kernel<T, 1, Full, 256, 2>, kNormRing / 2);
-  room(norm_bwd_kernel<T, 1, Full, 128, 4>, kNormRing / 4); room(norm_bwd_kernel<T, 1, Full, 64, 8>, kNormRing / 8);
+  room(norm_bwd_kernel<T, 1, Full, 64, 8>, kNormRing / 8); room(norm_bwd_kernel<T, 1, Full, 128, 4>, kNormRing / 4);
+  room(norm_bwd_kernel<T, 1, Full, 256, 2>, kNormRing / 2); room(norm_bwd_kernel<T, 1, Full, 512, 1>, kNormRing);
+  room(norm_bwd_kernel<T, 2, Full, 512, 1>, kNormRing); room(norm_bwd_kernel<T, 4, Full, 512, 1>, kNormRing);
 }
 
 }  // namespace
@@ -518,8 +517,10 @@ maxscore_status maxscore_create(maxscore_ctx** out, const maxscore_params* param
   MS_CUDA(cudaFuncSetAttribute(gate_bwd_dh_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDhSmemMax));
   MS_CUDA(cudaFuncSetAttribute(gate_bwd_dw_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDwSmemMax));
   MS_CUDA(cudaFuncSetAttribute(dispatch_tma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kTmaWarps * kTmaStages * kTmaChunk));
-  static std::atomic<uint64_t> ready{0};                 // devices on which the kernels below have their shared memory
-  if (dev >= 64 || !(ready.load(std::memory_order_acquire) >> dev & 1)) {
+  // shared memory of the expert and norm kernels: asked for once per device (the last of them tells whether it has been)
+  cudaFuncAttributes last{};
+  MS_CUDA(cudaFuncGetAttributes(&last, norm_bwd_kernel<__nv_bfloat16, 4, false, 512, 1>));
+  if (last.maxDynamicSharedSizeBytes < kNormRing) {
     cudaError_t e_ = cudaSuccess;
     auto room = [&](auto kernel, int bytes) { if (e_ == cudaSuccess) e_ = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
     room(expert_tc_kernel<kEpiPlain, false, 1>, x_smem(kEpiPlain, 1)); room(expert_tc_kernel<kEpiPlain, false, 2>, x_smem(kEpiPlain, 2));
@@ -532,7 +533,6 @@ maxscore_status maxscore_create(maxscore_ctx** out, const maxscore_params* param
     room(expert_few_kernel<kEpiGlu, false>, few_smem(kEpiGlu, kFewRows)); room(expert_few_kernel<kEpiGlu, true>, few_smem(kEpiGlu, kFewRows));
     norm_room<float, true>(room); norm_room<float, false>(room); norm_room<__nv_bfloat16, true>(room); norm_room<__nv_bfloat16, false>(room);
     if (e_ != cudaSuccess) return cuda_fail(e_, "cudaFuncSetAttribute(expert and norm kernels)");
-    if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
   }
   int coop = 0, sweep_occ = 0;
   MS_CUDA(cudaDeviceGetAttribute(&coop, cudaDevAttrCooperativeLaunch, dev));
@@ -1321,7 +1321,8 @@ maxscore_status maxscore_combine_norm(maxscore_ctx* c, const void* src, const in
   if (!src || !expert_idx || !slot_idx || !residual || !r_out || (h == nullptr) != (n->w_pre == nullptr)) return MAXSCORE_ERR_INVALID_ARG;
   for (const void* p : {src, residual, (const void*)y, (const void*)r_out, (const void*)h})
     if (!aligned16(p)) return MAXSCORE_ERR_INVALID_ARG;
-  if (y == r_out || y == residual || (h && (h == y || h == r_out || h == residual))) return MAXSCORE_ERR_INVALID_ARG;
+  if (y == r_out || y == residual || y == src || r_out == src || (h && (h == y || h == r_out || h == residual || h == src)))
+    return MAXSCORE_ERR_INVALID_ARG;
   if (c->p.io_dtype == MAXSCORE_BF16)
     return launch_norm_fwd<__nv_bfloat16, 2>(c, nullptr, src, expert_idx, slot_idx, gate_w, residual, n, y, r_out, h, (cudaStream_t)stream);
   return launch_norm_fwd<float, 2>(c, nullptr, src, expert_idx, slot_idx, gate_w, residual, n, y, r_out, h, (cudaStream_t)stream);

@@ -336,6 +336,13 @@ def test_refusals(ms):
     assert status(ms.block_norm, y, res, n(w_pre=c.w_pre), y, h) == INVALID
     assert status(ms.block_norm, y, res, n(w_pre=c.w_pre), r, r) == INVALID
     assert status(ms.block_norm, y, res, n(), None, None) == INVALID
+    src = torch.zeros(c.E, c.C, 64, dtype=torch.bfloat16, device=DEV)
+    idx, slot = torch.zeros(8, 2, dtype=torch.int32, device=DEV), torch.zeros(8, 2, dtype=torch.int32, device=DEV)
+    if src.numel() == 8 * 64:
+        assert status(ms.combine_norm, src, idx, slot, None, res, n(w_pre=c.w_pre), None, r, src) == INVALID
+    assert status(ms.combine_norm, src, idx, slot, None, res, n(w_pre=c.w_pre), r, r, h) == INVALID
+    assert status(ms.combine_norm, src, idx, slot, None, res, n(w_pre=c.w_pre), res, r, h) == INVALID
+    assert status(ms.combine_norm, src, idx, slot, None, res, n(w_pre=c.w_pre), None, r, None) == INVALID
     f = torch.empty(64, device=DEV)
     assert status(ms.block_norm_bwd, res, h, y, r, n(w_pre=c.w_pre), None, torch.empty_like(r), None, None, f) == INVALID
     assert status(ms.block_norm_bwd, res, h, y, r, n(w_pre=c.w_pre), torch.empty_like(r), y, None, None, f) == INVALID
