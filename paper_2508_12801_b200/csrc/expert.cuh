@@ -80,12 +80,16 @@ __global__ void __launch_bounds__(256, BM == 128 ? 2 : 4)
 expert_fma_kernel(const float* __restrict__ A, const float* __restrict__ B, const float* __restrict__ pre_in,
                   float* __restrict__ out, float* __restrict__ pre_out, ExpertArgs a) {
   constexpr int TM = BM / 16, TN = BN / 16;
-  constexpr int GM = TM < 4 ? TM : 4, GN = EPI == kEpiGlu ? TN / 2 : TN < 4 ? TN : 4;      // rows and columns of a group
+  constexpr int GM = 4, GN = EPI == kEpiGlu ? TN / 2 : TN < 4 ? TN : 4;      // rows and columns of a group
   constexpr int HN = TN / 2;
-  static_assert(GN % 2 == 0, "columns are packed in pairs");
+  static_assert(GM == 4 && (GN == 4 || GN == 2), "rows are read in fours, columns in fours or (gated small tiles) pairs");
   // where a thread's i-th row / j-th column lies in the tile: groups are spread over the tile's halves
   auto row_of = [](int i, int ty) { return i / GM * (BM / (TM / GM)) + ty * GM + i % GM; };
   auto col_of = [](int j, int tx) { return j / GN * (BN / (TN / GN)) + tx * GN + j % GN; };
+  // Operands with the contraction contiguous are transposed on the way into shared memory: there the groups of eight rows are
+  // permuted with the depth, so that neither those scattered stores nor the reads meet in a bank.
+  auto swa = [](int k, int m) { return A_MN ? m : m ^ (((k >> 2) & 3) << 3); };
+  auto swb = [](int k, int n) { return B_MN ? n : n ^ (((k >> 2) & 3) << 3); };
   constexpr int LA = BM * BK / 4 / 256, LB = BN * BK / 4 / 256;   // float4 loads per thread and slice
   static_assert(LA >= 1 && LB >= 1, "tile too small for 256 threads");
   __shared__ __align__(16) float sa[2][BK][BM + 4], sb[2][BK][BN + 4];
@@ -131,13 +135,13 @@ expert_fma_kernel(const float* __restrict__ A, const float* __restrict__ B, cons
         for (int i = 0; i < LA; ++i) {
           const int q = tid + i * 256;
           if (A_MN) *reinterpret_cast<float4*>(&sa[s][q / (BM / 4)][(q % (BM / 4)) * 4]) = ra[i];
-          else { const int k = (q % (BK / 4)) * 4, m = q / (BK / 4); sa[s][k][m] = ra[i].x; sa[s][k + 1][m] = ra[i].y; sa[s][k + 2][m] = ra[i].z; sa[s][k + 3][m] = ra[i].w; }
+          else { const int k = (q % (BK / 4)) * 4, m = q / (BK / 4); const int w = swa(k, m); sa[s][k][w] = ra[i].x; sa[s][k + 1][w] = ra[i].y; sa[s][k + 2][w] = ra[i].z; sa[s][k + 3][w] = ra[i].w; }
         }
 #pragma unroll
         for (int i = 0; i < LB; ++i) {
           const int q = tid + i * 256;
           if (B_MN) *reinterpret_cast<float4*>(&sb[s][q / (BN / 4)][(q % (BN / 4)) * 4]) = rb[i];
-          else { const int k = (q % (BK / 4)) * 4, n = q / (BK / 4); sb[s][k][n] = rb[i].x; sb[s][k + 1][n] = rb[i].y; sb[s][k + 2][n] = rb[i].z; sb[s][k + 3][n] = rb[i].w; }
+          else { const int k = (q % (BK / 4)) * 4, n = q / (BK / 4); const int w = swb(k, n); sb[s][k][w] = rb[i].x; sb[s][k + 1][w] = rb[i].y; sb[s][k + 2][w] = rb[i].z; sb[s][k + 3][w] = rb[i].w; }
         }
       };
       float2 acc[TM][TN / 2];
@@ -155,9 +159,17 @@ expert_fma_kernel(const float* __restrict__ A, const float* __restrict__ B, cons
           float x[TM];
           float2 w[TN / 2];
 #pragma unroll
-          for (int i = 0; i < TM; ++i) x[i] = sa[s & 1][k][row_of(i, ty)];
+          for (int i = 0; i < TM; i += 4) *reinterpret_cast<float4*>(&x[i]) = *reinterpret_cast<const float4*>(&sa[s & 1][k][swa(k, row_of(i, ty))]);
+          if constexpr (GN == 4) {
 #pragma unroll
-          for (int j = 0; j < TN / 2; ++j) w[j] = *reinterpret_cast<const float2*>(&sb[s & 1][k][col_of(2 * j, tx)]);
+            for (int j = 0; j < TN / 2; j += 2) {
+              const float4 v = *reinterpret_cast<const float4*>(&sb[s & 1][k][swb(k, col_of(2 * j, tx))]);
+              w[j] = make_float2(v.x, v.y); w[j + 1] = make_float2(v.z, v.w);
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < TN / 2; ++j) w[j] = *reinterpret_cast<const float2*>(&sb[s & 1][k][swb(k, col_of(2 * j, tx))]);
+          }
 #pragma unroll
           for (int i = 0; i < TM; ++i)
 #pragma unroll
