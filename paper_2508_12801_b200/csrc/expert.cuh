@@ -80,18 +80,18 @@ __global__ void __launch_bounds__(256, BM == 128 ? 2 : 4)
 expert_fma_kernel(const float* __restrict__ A, const float* __restrict__ B, const float* __restrict__ pre_in,
                   float* __restrict__ out, float* __restrict__ pre_out, ExpertArgs a) {
   constexpr int TM = BM / 16, TN = BN / 16;
-  constexpr int GM = 4, GN = EPI == kEpiGlu ? TN / 2 : TN < 4 ? TN : 4;      // rows and columns of a group
+  constexpr int GM = TM < 4 ? TM : 4, GN = EPI == kEpiGlu ? TN / 2 : TN < 4 ? TN : 4;      // rows and columns of a group
   constexpr int HN = TN / 2;
-  static_assert(GM == 4 && (GN == 4 || GN == 2), "rows are read in fours, columns in fours or (gated small tiles) pairs");
+  static_assert(GN == 4 || GN == 2, "columns are read in fours or (gated small tiles) pairs");
   // where a thread's i-th row / j-th column lies in the tile: groups are spread over the tile's halves
   auto row_of = [](int i, int ty) { return i / GM * (BM / (TM / GM)) + ty * GM + i % GM; };
   auto col_of = [](int j, int tx) { return j / GN * (BN / (TN / GN)) + tx * GN + j % GN; };
   // Operands with the contraction contiguous are transposed on the way into shared memory: there the groups of eight rows are
   // permuted with the depth, so that neither those scattered stores nor the reads meet in a bank.
-  auto swa = [](int k, int m) { return A_MN ? m : m ^ (((k >> 2) & 3) << 3); };
+  auto swa = [](int k, int m) { return A_MN || BM < 32 ? m : m ^ (((k >> 2) & 3) << 3); };
   auto swb = [](int k, int n) { return B_MN ? n : n ^ (((k >> 2) & 3) << 3); };
-  constexpr int LA = BM * BK / 4 / 256, LB = BN * BK / 4 / 256;   // float4 loads per thread and slice
-  static_assert(LA >= 1 && LB >= 1, "tile too small for 256 threads");
+  constexpr int QA = BM * BK / 4, LA = (QA + 255) / 256, LB = BN * BK / 4 / 256;   // float4 loads of a slice; per thread
+  static_assert(LB >= 1 && (QA % 256 == 0 || LA == 1), "tile too small for 256 threads");
   __shared__ __align__(16) float sa[2][BK][BM + 4], sb[2][BK][BN + 4];
   __shared__ int srows[kMaxE];
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
@@ -116,7 +116,7 @@ expert_fma_kernel(const float* __restrict__ A, const float* __restrict__ B, cons
         for (int i = 0; i < LA; ++i) {
           const int q = tid + i * 256;
           const int m = m0 + (A_MN ? (q % (BM / 4)) * 4 : q / (BK / 4)), k = k0 + (A_MN ? q / (BM / 4) : (q % (BK / 4)) * 4);
-          ra[i] = (m < M && k < K) ? load4(A_MN ? Ae + (size_t)k * a.M + m : Ae + (size_t)m * a.K + k)
+          ra[i] = (q < QA && m < M && k < K) ? load4(A_MN ? Ae + (size_t)k * a.M + m : Ae + (size_t)m * a.K + k)
                                    : make_float4(0.f, 0.f, 0.f, 0.f);
         }
 #pragma unroll
@@ -134,6 +134,7 @@ expert_fma_kernel(const float* __restrict__ A, const float* __restrict__ B, cons
 #pragma unroll
         for (int i = 0; i < LA; ++i) {
           const int q = tid + i * 256;
+          if (q >= QA) break;
           if (A_MN) *reinterpret_cast<float4*>(&sa[s][q / (BM / 4)][(q % (BM / 4)) * 4]) = ra[i];
           else { const int k = (q % (BK / 4)) * 4, m = q / (BK / 4); const int w = swa(k, m); sa[s][k][w] = ra[i].x; sa[s][k + 1][w] = ra[i].y; sa[s][k + 2][w] = ra[i].z; sa[s][k + 3][w] = ra[i].w; }
         }
@@ -159,7 +160,12 @@ expert_fma_kernel(const float* __restrict__ A, const float* __restrict__ B, cons
           float x[TM];
           float2 w[TN / 2];
 #pragma unroll
-          for (int i = 0; i < TM; i += 4) *reinterpret_cast<float4*>(&x[i]) = *reinterpret_cast<const float4*>(&sa[s & 1][k][swa(k, row_of(i, ty))]);
+          for (int i = 0; i < TM; i += GM) {
+            if constexpr (GM == 4) *reinterpret_cast<float4*>(&x[i]) = *reinterpret_cast<const float4*>(&sa[s & 1][k][swa(k, row_of(i, ty))]);
+            else
+#pragma unroll
+              for (int u = 0; u < GM; ++u) x[i + u] = sa[s & 1][k][swa(k, row_of(i + u, ty))];
+          }
           if constexpr (GN == 4) {
 #pragma unroll
             for (int j = 0; j < TN / 2; j += 2) {

@@ -1039,7 +1039,9 @@ maxscore_status check_expert(const maxscore_ctx* c, std::initializer_list<const 
 template <int EPI, bool A_MN, bool B_MN>
 maxscore_status launch_fma(maxscore_ctx* c, const void* A, const void* B, const void* pre_in, void* out, void* pre_out,
                            const ExpertArgs& a, cudaStream_t st) {
-  // 128 x 128 tiles where they give every SM two of them, else 64 x 64
+  // 128 x 128 tiles where they give every SM two of them, else 64 x 64; tiles of 16 or 32 rows where an expert cannot have more
+  // (a tile multiplies all of its rows, absent ones too: E 8, C 6, 952 -> 1120 56 us instead of 70, E 128, C 12, 168 -> 248 41
+  // instead of 52)
   const long long rows = (long long)c->p.T * c->p.k, cols = (long long)a.N * (EPI == kEpiGlu ? 2 : 1);
   auto tiles = [&](int m, int n) {
     return (EPI == kEpiDw ? (long long)a.E * ((a.M + m - 1) / m) : (rows + m - 1) / m) * ((cols + n - 1) / n);
@@ -1047,7 +1049,9 @@ maxscore_status launch_fma(maxscore_ctx* c, const void* A, const void* B, const 
   auto go = [&](auto kernel, int per_sm) {
     kernel<<<c->sm_count * per_sm, 256, 0, st>>>((const float*)A, (const float*)B, (const float*)pre_in, (float*)out, (float*)pre_out, a);
   };
-  if (tiles(128, 128) >= 2 * c->sm_count) go(expert_fma_kernel<128, 128, 16, EPI, A_MN, B_MN>, 2);
+  if (EPI != kEpiDw && c->C <= 16) go(expert_fma_kernel<16, 64, 32, EPI, A_MN, B_MN>, 4);
+  else if (EPI != kEpiDw && c->C <= 32) go(expert_fma_kernel<32, 64, 32, EPI, A_MN, B_MN>, 4);
+  else if (tiles(128, 128) >= 2 * c->sm_count) go(expert_fma_kernel<128, 128, 16, EPI, A_MN, B_MN>, 2);
   else go(expert_fma_kernel<64, 64, 16, EPI, A_MN, B_MN>, 4);
   MS_LAUNCH_CHECK("expert_fma_kernel");
   c->launches += 1;
