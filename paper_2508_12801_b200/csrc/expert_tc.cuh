@@ -2,8 +2,8 @@
 //
 // A pair (cluster of two, tcgen05 cta_group::2) owns 256 rows x 256 columns: each CTA stages its own 128 rows of A and 128
 // columns of B, the pair's MMA reads both halves, and each CTA's tensor memory ends up with its 128 rows of all 256 columns.
-// That halves the operand traffic per flop of a single CTA's 128 x 256 tile (64 bytes per clock and SM at full rate instead
-// of 96, which the L2 cannot deliver).  Two accumulators alternate, so the epilogue of a tile runs under the MMAs of the next.
+// That takes a third off the operand traffic per flop of a single CTA's 128 x 256 tile (64 bytes per clock and SM at full rate
+// instead of 96; TMA loads that hit the L2 reach 67).  Two accumulators alternate, so the epilogue of a tile runs under the MMAs of the next.
 //   warp 0: TMA loads, five stages of 64-deep slices (three or four of the 256 x 512 tiles);  warp 1: TMEM, and in the leading CTA the MMAs;
 //   the other eight (sixteen): epilogue, a TMEM lane quarter and a part of the columns each, out through staging boxes.
 // Both operand majors are read in place through the descriptors: no weight is ever transposed.
