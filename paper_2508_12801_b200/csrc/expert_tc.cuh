@@ -101,7 +101,7 @@ __host__ __device__ constexpr int x_smem(int epi, int w) {
 }
 
 struct XSmem {
-  uint64_t full[6], empty[6], acc_full[2], acc_empty[2], tail, tail_peer;
+  uint64_t full[6], empty[6], acc_full[2], acc_empty[2], tail, tail_peer[6];
   uint32_t tmem;
   int failed;
   int rows[kMaxE], first[kMaxE + 1];     // rows in use; tiles before each expert
@@ -192,9 +192,9 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
 
   if (threadIdx.x == 0) {
     prefetch_tmap(&tA); prefetch_tmap(rank ? &tB1 : &tB0);
-    for (int s = 0; s < kStages; ++s) { mbar_init(&sm.full[s], 1); mbar_init(&sm.empty[s], 1); }
+    for (int s = 0; s < kStages; ++s) { mbar_init(&sm.full[s], 1); mbar_init(&sm.empty[s], 1); mbar_init(&sm.tail_peer[s], 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(&sm.acc_full[b], 1); mbar_init(&sm.acc_empty[b], 2 * kEpiWarps); }
-    mbar_init(&sm.tail, 1); mbar_init(&sm.tail_peer, 1);
+    mbar_init(&sm.tail, 1);
     sm.failed = 0;
     fence_barrier_init();
   }
@@ -215,8 +215,8 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
     // ---- producer ----------------------------------------------------------------------------------------------
     XWalk<W> walk(sm, a, ntn, pair, pairs);
     XTile x;
-    int it = 0; uint32_t tail_phase = 0; bool ok = true;
-    const uint32_t full0 = map_to_rank(smem_u32(&sm.full[0]), 0), tail_peer0 = map_to_rank(smem_u32(&sm.tail_peer), 0);
+    int it = 0; uint32_t tail_phase = 0, peer_phase = 0; bool ok = true;      // peer_phase: bit s, parity to wait for at tail_peer[s]
+    const uint32_t full0 = map_to_rank(smem_u32(&sm.full[0]), 0), tail_peer0 = map_to_rank(smem_u32(&sm.tail_peer[0]), 0);
     const CUtensorMap* tB = rank ? &tB1 : &tB0;
     while (ok && walk.next(x)) {
       const int K = kDw ? x.rows : a.K;
@@ -273,10 +273,12 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
               *reinterpret_cast<uint4*>(st + (i / per_box) * 8192 + r0 * 128 + (i % per_box) * 16) = make_uint4(0, 0, 0, 0);
             fence_proxy_async();
             __syncwarp();
-            // the other CTA reports to the leading one, which then releases the slice to the MMA
-            if (rank == 1) { if (lane == 0) mbar_arrive_cluster(tail_peer0); }
+            // The other CTA reports to the leading one, which then releases the slice to the MMA.  One barrier a stage: the other CTA
+            // may be several masked slices ahead, and reuses a stage only after the MMA has read it.
+            if (rank == 1) { if (lane == 0) mbar_arrive_cluster(tail_peer0 + 8u * (uint32_t)s); }
             else {
-              good = __all_sync(0xffffffffu, mbar_wait_cluster(&sm.tail_peer, tail_phase ^ 1));
+              good = __all_sync(0xffffffffu, mbar_wait_cluster(&sm.tail_peer[s], (peer_phase >> s) & 1));
+              peer_phase ^= 1u << s;
               if (good && lane == 0) mbar_arrive(&sm.full[s]);
             }
           }
