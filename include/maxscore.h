@@ -267,7 +267,10 @@ maxscore_status maxscore_gate_bwd(maxscore_ctx* ctx, const void* hidden, const v
  * them is never used, whatever it holds, and the rows behind them in an output buffer become zero, as in dispatch.
  *   w_layout 0: weights are [E, d_in, d_out] as w_gate in Eq. 2;  1: [E, d_out, d_in].
  *   Widths (d_in, d_out, d_ff) need not be d_model; a multiple of 8 for bf16 I/O and of 4 for fp32, as d_model.
- * Products are accumulated in fp32 and rounded once.  Outputs must not overlap inputs.  Reproducible bit for bit.
+ * Products are accumulated in fp32 and rounded once.  With bf16 I/O the tensor cores cut their fp32 sums off instead of rounding
+ * them, 3.5e-9 of the sum a term when all have one sign: below the rounding of a bf16 output up to contractions of 2^18 terms.
+ * dw, which is fp32, is formed from parts of 256 rows that are added with rounding (error 4e-7 of the sum, as fp32 sums have it).
+ * Outputs must not overlap inputs.  Reproducible bit for bit.
  * After these calls maxscore_check_internal tells whether a bounded wait gave up, as for maxscore_gate.
  * Errors: NULL (unless said otherwise) or misaligned pointers, an output that is an input's own buffer, non-positive
  * widths, w_layout not 0 or 1 -> MAXSCORE_ERR_INVALID_ARG; widths that are no such multiple -> MAXSCORE_ERR_UNSUPPORTED. */
@@ -278,8 +281,8 @@ maxscore_status maxscore_expert_gemm(maxscore_ctx* ctx, const void* x, const voi
                                      int32_t d_in, int32_t d_out, int32_t w_layout, void* cuda_stream);
 
 /* Gradient with respect to the weights: dw_e = sum over the rows s in use of x[e, s, :]^T dy[e, s, :], always fp32, in the
- * layout of the weights ([E, d_in, d_out] or [E, d_out, d_in]).  accumulate != 0 adds to dw; an expert without rows
- * gets (adds) zero. */
+ * layout of the weights ([E, d_in, d_out] or [E, d_out, d_in]).  accumulate != 0 adds to dw (one more
+ * rounding; with bf16 I/O sums below 2^-126 may become zero); an expert without rows gets (adds) zero. */
 maxscore_status maxscore_expert_gemm_dw(maxscore_ctx* ctx, const void* x, const void* dy, const int32_t* expert_load, float* dw,
                                         int32_t d_in, int32_t d_out, int32_t w_layout, int accumulate, void* cuda_stream);
 

@@ -84,9 +84,12 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {     // arrives
 // ---- the kernel ----------------------------------------------------------------------------------------------------
 constexpr int kXTile = 256, kXBK = 64;
 // The tensor pipe cuts the accumulator off at 24 bits with every MMA instead of rounding it, so a long coherent sum shrinks by
-// about 1.1e-9 of itself a row.  dW folds its accumulator into the fp32 result in memory, with rounding, every 4096 rows: its
-// error stays below 5e-6 of the sum (8e-5 over 66 000 rows without).  Capacities up to that need no fold.
-constexpr int kXFoldRows = 4096, kXFoldKb = kXFoldRows / kXBK;
+// about 3.5e-9 of itself a row (1.4e-5 over 4096 rows of one sign): too much for dW, whose result is fp32.  There an accumulator
+// takes kXPartKb slices at a time, and the epilogue adds these parts up in registers, with rounding, while the next part runs in the
+// other accumulator.  Error of dW on positive rows, whatever their number: 3.8e-7 (8 slices 9.0e-7, plain fp32 sums 2.6e-7 over 512
+// rows, 9.7e-7 over 4096).  What it costs: E 64, C 2560, 2048 x 2048 1 290 us, 8 slices 1 265; undivided sums in 256 x 512 tiles, for
+// which the registers do not reach, 1 165.
+constexpr int kXPartKb = 4, kXPartRows = kXPartKb * kXBK;
 // W: column tiles of a pair at a time (1: 256 x 256, two accumulators in turn; 2: 256 x 512)
 __host__ __device__ constexpr int x_stage_bytes(int w) { return 16384 * (1 + w); }
 // Epilogue warps: two for each of the four TMEM lane quarters; four in the backward of the activation, whose epilogue (two
@@ -173,13 +176,14 @@ __device__ __forceinline__ void expert_prefix(const ExpertArgs& a, int* rows, in
 
 // EPI as in expert.cuh.  B_MN: B is stored with its columns contiguous.  dW: both operands run along the rows.
 // Maps: tA; tB0 / tB1 = B of the leading / the other CTA (gate and up columns in the gated form, else the same).
-// Add: dW is added to, or its rows may be more than one sum takes.  tO0: y or h; tO1 / tO2: g / u kept (gated).  out: y, h, dpre or dW; pre_out: [g | u] kept or null; pre_in: [g | u] (backward).
+// Add: dW is added to what is there.  W = 2 with dW: one sum whatever its length, for capacities up to kXPartRows.
+// tO0: y or h; tO1 / tO2: g / u kept (gated).  out: y, h, dpre or dW; pre_out: [g | u] kept or null; pre_in: [g | u] (backward).
 template <int EPI, bool B_MN, int W, bool Add = false>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(x_threads(EPI))
 expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUtensorMap tB0, const __grid_constant__ CUtensorMap tB1,
                  const __grid_constant__ CUtensorMap tO0, const __grid_constant__ CUtensorMap tO1, const __grid_constant__ CUtensorMap tO2,
                  char* __restrict__ out, char* __restrict__ pre_out, const char* __restrict__ pre_in, ExpertArgs a, unsigned* error_flag) {
-  constexpr bool kDw = EPI == kEpiDw, kA_MN = kDw, kFold = kDw && Add;
+  constexpr bool kDw = EPI == kEpiDw, kA_MN = kDw, kParts = kDw && W == 1;
   constexpr int kEpiWarps = x_epi_warps(EPI);
   constexpr int kStages = x_stages(EPI, W), kStageBytes = x_stage_bytes(W);
   constexpr int kTileN = EPI == kEpiGlu ? 128 : kXTile;               // output columns of a tile
@@ -308,9 +312,9 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       // With two column tiles the first and the last slices are multiplied group-wise, the first column tile ahead of the
       // second: its accumulator is complete (and free again) that much earlier, which is what hides the epilogues.
       const int group = x.subs == 2 ? kStages : 1;
-      int begin = 0, end = kFold ? min(nkb, kXFoldKb) : nkb;           // slices of the present sum
+      int begin = 0, end = kParts ? min(nkb, kXPartKb) : nkb;          // slices of the present sum
       for (int kb = 0; kb < nkb && ok;) {
-        if (kFold && kb == end) { begin = end; end = min(nkb, end + kXFoldKb); }
+        if (kParts && kb == end) { begin = end; end = min(nkb, end + kXPartKb); ++turn; }
         const int n = (kb == begin || end - kb <= group) ? min(group, end - kb) : 1;
         int s = s0;
 #pragma unroll
@@ -371,28 +375,24 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       to_box(box, 2 * i, make_uint4(w[0], w[1], w[2], w[3]));
       to_box(box, 2 * i + 1, make_uint4(w[4], w[5], w[6], w[7]));
     };
-    // box -> memory: rows and bytes beyond the tensor are left out; add: fp32 sums instead of stores.  (Kept small, and the sums
-    // a form of the kernel of their own: the MMA warp's loop shares the instruction cache with this.  dW at E 64, C 1024,
-    // 2048 x 2048: 480 us; 537 us with a branch on adding.)
-    auto box_out = [&](const unsigned char* box, char* dst, size_t stride, int rows, int bytes, bool add = false) {
+    // Box -> memory: rows and bytes beyond the tensor are left out.  Add: reductions at the L2, one per entry and call, so nothing
+    // depends on an order; rounded to nearest, subnormal results may come out as zeros.  (E 64, C 2560, 2048 x 2048: 1 400 us;
+    // loads, sums and stores by the warp 1 610.)
+    auto box_out = [&](const unsigned char* box, char* dst, size_t stride, int rows, int bytes) {
       const int c = (int)((unsigned)lane % kPer), r0 = (int)((unsigned)lane / kPer);
       if (c * 16 >= bytes) rows = 0;
       dst += r0 * stride + c * 16;
-      float4 old[kPer];
-      if constexpr (Add) {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-          old[i] = add && i * kRows + r0 < rows ? *reinterpret_cast<const float4*>(dst + i * kRows * stride) : make_float4(0.f, 0.f, 0.f, 0.f);
-      }
       __syncwarp();
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         const int r = i * kRows + r0;
-        uint4 v = *reinterpret_cast<const uint4*>(box + r * kRow + ((c ^ swz(r)) << 4));
-        if constexpr (Add)
-          v = make_uint4(__float_as_uint(old[i].x + __uint_as_float(v.x)), __float_as_uint(old[i].y + __uint_as_float(v.y)),
-                         __float_as_uint(old[i].z + __uint_as_float(v.z)), __float_as_uint(old[i].w + __uint_as_float(v.w)));
-        if (r < rows) *reinterpret_cast<uint4*>(dst) = v;
+        const uint4 v = *reinterpret_cast<const uint4*>(box + r * kRow + ((c ^ swz(r)) << 4));
+        if (r < rows) {
+          if constexpr (Add)
+            asm volatile("red.relaxed.gpu.global.v4.f32.add [%0], {%1, %2, %3, %4};" ::"l"(dst), "f"(__uint_as_float(v.x)), "f"(__uint_as_float(v.y)),
+                         "f"(__uint_as_float(v.z)), "f"(__uint_as_float(v.w)) : "memory");
+          else *reinterpret_cast<uint4*>(dst) = v;
+        }
         dst += kRows * stride;
       }
       __syncwarp();
@@ -435,12 +435,49 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       const int y0 = x.m * kXTile + 128 * rank + 32 * q;              // first row of this warp
       const int rows = min(32, (kDw ? a.M : a.C) - y0);               // rows of the tensor; may be none
       const size_t row0 = (size_t)x.e * (kDw ? a.M : a.C) + y0;
-      const int folds = kFold ? max(1, (nkb + kXFoldKb - 1) / kXFoldKb) : 1;
-      for (int fs = 0; fs < folds * x.subs && ok; ++fs) {
-        const int sub = kFold ? fs % x.subs : fs;
-        const bool add = kFold && (a.accumulate || fs >= x.subs);      // to what is there, or to the sums folded so far
+      constexpr int kTileCols = EPI == kEpiGlu ? 128 : kXTile, kCols = kTileCols / (kEpiWarps / 4);     // columns of this warp
+      if constexpr (kParts) {
+        const int col0 = x.n * kTileCols + part * kCols;
+        char* dst = out + (row0 * a.N + col0) * 4;
+        float2 sum[kCols / 2];
+#pragma unroll
+        for (int i = 0; i < kCols / 2; ++i) sum[i] = both(0.f);
+        for (int kb = 0; kb < nkb; kb += kXPartKb, ++turn) {
+          const int buf = turn & 1;
+          const uint32_t acc = tmem + lanes + (uint32_t)(buf * 256 + part * kCols);
+          ok = mbar_wait_bounded(&sm.acc_full[buf], (acc_ph >> buf) & 1);
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll
+          for (int c0 = 0; c0 < kCols; c0 += 32) {
+            uint32_t u[2][16];
+            tmem_ld16_issue(acc + c0, u[0]); tmem_ld16_issue(acc + c0 + 16, u[1]);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              uint32_t &lo = u[i >> 3][(i & 7) * 2], &hi = u[i >> 3][(i & 7) * 2 + 1];
+              asm volatile("" : "+r"(lo), "+r"(hi));                   // the sum stays behind the wait
+              sum[c0 / 2 + i] = add2(sum[c0 / 2 + i], make_float2(__uint_as_float(lo), __uint_as_float(hi)));
+            }
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster_relaxed(acc_empty0 + 8u * (uint32_t)buf);
+          acc_ph ^= 1u << buf;
+        }
+        if (!ok || (Add && nkb == 0)) continue;                        // an expert without rows adds nothing
+#pragma unroll
+        for (int c0 = 0; c0 < kCols; c0 += 32) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float2 p0 = sum[c0 / 2 + 2 * i], p1 = sum[c0 / 2 + 2 * i + 1];
+            to_box(stage, i, make_uint4(__float_as_uint(p0.x), __float_as_uint(p0.y), __float_as_uint(p1.x), __float_as_uint(p1.y)));
+          }
+          box_out(stage, dst + c0 * 4, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 4);
+        }
+      } else   // one sum per column tile
+      for (int sub = 0; sub < x.subs && ok; ++sub) {
         const int buf = W == 2 ? sub : turn & 1;
-        constexpr int kTileCols = EPI == kEpiGlu ? 128 : kXTile, kCols = kTileCols / (kEpiWarps / 4);     // columns of this warp
         const int col0 = (x.n + sub) * kTileCols + part * kCols;
         const uint32_t acc = tmem + lanes + (uint32_t)(buf * 256 + part * kCols);
         const bool keep_row = kDw || y0 + lane < x.rows;              // rows behind the load come out as zeros
@@ -461,11 +498,11 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
 #pragma unroll
               for (int i = 0; i < 16; ++i) u[0][i] = u[1][i] = 0;
             }
-            if (Add && nkb == 0 && add) continue;                      // an expert without rows adds nothing
+            if (Add && nkb == 0) continue;                             // an expert without rows adds nothing
 #pragma unroll
             for (int i = 0; i < 8; ++i)
               to_box(stage, i, make_uint4(u[i >> 2][(i & 3) * 4], u[i >> 2][(i & 3) * 4 + 1], u[i >> 2][(i & 3) * 4 + 2], u[i >> 2][(i & 3) * 4 + 3]));
-            box_out(stage, out + (row0 * a.N + col0 + c0) * 4, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 4, add);
+            box_out(stage, out + (row0 * a.N + col0 + c0) * 4, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 4);
           }
         } else if constexpr (EPI == kEpiPlain) {
 #pragma unroll 1
@@ -535,7 +572,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
           acc_ph ^= 1u << buf;
         }
       }
-      if (nkb > 0) ++turn;
+      if (!kParts && nkb > 0) ++turn;
     }
     if (EPI == kEpiDact) asm volatile("cp.async.wait_group 0;" ::: "memory");
     if (lane == 0) bulk_wait_all<0>();

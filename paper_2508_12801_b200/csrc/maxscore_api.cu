@@ -528,6 +528,7 @@ maxscore_status maxscore_create(maxscore_ctx** out, const maxscore_params* param
     room(expert_tc_kernel<kEpiGlu, false, 1>, x_smem(kEpiGlu, 1)); room(expert_tc_kernel<kEpiGlu, false, 2>, x_smem(kEpiGlu, 2));
     room(expert_tc_kernel<kEpiGlu, true, 1>, x_smem(kEpiGlu, 1)); room(expert_tc_kernel<kEpiGlu, true, 2>, x_smem(kEpiGlu, 2));
     room(expert_tc_kernel<kEpiDact, false, 1>, x_smem(kEpiDact, 1)); room(expert_tc_kernel<kEpiDact, true, 1>, x_smem(kEpiDact, 1));
+    room(expert_tc_kernel<kEpiDw, true, 1>, x_smem(kEpiDw, 1)); room(expert_tc_kernel<kEpiDw, true, 1, true>, x_smem(kEpiDw, 1));
     room(expert_tc_kernel<kEpiDw, true, 2>, x_smem(kEpiDw, 2)); room(expert_tc_kernel<kEpiDw, true, 2, true>, x_smem(kEpiDw, 2));
     room(expert_few_kernel<kEpiPlain, false>, few_smem(kEpiPlain, kFewRows)); room(expert_few_kernel<kEpiPlain, true>, few_smem(kEpiPlain, kFewRows));
     room(expert_few_kernel<kEpiGlu, false>, few_smem(kEpiGlu, kFewRows)); room(expert_few_kernel<kEpiGlu, true>, few_smem(kEpiGlu, kFewRows));
@@ -1100,9 +1101,13 @@ maxscore_status launch_tc(maxscore_ctx* c, const void* A, const void* B, const v
   };
   // Two column tiles at a time read a quarter less per flop, but their epilogues hide less well.  Long runs, 256 x 512 against
   // 256 x 256: y at C 4096, K 4096 1 248 / 1 234 TFLOP/s, at C 1024, K 2048 1 150 / 1 145, K 1024 1 041 / 1 055, K 512 853 / 904;
-  // h 1 286 / 1 257 at K 4096, 1 125 / 1 178 at K 2048.  dW gains at every size (4096 x 2048 over 4096 rows: 1 187 / 1 000,
-  // over 300 rows 434 / 388); the backward of the activation loses at every size (1 022 / 1 058 at K 4096, 561 / 705 at 1024).
-  if constexpr (kDw) { if (a.accumulate || a.C > kXFoldRows) go(expert_tc_kernel<EPI, B_MN, 2, true>, 2); else go(expert_tc_kernel<EPI, B_MN, 2>, 2); }
+  // h 1 286 / 1 257 at K 4096, 1 125 / 1 178 at K 2048.  dW takes them where one accumulator holds its sum (E 64, C 128, 2048 x 1024:
+  // 112 us / 136 us); the backward of the activation loses at every size (1 022 / 1 058 at K 4096, 561 / 705 at 1024).
+  if constexpr (kDw) {
+    if (a.C <= kXPartRows) { if (a.accumulate) go(expert_tc_kernel<EPI, B_MN, 2, true>, 2); else go(expert_tc_kernel<EPI, B_MN, 2>, 2); }
+    else if (a.accumulate) go(expert_tc_kernel<EPI, B_MN, 1, true>, 1);
+    else go(expert_tc_kernel<EPI, B_MN, 1>, 1);
+  }
   else if constexpr (EPI == kEpiDact) go(expert_tc_kernel<EPI, B_MN, 1>, 1);
   else if (a.K >= 4096 && tiles >= 4 * pairs) go(expert_tc_kernel<EPI, B_MN, 2>, 2);
   else go(expert_tc_kernel<EPI, B_MN, 1>, 1);
