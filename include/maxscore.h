@@ -272,8 +272,9 @@ maxscore_status maxscore_gate_bwd(maxscore_ctx* ctx, const void* hidden, const v
  * dw, which is fp32, is formed from parts of 256 rows that are added with rounding (error 4e-7 of the sum, as fp32 sums have it).
  * Outputs must not overlap inputs.  Reproducible bit for bit.
  * After these calls maxscore_check_internal tells whether a bounded wait gave up, as for maxscore_gate.
- * Errors: NULL (unless said otherwise) or misaligned pointers, an output that is an input's own buffer, non-positive
- * widths, w_layout not 0 or 1 -> MAXSCORE_ERR_INVALID_ARG; widths that are no such multiple -> MAXSCORE_ERR_UNSUPPORTED. */
+ * Errors: NULL (unless said otherwise) or misaligned pointers, an output that shares memory with another argument,
+ * non-positive widths, w_layout not 0 or 1 -> MAXSCORE_ERR_INVALID_ARG; widths that are no such multiple, or above 2^24 ->
+ * MAXSCORE_ERR_UNSUPPORTED. */
 
 /* y[e, s, :] = x[e, s, :] . W_e.   x [E, C, d_in], y [E, C, d_out].
  * The gradient with respect to x is the same call on dy with d_in and d_out exchanged and the other w_layout. */
@@ -313,8 +314,8 @@ maxscore_status maxscore_expert_glu_bwd(maxscore_ctx* ctx, const void* dy, const
  * when they are stored.  The backward call works from the stored rows.
  *   w_post, w_pre [d_model], gate [ceil(T / rows_per_gate), d_model]: DEVICE memory, io_dtype, 16-byte aligned.
  * After these calls maxscore_check_internal tells whether a bounded wait gave up.
- * Errors: a NULL that is not allowed below, a misaligned pointer, eps or rows_per_gate out of range, an output that is
- * another argument's buffer (but for the two pairs named below) -> MAXSCORE_ERR_INVALID_ARG.
+ * Errors: a NULL that is not allowed below, a misaligned pointer, eps or rows_per_gate out of range, an output that shares
+ * memory with another argument (but for the two pairs named below, which may be one buffer) -> MAXSCORE_ERR_INVALID_ARG.
  * Limits: d_model <= 16384 for bf16 I/O, 8192 for fp32 (MAXSCORE_ERR_UNSUPPORTED). */
 typedef struct {
   const void* w_post;    /* after-norm weight or NULL                                              */

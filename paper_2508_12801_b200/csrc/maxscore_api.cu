@@ -1028,6 +1028,23 @@ extern "C" maxscore_status maxscore_index_build_noalloc(int32_t T, int32_t E, in
 // Experts and norms
 namespace {
 
+// A caller's buffer.  Outputs must share no byte with an input or with one another.
+struct Span { const void* p; size_t bytes; };
+bool apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  auto meet = [](const Span& a, const Span& b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return a.p && b.p && (x < y ? y - x < a.bytes : x - y < b.bytes);
+  };
+  for (const Span* o = outs.begin(); o != outs.end(); ++o) {
+    for (const Span* i = outs.begin(); i != o; ++i) if (meet(*o, *i)) return false;
+    for (const Span& i : ins) if (meet(*o, i)) return false;
+  }
+  return true;
+}
+Span load_span(const maxscore_ctx* c, const int32_t* load) { return {load, sizeof(int32_t) * (size_t)c->p.E}; }
+Span rows_span(const maxscore_ctx* c, const void* p, int64_t width) { return {p, (size_t)c->p.E * c->C * width * elem_bytes(c)}; }
+Span weight_span(const maxscore_ctx* c, const void* p, int64_t d_in, int64_t d_out, size_t elem) { return {p, (size_t)c->p.E * d_in * d_out * elem}; }
+
 maxscore_status check_expert(const maxscore_ctx* c, std::initializer_list<const void*> ptrs, int32_t w0, int32_t w1, int32_t w_layout) {
   if (!c) return MAXSCORE_ERR_INVALID_ARG;
   for (const void* p : ptrs) if (!p || !aligned16(p)) return MAXSCORE_ERR_INVALID_ARG;
@@ -1177,6 +1194,19 @@ maxscore_status check_norm(const maxscore_ctx* c, const maxscore_norm* n, bool y
   return MAXSCORE_OK;
 }
 
+struct NormSpans {
+  size_t token, d;                         // bytes of [T, d_model] in io_dtype, and of [d_model]
+  Span w_post, gate, w_pre;
+  size_t gate_rows;
+};
+NormSpans norm_spans(const maxscore_ctx* c, const maxscore_norm* n) {
+  NormSpans s{};
+  s.d = (size_t)c->p.d_model * elem_bytes(c); s.token = s.d * c->p.T;
+  s.gate_rows = n->gate ? ((size_t)c->p.T + n->rows_per_gate - 1) / n->rows_per_gate : 0;
+  s.w_post = {n->w_post, s.d}; s.gate = {n->gate, s.gate_rows * s.d}; s.w_pre = {n->w_pre, s.d};
+  return s;
+}
+
 NormArgs norm_args(const maxscore_ctx* c, const maxscore_norm* n) {
   NormArgs a{};
   a.T = c->p.T; a.d = c->p.d_model; a.nvec = (int)(c->p.d_model * elem_bytes(c) / 16);
@@ -1285,7 +1315,8 @@ maxscore_status maxscore_expert_gemm(maxscore_ctx* c, const void* x, const void*
                                      int32_t d_in, int32_t d_out, int32_t w_layout, void* stream) {
   maxscore_status s = check_expert(c, {x, w, y}, d_in, d_out, w_layout);
   if (s) return s;
-  if (!expert_load || y == x || y == w) return MAXSCORE_ERR_INVALID_ARG;
+  if (!expert_load || !apart({rows_span(c, y, d_out)}, {rows_span(c, x, d_in), weight_span(c, w, d_in, d_out, elem_bytes(c)), load_span(c, expert_load)}))
+    return MAXSCORE_ERR_INVALID_ARG;
   return launch_expert<kEpiPlain>(c, x, w, nullptr, y, nullptr, expert_args(c, expert_load, 0, d_out, d_in), w_layout == 0,
                                   (cudaStream_t)stream);
 }
@@ -1294,7 +1325,8 @@ maxscore_status maxscore_expert_gemm_dw(maxscore_ctx* c, const void* x, const vo
                                         int32_t d_in, int32_t d_out, int32_t w_layout, int accumulate, void* stream) {
   maxscore_status s = check_expert(c, {x, dy, dw}, d_in, d_out, w_layout);
   if (s) return s;
-  if (!expert_load || (const void*)dw == x || (const void*)dw == dy) return MAXSCORE_ERR_INVALID_ARG;
+  if (!expert_load || !apart({weight_span(c, dw, d_in, d_out, sizeof(float))}, {rows_span(c, x, d_in), rows_span(c, dy, d_out), load_span(c, expert_load)}))
+    return MAXSCORE_ERR_INVALID_ARG;
   // layout 1 is the transposed product: the two operands change places
   const bool t = w_layout == 1;
   return launch_expert<kEpiDw>(c, t ? dy : x, t ? x : dy, nullptr, dw, nullptr,
@@ -1306,7 +1338,10 @@ maxscore_status maxscore_expert_glu(maxscore_ctx* c, const void* x, const void* 
                                     void* h, int32_t d_in, int32_t d_ff, int32_t w_layout, void* stream) {
   maxscore_status s = check_expert(c, {x, w_up, h}, d_in, d_ff, w_layout);
   if (s) return s;
-  if (!expert_load || !aligned16(pre) || h == x || h == w_up || pre == x || pre == w_up || pre == h) return MAXSCORE_ERR_INVALID_ARG;
+  if (!expert_load || !aligned16(pre) ||
+      !apart({rows_span(c, h, d_ff), rows_span(c, pre, 2 * (int64_t)d_ff)},
+             {rows_span(c, x, d_in), weight_span(c, w_up, d_in, 2 * (int64_t)d_ff, elem_bytes(c)), load_span(c, expert_load)}))
+    return MAXSCORE_ERR_INVALID_ARG;
   return launch_expert<kEpiGlu>(c, x, w_up, nullptr, h, pre, expert_args(c, expert_load, 0, d_ff, d_in), w_layout == 0,
                                 (cudaStream_t)stream);
 }
@@ -1316,7 +1351,9 @@ maxscore_status maxscore_expert_glu_bwd(maxscore_ctx* c, const void* dy, const v
                                         void* stream) {
   maxscore_status s = check_expert(c, {dy, w_down, pre, dpre}, d_out, d_ff, w_layout);
   if (s) return s;
-  if (!expert_load || dpre == dy || dpre == w_down || dpre == pre) return MAXSCORE_ERR_INVALID_ARG;
+  if (!expert_load || !apart({rows_span(c, dpre, 2 * (int64_t)d_ff)}, {rows_span(c, dy, d_out), weight_span(c, w_down, d_ff, d_out, elem_bytes(c)),
+                                                                         rows_span(c, pre, 2 * (int64_t)d_ff), load_span(c, expert_load)}))
+    return MAXSCORE_ERR_INVALID_ARG;
   // dh = dy . W_down^T: the weight's d_ff side is the product's N side, contiguous in layout 1 ([E, d_out, d_ff])
   return launch_expert<kEpiDact>(c, dy, w_down, pre, dpre, nullptr, expert_args(c, expert_load, 0, d_ff, d_out), w_layout == 1,
                                  (cudaStream_t)stream);
@@ -1330,7 +1367,11 @@ maxscore_status maxscore_combine_norm(maxscore_ctx* c, const void* src, const in
   if (!src || !expert_idx || !slot_idx || !residual || !r_out || (h == nullptr) != (n->w_pre == nullptr)) return MAXSCORE_ERR_INVALID_ARG;
   for (const void* p : {src, residual, (const void*)y, (const void*)r_out, (const void*)h})
     if (!aligned16(p)) return MAXSCORE_ERR_INVALID_ARG;
-  if (y == r_out || y == residual || y == src || r_out == src || (h && (h == y || h == r_out || h == residual || h == src)))
+  const NormSpans sp = norm_spans(c, n);
+  const size_t pairs = sizeof(int32_t) * (size_t)c->p.T * c->p.k;
+  if (!apart({{y, sp.token}, {r_out, sp.token}, {h, sp.token}},
+             {rows_span(c, src, c->p.d_model), {expert_idx, pairs}, {slot_idx, pairs}, {gate_w, pairs}, {r_out == residual ? nullptr : residual, sp.token},
+              sp.w_post, sp.gate, sp.w_pre}))
     return MAXSCORE_ERR_INVALID_ARG;
   if (c->p.io_dtype == MAXSCORE_BF16)
     return launch_norm_fwd<__nv_bfloat16, 2>(c, nullptr, src, expert_idx, slot_idx, gate_w, residual, n, y, r_out, h, (cudaStream_t)stream);
@@ -1344,7 +1385,9 @@ maxscore_status maxscore_block_norm(maxscore_ctx* c, const void* y, const void* 
   if (!residual || (!r_out && !h) || (h == nullptr) != (n->w_pre == nullptr)) return MAXSCORE_ERR_INVALID_ARG;
   for (const void* p : {y, residual, (const void*)r_out, (const void*)h})
     if (!aligned16(p)) return MAXSCORE_ERR_INVALID_ARG;
-  if ((r_out && r_out == y) || (h && (h == y || h == r_out || h == residual))) return MAXSCORE_ERR_INVALID_ARG;
+  const NormSpans sp = norm_spans(c, n);
+  if (!apart({{r_out, sp.token}, {h, sp.token}}, {{y, sp.token}, {r_out == residual ? nullptr : residual, sp.token}, sp.w_post, sp.gate, sp.w_pre}))
+    return MAXSCORE_ERR_INVALID_ARG;
   const bool bf = c->p.io_dtype == MAXSCORE_BF16;
   cudaStream_t st = (cudaStream_t)stream;
   if (y)
@@ -1365,8 +1408,11 @@ maxscore_status maxscore_block_norm_bwd(maxscore_ctx* c, const void* dr_out, con
     return MAXSCORE_ERR_INVALID_ARG;
   for (const void* p : {dr_out, dh, y, r_out, (const void*)dy, (const void*)dr, (const void*)dw_post, (const void*)dgate, (const void*)dw_pre})
     if (!aligned16(p)) return MAXSCORE_ERR_INVALID_ARG;
-  for (const void* p : {dh, y, r_out}) if (p && (p == dr || p == dy)) return MAXSCORE_ERR_INVALID_ARG;
-  if (dy && (dy == dr || dy == dr_out)) return MAXSCORE_ERR_INVALID_ARG;
+  const NormSpans sp = norm_spans(c, n);
+  const size_t col = sizeof(float) * (size_t)c->p.d_model;
+  if (!apart({{dy, sp.token}, {dr, sp.token}, {dw_post, col}, {dgate, sp.gate_rows * col}, {dw_pre, col}},
+             {{dr == dr_out ? nullptr : dr_out, sp.token}, {dh, sp.token}, {y, sp.token}, {r_out, sp.token}, sp.w_post, sp.gate, sp.w_pre}))
+    return MAXSCORE_ERR_INVALID_ARG;
   if (c->p.io_dtype == MAXSCORE_BF16)
     return launch_norm_bwd<__nv_bfloat16>(c, dr_out, dh, y, r_out, n, dy, dr, dw_post, dgate, dw_pre, (cudaStream_t)stream);
   return launch_norm_bwd<float>(c, dr_out, dh, y, r_out, n, dy, dr, dw_post, dgate, dw_pre, (cudaStream_t)stream);
