@@ -128,8 +128,9 @@ Layout layout_of(const maxscore_params& p) {
   l.dls = off; off = align_up(off + (bf ? sizeof(__nv_bfloat16) * (size_t)p.T * 2 * l.Kpad : 0), 1024);
   l.wk = off; off = align_up(off + (bf ? sizeof(__nv_bfloat16) * (size_t)p.d_model * l.Kpad : 0), 1024);
   l.dwpart = off; off = align_up(off + (bf ? sizeof(float) * (size_t)l.dw_splits * p.d_model * p.E : 0), 1024);
-  l.normpart = off; off = align_up(off + sizeof(float) * 3 * (size_t)(p.T < kNormParts ? p.T : kNormParts) * p.d_model, 1024);
-  l.total = off;
+  // The norm backward's partial sums lie over the others' scratch: behind `aux` nothing is kept from one call to the next.
+  l.normpart = align_up(l.cand, 1024);
+  l.total = std::max(off, align_up(l.normpart + sizeof(float) * 3 * (size_t)std::min(p.T, kNormParts) * p.d_model, 1024));
   return l;
 }
 
