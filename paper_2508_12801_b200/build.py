@@ -8,8 +8,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmaxscore.so")
-SOURCES = ["maxscore_api.cu"]
-HEADERS = ["common.cuh", "flow.cuh", "gate.cuh", "move.cuh", "softtopk.cuh", "reroute.cuh", "alg1.cuh", "expert.cuh", "expert_tc.cuh", "expert_few.cuh", "norm.cuh",
+SOURCES = ["maxscore_api.cu", "blocks_api.cu"]
+HEADERS = ["common.cuh", "context.cuh", "tc.cuh", "flow.cuh", "gate.cuh", "move.cuh", "softtopk.cuh", "reroute.cuh", "alg1.cuh", "expert.cuh",
+           "expert_tc.cuh", "expert_few.cuh", "norm.cuh",
            os.path.join("..", "..", "include", "maxscore.h")]
 
 
@@ -26,7 +27,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
-           "-shared", "-Xcompiler", "-fPIC", "--cudart", "static", "-o", tmp]
+           "-shared", "-Xcompiler", "-fPIC", "--cudart", "static", "--threads", str(len(SOURCES)), "-o", tmp]
     if verbose:
         cmd += ["-Xptxas", "-v"]
     cmd += os.environ.get("MAXSCORE_NVCC_FLAGS", "").split()

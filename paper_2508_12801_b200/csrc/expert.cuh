@@ -10,7 +10,7 @@
 // fp32 I/O: plain FMA tiles (tensor cores would round the inputs to tf32).
 #pragma once
 #include "common.cuh"
-#include "gate.cuh"
+#include "tc.cuh"
 
 namespace msr {
 
