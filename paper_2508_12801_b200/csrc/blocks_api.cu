@@ -88,10 +88,14 @@ maxscore_status launch_fma(maxscore_ctx* c, const void* A, const void* B, const 
   auto go = [&](auto kernel, int per_sm) {
     kernel<<<c->sm_count * per_sm, 256, 0, st>>>((const float*)A, (const float*)B, (const float*)pre_in, (float*)out, (float*)pre_out, a);
   };
-  if (EPI != kEpiDw && c->C <= 16) go(expert_fma_kernel<16, 64, 32, EPI, A_MN, B_MN>, 4);
-  else if (EPI != kEpiDw && c->C <= 32) go(expert_fma_kernel<32, 64, 32, EPI, A_MN, B_MN>, 4);
-  else if (tiles(128, 128) >= 2 * c->sm_count) go(expert_fma_kernel<128, 128, 16, EPI, A_MN, B_MN>, 2);
-  else go(expert_fma_kernel<64, 64, 16, EPI, A_MN, B_MN>, 4);
+  auto by_tiles = [&] {
+    if (tiles(128, 128) >= 2 * c->sm_count) go(expert_fma_kernel<128, 128, 16, EPI, A_MN, B_MN>, 2);
+    else go(expert_fma_kernel<64, 64, 16, EPI, A_MN, B_MN>, 4);
+  };
+  if constexpr (EPI == kEpiDw) by_tiles();                             // its tiles are of the weight, whatever the rows
+  else if (c->C <= 16) go(expert_fma_kernel<16, 64, 32, EPI, A_MN, B_MN>, 4);
+  else if (c->C <= 32) go(expert_fma_kernel<32, 64, 32, EPI, A_MN, B_MN>, 4);
+  else by_tiles();
   MS_LAUNCH_CHECK("expert_fma_kernel");
   c->launches += 1;
   return MAXSCORE_OK;
