@@ -280,13 +280,18 @@ maxscore_status launch_norm_fwd(maxscore_ctx* c, const void* y_in, const void* s
   };
   auto pick = [&](auto full) {
     constexpr bool F = decltype(full)::value;
-    if (f.V == 4) go(norm_fwd_kernel<T, 4, SRC, F, 512, 1>);
-    else if (f.G > 256) go(norm_fwd_kernel<T, 2, SRC, F, 512, 1>);
+    if (f.G > 256) go(norm_fwd_kernel<T, 2, SRC, F, 512, 1>);
     else if (f.G > 128) go(norm_fwd_kernel<T, 2, SRC, F, 256, 2>);
     else if (f.G > 64) go(norm_fwd_kernel<T, 2, SRC, F, 128, 4>);
     else go(norm_fwd_kernel<T, 2, SRC, F, 64, 8>);
   };
-  if (f.full) pick(std::true_type{}); else pick(std::false_type{});
+  // Threads that know that their vectors are exactly the row, against threads that compare, us: behind combine, k 8, T 32768, fp32,
+  // d 4096 939 / 1 000, d 1024 233 / 252, bf16 at T 65536, d 4096 930 / 938, T 8192, d 16384 623 / 665; four vectors a thread with y
+  // given 275 / 291.  With two vectors and y given, or without y, it makes no difference or loses (T 65536, d 1024: 101 / 99).
+  if (f.V == 4 && SRC > 0 && f.full) { if constexpr (SRC > 0) go(norm_fwd_kernel<T, 4, SRC, true, 512, 1>); }
+  else if (f.V == 4) go(norm_fwd_kernel<T, 4, SRC, false, 512, 1>);
+  else if (SRC == 2 && f.full) { if constexpr (SRC == 2) pick(std::true_type{}); }
+  else pick(std::false_type{});
   if (s) return s;
   MS_LAUNCH_CHECK("norm_fwd_kernel");
   c->launches += 1;
@@ -319,16 +324,13 @@ maxscore_status launch_norm_bwd(maxscore_ctx* c, const void* dr_out, const void*
     if (!s) kernel<<<grid, f.G + 32, f.smem, st>>>((const T*)dr_out, (const T*)dh, (const T*)y, (const T*)r_out, (T*)dy, (T*)dr, pp, pr, pg, u, a, f.slots,
                                            error_flag_of(c));
   };
-  auto pick = [&](auto full) {
-    constexpr bool F = decltype(full)::value;
-    if (f.V == 4) go(norm_bwd_kernel<T, 4, F, 512, 1>);
-    else if (f.V == 2) go(norm_bwd_kernel<T, 2, F, 512, 1>);
-    else if (f.G > 256) go(norm_bwd_kernel<T, 1, F, 512, 1>);
-    else if (f.G > 128) go(norm_bwd_kernel<T, 1, F, 256, 2>);
-    else if (f.G > 64) go(norm_bwd_kernel<T, 1, F, 128, 4>);
-    else go(norm_bwd_kernel<T, 1, F, 64, 8>);
-  };
-  if (f.full) pick(std::true_type{}); else pick(std::false_type{});
+  // exactly the row or compared (see above): bf16, d 8192 1 046 / 1 124 us, d 16384 1 322 / 1 332; no difference with one vector a thread
+  if (f.V == 4) { if (f.full) go(norm_bwd_kernel<T, 4, true, 512, 1>); else go(norm_bwd_kernel<T, 4, false, 512, 1>); }
+  else if (f.V == 2) { if (f.full) go(norm_bwd_kernel<T, 2, true, 512, 1>); else go(norm_bwd_kernel<T, 2, false, 512, 1>); }
+  else if (f.G > 256) go(norm_bwd_kernel<T, 1, false, 512, 1>);
+  else if (f.G > 128) go(norm_bwd_kernel<T, 1, false, 256, 2>);
+  else if (f.G > 64) go(norm_bwd_kernel<T, 1, false, 128, 4>);
+  else go(norm_bwd_kernel<T, 1, false, 64, 8>);
   if (s) return s;
   MS_LAUNCH_CHECK("norm_bwd_kernel");
   c->launches += 1;
