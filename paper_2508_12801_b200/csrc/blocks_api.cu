@@ -256,7 +256,8 @@ NormShape norm_shape(int nvec, bool bwd, bool gathers, int rows) {
   s.full = nvec == s.V * s.G;
   // How much to have in flight matters more than how much fits: with 210 KB of rows on their way per SM reads and writes get in
   // each other's way (combine and norms at T 65536, d 4096, k 8: 1 018 us; 105 KB 926 us, 70 KB 977 us, 52 KB 1 049 us; without
-  // combine 387, 379, 355, 378 us).  Two slots at least, or nothing runs ahead.
+  // combine 387, 379, 355, 378 us).  Two slots at least where they fit, or nothing runs ahead (only the backward of four given rows of
+  // more than 26 KB has a single one).
   const size_t slot = (size_t)nvec * 16 * rows, share = kNormRing / s.ctas - sizeof(NormSmem);
   const size_t wanted = (size_t)kNormRing / (gathers ? 2 : 3) / s.ctas / slot;
   s.slots = (int)std::min<size_t>({kNormSlots, share / slot, std::max<size_t>(2, wanted)});

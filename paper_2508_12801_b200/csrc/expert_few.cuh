@@ -3,7 +3,7 @@
 // The weights of the experts in use are read once and that read is the whole cost (2 flops per weight byte and row), so the
 // product is turned round: 128 weight columns are the M side of the MMA and the expert's rows its N side, 16 to 128 of them.
 // Nothing of a weight tile is wasted on absent rows, and a stage is little more than its 16 KB of weights: a ring of 6 to 10
-// stages keeps about 190 KB of weights in flight on every SM.  One CTA per SM walks (expert with rows, 128 columns) items.
+// stages keeps 96 to 160 KB of weights in flight on every SM.  One CTA per SM walks (expert with rows, 128 columns) items.
 //   warp 0: TMA loads;  warp 1: TMEM and MMAs;  warps 2-5: epilogue, a TMEM lane (= output column) per thread.
 // Measured (cold caches): E 64 with 2 rows each, 2048 -> 1024 gated 104 us, 5.1 TB/s; E 128 with 4 rows, 4096 -> 1024 346 us,
 // 6.2 TB/s; one token 15 us on the device (10 by its bytes).  At C 128 it still leads the 256-row tiles (112 against 135 us,

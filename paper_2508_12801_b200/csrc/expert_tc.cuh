@@ -4,11 +4,12 @@
 // columns of B, the pair's MMA reads both halves, and each CTA's tensor memory ends up with its 128 rows of all 256 columns.
 // That takes a third off the operand traffic per flop of a single CTA's 128 x 256 tile (64 bytes per clock and SM at full rate
 // instead of 96; TMA loads that hit the L2 reach 67).  Two accumulators alternate, so the epilogue of a tile runs under the MMAs of the next.
-//   warp 0: TMA loads, five stages of 64-deep slices (three or four of the 256 x 512 tiles);  warp 1: TMEM, and in the leading CTA the MMAs;
+//   warp 0: TMA loads, five or six stages of 64-deep slices (three or four of the 256 x 512 tiles);  warp 1: TMEM, and in the leading CTA the MMAs;
 //   the other eight (sixteen): epilogue, a TMEM lane quarter and a part of the columns each, out through staging boxes.
 // Both operand majors are read in place through the descriptors: no weight is ever transposed.
 //
-// Ragged loads.  Rows: a tile is whole or partial, rows behind the load come out as zeros.  Contraction over rows (dW): the
+// Ragged loads.  Rows: a tile is whole or partial, rows behind the load come out as zeros (the epilogue warps write the whole
+// tiles of zeros before they look at the first accumulator; the MMAs run two tiles ahead meanwhile).  Contraction over rows (dW): the
 // last slice goes up to the load only; the up to 15 rows between the load and the next multiple of the MMA depth are zeroed in
 // shared memory by the producer warp before the pair's MMA may read the slice.
 #pragma once

@@ -11,8 +11,10 @@
 // All of it is bound by HBM.  A producer warp streams the rows of the coming tokens into a ring of row buffers in shared
 // memory (bulk copies on mbarriers), so the loads never wait for the two reductions a token goes through; a group of G
 // threads owns a token at a time, V 16-byte vectors of the row each, weights in registers from token to token.
-// T 65536, d 4096, bf16: with combine of k 8 926 us (6.96 TB/s where a plain copy makes 6.54; some pairs are beyond the
-// capacity), without 351 us (6.1 TB/s), backward 615 us (5.2 TB/s: 16 warps an SM, short of issue slots and registers).
+// T 65536, d 4096, bf16: with combine of k 8 930 us (6.9 TB/s where a plain copy, which writes a byte for each that it reads, makes
+// 6.54: here nine rows are read for three written), without 350 us (6.1 TB/s), backward 620 us (5.2 TB/s).  The backward is short of
+// issue slots and of registers: with the producer's warp a CTA has 17, five of them on one quarter of the SM, which leaves 96
+// registers a thread, and its bf16 forms spill (72 bytes at d 4096, 570 at 8192, 1 900 at 16384, where it makes 3.1 and 1.2 TB/s).
 #pragma once
 #include "common.cuh"
 
@@ -362,7 +364,7 @@ norm_bwd_kernel(const T* dr_out, const T* dh, const T* y, const T* r_out, T* __r
   NormGroup group(sm, norm_ring, rows * row_bytes, slots, G);
   auto mine = [&](int v) { return Full || v < a.nvec; };
   // Per column only two sums run along the tokens: S = sum dr y / rms(y) (within a gate row: dgate = w_post S, and gate S goes
-  // to dw_post when the unit ends) and dw_pre.
+  // to dw_post, apost, when the unit ends) and dw_pre.
   float2 wpre[V][P], gw[V][P], acc[V][P], apre[V][P], apost[V][P];
 #pragma unroll
   for (int j = 0; j < V; ++j) {

@@ -1,11 +1,13 @@
 """One MoE layer of a decoder from the library's calls: routing, dispatch, SwiGLU experts, combine, and the norms,
-gate and residual around them (the MLP block of the paper's models, Sec. 4.1: RMSNorm, SwiGLU experts).
+gate and residual around them.  The paper's models (Sec. 4.1) have SwiGLU experts and a plain RMSNorm before each block: a norm with
+w_pre alone; after-norm and gate are for models that have them.
 
     r' = res_scale * r + gate * norm_post(combine(experts(dispatch(h))))        h' = norm_pre(r')
 
-h is the normalised stream that the norm in front of the block left (norm_in for a first layer); h' is what the next
-block takes.  Every step is one call of the C library on buffers that the layer allocates once; forward and backward
-enqueue work on the current stream and can be captured into a CUDA graph.
+h is the normalised stream that the norm in front of the block left (binding.block_norm without y for a first layer); h' is what
+the next block takes.  Every step is one call of the C library on buffers that the layer allocates once; forward and backward
+enqueue work on the current stream and can be captured into a CUDA graph.  The auxiliary loss is not part of it: a caller who wants
+it takes the calls below with combine_bwd, softtopk_bwd_aux and gate_bwd in route_bwd's place.
 """
 from __future__ import annotations
 
@@ -46,7 +48,8 @@ class MoELayer:
     def backward(self, dr_out, dh_out, h, r_out, w_gate, w_up, w_down, norm, dh, dr, dw_gate, dw_up, dw_down, dw_post=None,
                  dgate=None, dw_pre=None, accumulate=0, stream=None):
         """Gradients of the last forward pass with the assignment held constant: dh and dr [T, d_model] of h and residual,
-        parameter gradients in fp32 (accumulate != 0 adds to dw_up and dw_down; the others are overwritten)."""
+        parameter gradients in fp32 (accumulate != 0 adds to dw_up and dw_down; the others are overwritten).  In bf16 dh is rounded
+        twice: route_bwd stores the gate's part of it and combine adds the experts' part, which saves an fp32 image of [T, d_model]."""
         if not self.training:
             raise ValueError("backward: the layer was made with training=False")
         c, b, d, f, L = self.ctx, self.route, self.ctx.params.d_model, self.d_ff, self.w_layout
