@@ -250,9 +250,9 @@ NormArgs norm_args(const maxscore_ctx* c, const maxscore_norm* n) {
 struct NormShape { int V, G, ctas, slots; size_t smem; bool full; };
 NormShape norm_shape(int nvec, bool bwd, bool gathers, int rows) {
   NormShape s{};
-  s.V = bwd ? (nvec <= 512 ? 1 : nvec <= 1024 ? 2 : 4) : nvec <= 1024 ? 2 : 4;
-  s.G = ((nvec + s.V - 1) / s.V + 31) / 32 * 32;
-  s.ctas = s.V == 1 || !bwd ? (s.G <= 64 ? 8 : s.G <= 128 ? 4 : s.G <= 256 ? 2 : 1) : 1;
+  s.V = bwd ? norm_bwd_vecs(nvec) : nvec <= 1024 ? 2 : 4;
+  s.G = norm_threads(nvec, s.V);
+  s.ctas = bwd ? norm_bwd_ctas(nvec) : norm_ctas(s.G);
   s.full = nvec == s.V * s.G;
   // How much to have in flight matters more than how much fits: with 210 KB of rows on their way per SM reads and writes get in
   // each other's way (combine and norms at T 65536, d 4096, k 8: 1 018 us; 105 KB 926 us, 70 KB 977 us, 52 KB 1 049 us; without
@@ -306,7 +306,7 @@ maxscore_status launch_norm_bwd(maxscore_ctx* c, const void* dr_out, const void*
   const maxscore_params& p = c->p;
   const NormArgs a = norm_args(c, n);
   const NormShape f = norm_shape(a.nvec, true, false, std::max(1, (dh ? 2 : 0) + (y ? 1 : 0) + (dr_out ? 1 : 0)));
-  const int parts = std::min(p.T, kNormParts);                       // rows of each partial matrix in the workspace
+  const int parts = norm_parts(p);                                   // rows of each partial matrix in the workspace
   const int ctas = std::min(parts, c->sm_count * f.ctas);
   const int gate_rows = (p.T + a.rows_per_gate - 1) / a.rows_per_gate;
   NormUnits u{};

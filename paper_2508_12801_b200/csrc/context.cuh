@@ -39,7 +39,16 @@ struct Layout {          // byte offsets inside the workspace
   int Kpad, dw_splits, dw_tokens_per_split;   // tensor-core backward GEMMs (bf16 I/O)
 };
 
-constexpr int kNormParts = 592;          // partial column sums of the norm backward, at most (units, and CTAs)
+// The norm backward on rows of nvec 16-byte vectors: vectors a thread, threads (without the producer's warp), CTAs of an SM, and
+// the rows of partial column sums in the workspace (units, and CTAs, at most; a B200 has 148 SMs).
+inline int norm_bwd_vecs(int nvec) { return nvec <= 512 ? 1 : nvec <= 1024 ? 2 : 4; }
+inline int norm_threads(int nvec, int vecs) { return ((nvec + vecs - 1) / vecs + 31) / 32 * 32; }
+inline int norm_ctas(int threads) { return threads <= 64 ? 8 : threads <= 128 ? 4 : threads <= 256 ? 2 : 1; }
+inline int norm_bwd_ctas(int nvec) { return norm_bwd_vecs(nvec) == 1 ? norm_ctas(norm_threads(nvec, 1)) : 1; }
+inline int norm_parts(const maxscore_params& p) {
+  const int nvec = (int)((size_t)p.d_model * (p.io_dtype == MAXSCORE_BF16 ? 2 : 4) / 16), parts = 148 * (norm_bwd_ctas(nvec) < 4 ? norm_bwd_ctas(nvec) : 4);
+  return p.T < parts ? p.T : parts;
+}
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,

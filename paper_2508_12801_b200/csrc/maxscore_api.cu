@@ -94,7 +94,7 @@ Layout layout_of(const maxscore_params& p) {
   l.dwpart = off; off = align_up(off + (bf ? sizeof(float) * (size_t)l.dw_splits * p.d_model * p.E : 0), 1024);
   // The norm backward's partial sums lie over the others' scratch: behind `aux` nothing is kept from one call to the next.
   l.normpart = align_up(l.cand, 1024);
-  l.total = std::max(off, align_up(l.normpart + sizeof(float) * 3 * (size_t)std::min(p.T, kNormParts) * p.d_model, 1024));
+  l.total = std::max(off, align_up(l.normpart + sizeof(float) * 3 * (size_t)norm_parts(p) * p.d_model, 1024));
   return l;
 }
 

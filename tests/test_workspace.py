@@ -13,6 +13,12 @@ def test_norm_partials_add_nothing_to_a_training_batch(T, d, E, k, io, router):
     assert ms.workspace_bytes(p) <= router
 
 
+def test_norm_partials_of_wide_rows():
+    """Three rows of partial sums for each CTA that a B200 runs, one an SM on wide rows."""
+    p = ms.make_params(600, 8192, 128, 8, 1.0, io_dtype=ms.F32)
+    assert ms.workspace_bytes(p) <= 3040256 + 3 * 148 * 8192 * 4
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("T,d,E,k,io", [(1, 512, 8, 2, "bf16"), (512, 256, 8, 2, "f32"), (4096, 1024, 16, 2, "bf16"), (3000, 2048, 33, 5, "f32")])
 def test_norm_backward_between_the_router_calls(T, d, E, k, io):
