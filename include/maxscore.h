@@ -268,13 +268,14 @@ maxscore_status maxscore_gate_bwd(maxscore_ctx* ctx, const void* hidden, const v
  *   w_layout 0: weights are [E, d_in, d_out] as w_gate in Eq. 2;  1: [E, d_out, d_in].
  *   Widths (d_in, d_out, d_ff) need not be d_model; a multiple of 8 for bf16 I/O and of 4 for fp32, as d_model.
  * Products are accumulated in fp32 and rounded once.  With bf16 I/O the tensor cores cut their fp32 sums off instead of rounding
- * them, 3.5e-9 of the sum a term when all have one sign: below the rounding of a bf16 output up to contractions of 2^18 terms.
+ * them, up to 8e-9 of the sum a term when all have one sign: below the rounding of a bf16 output up to contractions of 2^18 terms
+ * (d_in of maxscore_expert_gemm and _glu, d_out of _glu_bwd), and longer ones are not taken.
  * dw, which is fp32, is formed from parts of 256 rows that are added with rounding (error 4e-7 of the sum, as fp32 sums have it).
  * Outputs must not overlap inputs.  Reproducible bit for bit.
  * After these calls maxscore_check_internal tells whether a bounded wait gave up, as for maxscore_gate.
  * Errors: NULL (unless said otherwise) or misaligned pointers, an output that shares memory with another argument,
- * non-positive widths, w_layout not 0 or 1 -> MAXSCORE_ERR_INVALID_ARG; widths that are no such multiple, or above 2^24 ->
- * MAXSCORE_ERR_UNSUPPORTED. */
+ * non-positive widths, w_layout not 0 or 1 -> MAXSCORE_ERR_INVALID_ARG; widths that are no such multiple, above 2^24, or contracted
+ * and above 2^18 with bf16 I/O -> MAXSCORE_ERR_UNSUPPORTED. */
 
 /* y[e, s, :] = x[e, s, :] . W_e.   x [E, C, d_in], y [E, C, d_out].
  * The gradient with respect to x is the same call on dy with d_in and d_out exchanged and the other w_layout. */

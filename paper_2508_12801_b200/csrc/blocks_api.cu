@@ -66,12 +66,16 @@ Span load_span(const maxscore_ctx* c, const int32_t* load) { return {load, sizeo
 Span rows_span(const maxscore_ctx* c, const void* p, int64_t width) { return {p, (size_t)c->p.E * c->C * width * elem_bytes(c)}; }
 Span weight_span(const maxscore_ctx* c, const void* p, int64_t d_in, int64_t d_out, size_t elem) { return {p, (size_t)c->p.E * d_in * d_out * elem}; }
 
-maxscore_status check_expert(const maxscore_ctx* c, std::initializer_list<const void*> ptrs, int32_t w0, int32_t w1, int32_t w_layout) {
+// contracted: the width that is summed over (0: the rows are)
+maxscore_status check_expert(const maxscore_ctx* c, std::initializer_list<const void*> ptrs, int32_t w0, int32_t w1, int32_t contracted,
+                             int32_t w_layout) {
   if (!c) return MAXSCORE_ERR_INVALID_ARG;
   for (const void* p : ptrs) if (!p || !aligned16(p)) return MAXSCORE_ERR_INVALID_ARG;
   if (w0 <= 0 || w1 <= 0 || (w_layout != 0 && w_layout != 1)) return MAXSCORE_ERR_INVALID_ARG;
   const int m = c->p.io_dtype == MAXSCORE_BF16 ? 8 : 4;
   if (w0 % m || w1 % m || w0 > (1 << 24) || w1 > (1 << 24)) return MAXSCORE_ERR_UNSUPPORTED;
+  // adding 16 products cuts off about two steps of a long sum's last bit: 2^18 terms lose 2e-3 of it, as much as a rounding to bf16
+  if (c->p.io_dtype == MAXSCORE_BF16 && contracted > (1 << 18)) return MAXSCORE_ERR_UNSUPPORTED;
   return MAXSCORE_OK;
 }
 
@@ -351,7 +355,7 @@ extern "C" {
 
 maxscore_status maxscore_expert_gemm(maxscore_ctx* c, const void* x, const void* w, const int32_t* expert_load, void* y,
                                      int32_t d_in, int32_t d_out, int32_t w_layout, void* stream) {
-  maxscore_status s = check_expert(c, {x, w, y}, d_in, d_out, w_layout);
+  maxscore_status s = check_expert(c, {x, w, y}, d_in, d_out, d_in, w_layout);
   if (s) return s;
   if (!expert_load || !apart({rows_span(c, y, d_out)}, {rows_span(c, x, d_in), weight_span(c, w, d_in, d_out, elem_bytes(c)), load_span(c, expert_load)}))
     return MAXSCORE_ERR_INVALID_ARG;
@@ -361,7 +365,7 @@ maxscore_status maxscore_expert_gemm(maxscore_ctx* c, const void* x, const void*
 
 maxscore_status maxscore_expert_gemm_dw(maxscore_ctx* c, const void* x, const void* dy, const int32_t* expert_load, float* dw,
                                         int32_t d_in, int32_t d_out, int32_t w_layout, int accumulate, void* stream) {
-  maxscore_status s = check_expert(c, {x, dy, dw}, d_in, d_out, w_layout);
+  maxscore_status s = check_expert(c, {x, dy, dw}, d_in, d_out, 0, w_layout);
   if (s) return s;
   if (!expert_load || !apart({weight_span(c, dw, d_in, d_out, sizeof(float))}, {rows_span(c, x, d_in), rows_span(c, dy, d_out), load_span(c, expert_load)}))
     return MAXSCORE_ERR_INVALID_ARG;
@@ -374,7 +378,7 @@ maxscore_status maxscore_expert_gemm_dw(maxscore_ctx* c, const void* x, const vo
 
 maxscore_status maxscore_expert_glu(maxscore_ctx* c, const void* x, const void* w_up, const int32_t* expert_load, void* pre,
                                     void* h, int32_t d_in, int32_t d_ff, int32_t w_layout, void* stream) {
-  maxscore_status s = check_expert(c, {x, w_up, h}, d_in, d_ff, w_layout);
+  maxscore_status s = check_expert(c, {x, w_up, h}, d_in, d_ff, d_in, w_layout);
   if (s) return s;
   if (!expert_load || !aligned16(pre) ||
       !apart({rows_span(c, h, d_ff), rows_span(c, pre, 2 * (int64_t)d_ff)},
@@ -387,7 +391,7 @@ maxscore_status maxscore_expert_glu(maxscore_ctx* c, const void* x, const void* 
 maxscore_status maxscore_expert_glu_bwd(maxscore_ctx* c, const void* dy, const void* w_down, const void* pre,
                                         const int32_t* expert_load, void* dpre, int32_t d_out, int32_t d_ff, int32_t w_layout,
                                         void* stream) {
-  maxscore_status s = check_expert(c, {dy, w_down, pre, dpre}, d_out, d_ff, w_layout);
+  maxscore_status s = check_expert(c, {dy, w_down, pre, dpre}, d_out, d_ff, d_out, w_layout);
   if (s) return s;
   if (!expert_load || !apart({rows_span(c, dpre, 2 * (int64_t)d_ff)}, {rows_span(c, dy, d_out), weight_span(c, w_down, d_ff, d_out, elem_bytes(c)),
                                                                          rows_span(c, pre, 2 * (int64_t)d_ff), load_span(c, expert_load)}))

@@ -1,7 +1,9 @@
 """How exact dW is over many rows: fp32 sums, whatever the number of rows.
 
-Tolerance, for rows of one sign (every partial sum is below the result).  Sums over 256 rows are formed 16 rows at a time and each
-step may cut off up to one step of 2^-23 of the partial sum, which is 17/32 of the whole on average: 16 * 17/32 * 2^-23 = 1.0e-6.
+Tolerance, for rows of one sign (every partial sum is below the result).  Sums over 256 rows are formed 16 rows at a time, and each
+time the sum is cut off below its 24th bit, by up to one step of 2^-23 of the partial sum, which is 17/32 of the whole on average:
+16 * 17/32 * 2^-23 = 1.0e-6.  (The products, 16 bits each, are cut two bits further down: 2^-25 of a sum of at most 256 of them is below
+half of their last bit, so they come in whole but for the smallest ones.)
 The n partial sums are then added with rounding, half a step of 2^-24 of the sum so far each: (n + 1) / 2 * 2^-24 at worst, and as a
 root mean square, the roundings being independent, sqrt(n / 3) * 2^-24 / sqrt(3).  fp32 inputs are summed row by row with rounding:
 sqrt(rows / 3) * 2^-24 as a root mean square."""
