@@ -12,7 +12,7 @@
 // memory (bulk copies on mbarriers), so the loads never wait for the two reductions a token goes through; a group of G
 // threads owns a token at a time, V 16-byte vectors of the row each, weights in registers from token to token.
 // T 65536, d 4096, bf16: with combine of k 8 930 us (6.9 TB/s where a plain copy, which writes a byte for each that it reads, makes
-// 6.54: here nine rows are read for three written), without 350 us (6.1 TB/s), backward 620 us (5.2 TB/s).  The backward is short of
+// 6.54: here nine rows are read for three written), without 350 us (6.1 TB/s), backward 640 us (5.0 TB/s).  The backward is short of
 // issue slots and of registers: with the producer's warp a CTA has 17, five of them on one quarter of the SM, which leaves 96
 // registers a thread, and its bf16 forms spill (72 bytes at d 4096, 570 at 8192, 1 900 at 16384, where it makes 3.1 and 1.2 TB/s).
 #pragma once
@@ -45,7 +45,11 @@ struct NormGroup {
     if (ok) ok = mbar_wait_bounded(&sm.full[s], ph);
     return reinterpret_cast<const uint4*>(ring + (uint32_t)s * slot_bytes);
   }
-  __device__ void release() {                                      // the slot has been read by this warp
+  // The slot has been read by this warp.  The copy that fills it next is the async proxy's: the fence keeps it behind these ordinary
+  // reads, which the barrier alone does not (a load that was still on its way then met the rows of a later token).  It costs the
+  // backward 1 to 4 %.
+  __device__ void release() {
+    fence_proxy_async();
     __syncwarp();
     if ((threadIdx.x & 31) == 0) mbar_arrive(&sm.empty[s]);
     if (++s == slots) { s = 0; ph ^= 1; }
