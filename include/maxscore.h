@@ -260,6 +260,41 @@ maxscore_status maxscore_combine_bwd(maxscore_ctx* ctx, const void* dY, const vo
 maxscore_status maxscore_gate_bwd(maxscore_ctx* ctx, const void* hidden, const void* w_gate,
                                   const float* dlogits, float* dw_gate, void* dH, void* cuda_stream);
 
+/* ---- routing by top-k ------------------------------------------------------------------------------- */
+
+/* The usual router of a MoE layer in place of SoftTopk and the flow: every token goes to its k best experts.
+ *   s_e = softmax(logits)_e over the E experts, or sigmoid(logits_e)
+ *   c_e = s_e + bias_e                       the bias balances the experts' loads; it chooses, but does not weigh
+ *   groups: E / n_group consecutive experts each; a group's value is its largest c, or (group_pairs) the sum of its two
+ *           largest; the topk_group best groups stay
+ *   expert_idx: the k largest c among the experts of those groups, ascending
+ *   gate_w_c = scale * s_c / (sum of the chosen s + 1e-20) with renorm, else scale * s_c
+ * Equal values go to the lowest index.  Values are compared as if computed in 64 bits: bias NULL means the order of the
+ * logits, which is that of s.  A logit of -inf or a bias of -inf makes an expert the last choice.  Tokens are not limited by
+ * the experts' capacity here: index build, dispatch and combine leave out what does not fit.  A row with a NaN (or, with
+ * softmax, +inf or nothing but -inf) gets k distinct experts all the same, and NaN where its scores are. */
+typedef struct {
+  int32_t score;         /* 0: softmax, 1: sigmoid                                                 */
+  int32_t n_group;       /* divides E, at most 32; 0 or 1: no groups                               */
+  int32_t topk_group;    /* groups that a token may use, topk_group * E / n_group >= k             */
+  int32_t group_pairs;   /* 0 or 1                                                                 */
+  int32_t renorm;        /* 0 or 1                                                                 */
+  float scale;           /* finite                                                                 */
+} maxscore_topk;
+
+/* logits [T, E] fp32 (as maxscore_gate leaves them) in; bias [E] fp32 or NULL; scores [T, E] fp32 out, s, or NULL;
+ * expert_idx [T, k] int32 out; gate_w [T, k] fp32 out.  maxscore_index_build takes expert_idx next.
+ * Errors: NULL (unless said otherwise), logits or scores not 16-byte aligned, an output that shares memory with another
+ * argument, a member of `how` out of its range -> MAXSCORE_ERR_INVALID_ARG; n_group > 32 -> MAXSCORE_ERR_UNSUPPORTED. */
+maxscore_status maxscore_topk_fwd(maxscore_ctx* ctx, const float* logits, const float* bias, const maxscore_topk* how, float* scores,
+                                  int32_t* expert_idx, float* gate_w, void* cuda_stream);
+
+/* Gradient of the logits with the choice held constant: from dgate_w [T, k] (maxscore_combine_bwd's) through gate_w, plus, unless
+ * dscores_col is NULL, dscores_col [E] as the gradient of every token's s (maxscore_aux_loss's).  The experts of a token
+ * are distinct; pairs with expert_idx outside [0, E) take no part.  dlogits [T, E] fp32 out.  Errors as above. */
+maxscore_status maxscore_topk_bwd(maxscore_ctx* ctx, const float* logits, const int32_t* expert_idx, const float* dgate_w,
+                                  const float* dscores_col, const maxscore_topk* how, float* dlogits, void* cuda_stream);
+
 /* ---- the experts between dispatch and combine ----------------------------------------------------- */
 
 /* Products of the expert buffers with one weight matrix per expert.  A buffer is [E, C, width] in io_dtype; expert e

@@ -17,6 +17,7 @@ from . import build as _build
 C_int32 = C.c_int32
 
 F32, BF16 = 0, 1
+SOFTMAX, SIGMOID = 0, 1
 STAT_NOT_CONVERGED, STAT_NON_FINITE, STAT_INTERNAL = 1, 2, 4
 STATUS_NAMES = {0: "OK", 1: "ERR_INVALID_ARG", 2: "ERR_INFEASIBLE", 3: "ERR_WORKSPACE", 4: "ERR_CUDA",
                 5: "ERR_NOT_CONVERGED", 6: "ERR_UNSUPPORTED"}
@@ -46,6 +47,11 @@ class Norm(C.Structure):
                 ("eps", C.c_float), ("w_offset", C.c_float), ("res_scale", C.c_float)]
 
 
+class TopK(C.Structure):
+    _fields_ = [("score", C.c_int32), ("n_group", C.c_int32), ("topk_group", C.c_int32), ("group_pairs", C.c_int32),
+                ("renorm", C.c_int32), ("scale", C.c_float)]
+
+
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmaxscore.so")
 EXPORTS = ["maxscore_capacity", "maxscore_workspace_bytes", "maxscore_create", "maxscore_destroy",
            "maxscore_last_cuda_error", "maxscore_route_fwd", "maxscore_dispatch", "maxscore_combine",
@@ -55,7 +61,7 @@ EXPORTS = ["maxscore_capacity", "maxscore_workspace_bytes", "maxscore_create", "
            "maxscore_softtopk_bwd_aux", "maxscore_check_internal", "maxscore_launch_count",
            "maxscore_test_raise_internal", "maxscore_assign_iterative", "maxscore_assign_top2_sinkhorn",
            "maxscore_expert_gemm", "maxscore_expert_gemm_dw", "maxscore_expert_glu", "maxscore_expert_glu_bwd",
-           "maxscore_combine_norm", "maxscore_block_norm", "maxscore_block_norm_bwd"]
+           "maxscore_combine_norm", "maxscore_block_norm", "maxscore_block_norm_bwd", "maxscore_topk_fwd", "maxscore_topk_bwd"]
 
 
 def _load():
@@ -85,6 +91,8 @@ _lib.maxscore_expert_glu_bwd.argtypes = [_vp] * 6 + [_i32] * 3 + [_vp]
 _lib.maxscore_combine_norm.argtypes = [_vp] * 11
 _lib.maxscore_block_norm.argtypes = [_vp] * 7
 _lib.maxscore_block_norm_bwd.argtypes = [_vp] * 12
+_lib.maxscore_topk_fwd.argtypes = [_vp] * 8
+_lib.maxscore_topk_bwd.argtypes = [_vp] * 8
 
 
 class MaxScoreError(RuntimeError):
@@ -366,6 +374,27 @@ def block_norm_bwd(ctx, dr_out, dh, y, r_out, norm, dy, dr, dw_post, dgate, dw_p
           _need(ctx, "dr", dr, io, Td), _need(ctx, "dw_post", dw_post, f32, d, optional=True),
           _need(ctx, "dgate", dgate, f32, _gate_rows(ctx, norm) * d, optional=True), _need(ctx, "dw_pre", dw_pre, f32, d, optional=True),
           stream=stream)
+
+
+# ---- routing by top-k -------------------------------------------------------------------------------------
+def make_topk(score=SOFTMAX, n_group=1, topk_group=1, group_pairs=False, renorm=True, scale=1.0) -> TopK:
+    return TopK(score, n_group, topk_group, int(group_pairs), int(renorm), scale)
+
+
+def topk_fwd(ctx, logits, bias, how, scores, expert_idx, gate_w, stream=None):
+    """The k best experts of each token by score + bias within its best groups, and their weights; bias and scores may be None."""
+    T, E, k, f32 = ctx.params.T, ctx.params.E, ctx.params.k, torch.float32
+    _call(ctx, "maxscore_topk_fwd", _lib.maxscore_topk_fwd, _need(ctx, "logits", logits, f32, T * E), _need(ctx, "bias", bias, f32, E, optional=True),
+          C.byref(how), _need(ctx, "scores", scores, f32, T * E, optional=True), _need(ctx, "expert_idx", expert_idx, torch.int32, T * k),
+          _need(ctx, "gate_w", gate_w, f32, T * k), stream=stream)
+
+
+def topk_bwd(ctx, logits, expert_idx, dgate_w, dscores_col, how, dlogits, stream=None):
+    """Gradient of the logits through topk_fwd's weights and, unless dscores_col is None, of the balance loss through its scores."""
+    T, E, k, f32 = ctx.params.T, ctx.params.E, ctx.params.k, torch.float32
+    _call(ctx, "maxscore_topk_bwd", _lib.maxscore_topk_bwd, _need(ctx, "logits", logits, f32, T * E),
+          _need(ctx, "expert_idx", expert_idx, torch.int32, T * k), _need(ctx, "dgate_w", dgate_w, f32, T * k),
+          _need(ctx, "dscores_col", dscores_col, f32, E, optional=True), C.byref(how), _need(ctx, "dlogits", dlogits, f32, T * E), stream=stream)
 
 
 def check_internal(ctx, stream=None) -> int:

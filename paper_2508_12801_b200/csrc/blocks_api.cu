@@ -38,30 +38,6 @@ maxscore_status make_tmap_expert(const maxscore_ctx* c, CUtensorMap* tm, const v
   return MAXSCORE_OK;
 }
 
-// Asks for a kernel's shared memory on a context's first call of it: maxscore_create would have to load a hundred kernels for that,
-// of which a router uses none (first context of a process 48 ms, 7 without).
-template <typename K>
-maxscore_status room_for(maxscore_ctx* c, K kernel, int bytes) {
-  const void* key = reinterpret_cast<const void*>(kernel);
-  for (int i = 0; i < c->n_roomy; ++i) if (c->roomy[i] == key) return MAXSCORE_OK;
-  MS_CUDA(cudaFuncSetAttribute(key, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
-  if (c->n_roomy < kRoomyMax) c->roomy[c->n_roomy++] = key;
-  return MAXSCORE_OK;
-}
-
-// A caller's buffer.  Outputs must share no byte with an input or with one another.
-struct Span { const void* p; size_t bytes; };
-bool apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
-  auto meet = [](const Span& a, const Span& b) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-    return a.p && b.p && (x < y ? y - x < a.bytes : x - y < b.bytes);
-  };
-  for (const Span* o = outs.begin(); o != outs.end(); ++o) {
-    for (const Span* i = outs.begin(); i != o; ++i) if (meet(*o, *i)) return false;
-    for (const Span& i : ins) if (meet(*o, i)) return false;
-  }
-  return true;
-}
 Span load_span(const maxscore_ctx* c, const int32_t* load) { return {load, sizeof(int32_t) * (size_t)c->p.E}; }
 Span rows_span(const maxscore_ctx* c, const void* p, int64_t width) { return {p, (size_t)c->p.E * c->C * width * elem_bytes(c)}; }
 Span weight_span(const maxscore_ctx* c, const void* p, int64_t d_in, int64_t d_out, size_t elem) { return {p, (size_t)c->p.E * d_in * d_out * elem}; }

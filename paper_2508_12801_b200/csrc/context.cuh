@@ -10,6 +10,8 @@
 #include <stdint.h>
 #include <stdio.h>
 
+#include <initializer_list>
+
 namespace msr {
 
 extern thread_local char g_last_error[256] __attribute__((visibility("hidden")));
@@ -78,5 +80,31 @@ namespace msr {
 
 inline unsigned* error_flag_of(const maxscore_ctx* c) { return reinterpret_cast<unsigned*>(c->ws + c->lay.error_flag); }
 inline size_t elem_bytes(const maxscore_ctx* c) { return c->p.io_dtype == MAXSCORE_BF16 ? 2 : 4; }
+
+
+// Asks for a kernel's shared memory on a context's first call of it: maxscore_create would have to load a hundred kernels for that,
+// of which a router uses none (first context of a process 48 ms, 7 without).
+template <typename K>
+inline maxscore_status room_for(maxscore_ctx* c, K kernel, int bytes) {
+  const void* key = reinterpret_cast<const void*>(kernel);
+  for (int i = 0; i < c->n_roomy; ++i) if (c->roomy[i] == key) return MAXSCORE_OK;
+  MS_CUDA(cudaFuncSetAttribute(key, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  if (c->n_roomy < kRoomyMax) c->roomy[c->n_roomy++] = key;
+  return MAXSCORE_OK;
+}
+
+// A caller's buffer.  Outputs must share no byte with an input or with one another.
+struct Span { const void* p; size_t bytes; };
+inline bool apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  auto meet = [](const Span& a, const Span& b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return a.p && b.p && (x < y ? y - x < a.bytes : x - y < b.bytes);
+  };
+  for (const Span* o = outs.begin(); o != outs.end(); ++o) {
+    for (const Span* i = outs.begin(); i != o; ++i) if (meet(*o, *i)) return false;
+    for (const Span& i : ins) if (meet(*o, i)) return false;
+  }
+  return true;
+}
 
 }  // namespace msr
