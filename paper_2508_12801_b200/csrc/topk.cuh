@@ -22,23 +22,32 @@ constexpr float kTopkEps = 1e-20f;     // in the denominator of the weights: a r
 
 struct TopkArgs {
   int T, E, k;
-  int n_group, topk_group, group_size;
+  int n_group, topk_group, group_size, group_lanes;      // group_lanes: lanes of a group where that is a power of two, else 0
   int sigmoid, pairs, renorm;
   float scale;
 };
 
-// Integers in the order of floats; -0 and 0 are equal, NaN comes last but for 0, which stands for "cannot be chosen".
+// Integers in the order of floats: -0 equals 0, NaN equals -inf, and 0 is below them all ("cannot be chosen").
 __device__ __forceinline__ uint32_t order_key(float x) {
-  const uint32_t u = __float_as_uint(x + 0.f);
-  const uint32_t key = u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
-  return x == x ? key : 1u;
+  const uint32_t u = __float_as_uint(fmaxf(x, -INFINITY) + 0.f);
+  return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float order_value(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 
+// e^x for x <= 0: 2^t with t = x log2(e) rounded, then what the rounding left of the exponent as a factor 1 + r ln 2.  Off by 2^-22
+// (the approximation of 2^t) and some 2^-24 (the products) of itself; below 2^-126 it is 0.
+__device__ __forceinline__ float exp_down(float x) {
+  constexpr float log2e = 1.44269504f, rest = 1.92596303e-8f, ln2 = 0.693147181f;      // log2(e) = log2e + rest
+  const float t = fmaxf(x, -1e30f) * log2e;                                             // -inf: t - t would be NaN.  NaN: see the caller
+  const float r = fmaf(x, rest, fmaf(x, log2e, -t));
+  float e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
+  return x > -126.f ? fmaf(e * ln2, r, e) : e;
+}
 // sigmoid(l) and 1 - sigmoid(l), both to a few steps of their last bit
 __device__ __forceinline__ void sigmoid_pair(float l, float& s, float& rest) {
-  const float t = expf(-fabsf(l)), r = 1.f / (1.f + t), tr = t * r;
-  s = l < 0.f ? tr : r;                  // NaN stays NaN: t is
+  const float t = exp_down(-fabsf(l)), r = __fdividef(1.f, 1.f + t), tr = t * r;
+  s = l < 0.f ? tr : l >= 0.f ? r : l;   // NaN stays NaN
   rest = l < 0.f ? r : tr;
 }
 
@@ -83,7 +92,8 @@ __device__ __forceinline__ void topk_scores(const float (&l)[VPT], int E, int la
   float sum = 0.f;
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
-    s[j] = e0 + j < E ? expf(l[j] - m) : 0.f;
+    const float x = l[j] - m;                           // NaN for a NaN, and for rows whose largest is infinite
+    s[j] = e0 + j >= E ? 0.f : x == x ? exp_down(x) : x;
     sum += s[j];
   }
   const float inv = 1.f / warp_sum(sum);
@@ -146,7 +156,8 @@ __device__ __noinline__ uint32_t topk_choose_64(const float* __restrict__ row, c
   return chosen;
 }
 
-template <int VPT, bool Groups>
+// Groups: 0 none; 1 of `group_lanes` lanes each, a power of two; 2 of any size.
+template <int VPT, int Groups>
 __global__ void __launch_bounds__(kTopkWarps * 32)
 topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias, float* __restrict__ scores, int32_t* __restrict__ expert_idx,
                 float* __restrict__ gate_w, TopkArgs a) {
@@ -159,8 +170,10 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
     b[j] = bias && e0 + j < a.E ? __ldg(bias + e0 + j) : 0.f;
-    group[j] = Groups ? min((e0 + j) / a.group_size, kTopkMaxGroups - 1) : 0;
+    group[j] = Groups == 2 ? min((e0 + j) / a.group_size, kTopkMaxGroups - 1) : 0;
   }
+  const int group_stride = Groups == 1 ? a.group_lanes : 1;            // lanes that speak for the groups: g * group_stride
+  const int my_group = lane / group_stride;
   const int64_t step = gridDim.x * kTopkWarps;
   int64_t t = blockIdx.x * kTopkWarps + warp;
   float next[VPT];
@@ -177,74 +190,115 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
     for (int j = 0; j < VPT; ++j) key[j] = e0 + j < a.E ? order_key(bias ? s[j] + b[j] : l[j]) : 0u;
     bool near = false;                                                 // the same in all lanes
     if (Groups) {
-#pragma unroll
-      for (int j = 0; j < VPT; ++j)
-        if (e0 + j < a.E) grouped[e0 + j + group[j]] = bias ? s[j] + b[j] : a.pairs ? s[j] : l[j];
-      __syncwarp();
+      // the two largest of each group
       float m1 = -INFINITY, m2 = -INFINITY;
-      if (lane < a.n_group) {
-        const float* g = grouped + lane * (a.group_size + 1);
-        for (int i = 0; i < a.group_size; ++i) {
-          const float x = g[i] == g[i] ? g[i] : -INFINITY;
-          m2 = fmaxf(m2, fminf(m1, x)); m1 = fmaxf(m1, x);
+      auto take = [&](float x) { m2 = fmaxf(m2, fminf(m1, x)); m1 = fmaxf(m1, x); };
+      if (Groups == 1) {
+#pragma unroll
+        for (int j = 0; j < VPT; ++j)
+          if (e0 + j < a.E) take(fmaxf(bias ? s[j] + b[j] : a.pairs ? s[j] : l[j], -INFINITY));       // NaN comes last
+        for (int o = 1; o < a.group_lanes; o <<= 1) {
+          const float o1 = __shfl_xor_sync(0xffffffffu, m1, o), o2 = __shfl_xor_sync(0xffffffffu, m2, o);
+          m2 = fmaxf(fminf(m1, o1), fmaxf(m2, o2));
+          m1 = fmaxf(m1, o1);
         }
+      } else {
+#pragma unroll
+        for (int j = 0; j < VPT; ++j)
+          if (e0 + j < a.E) grouped[e0 + j + group[j]] = bias ? s[j] + b[j] : a.pairs ? s[j] : l[j];
+        __syncwarp();
+        if (lane < a.n_group)
+          for (int i = 0; i < a.group_size; ++i) take(fmaxf(grouped[lane * (a.group_size + 1) + i], -INFINITY));
+        __syncwarp();
       }
-      __syncwarp();
-      const uint32_t mine = lane < a.n_group ? order_key(a.pairs && a.group_size > 1 ? m1 + m2 : m1) : 0u;
+      const bool speaks = my_group < a.n_group;
+      const uint32_t mine = order_key(a.pairs && a.group_size > 1 ? m1 + m2 : m1);
       int before = 0;
-      for (int g = 0; g < a.n_group; ++g) {
-        const uint32_t other = __shfl_sync(0xffffffffu, mine, g);
-        before += other > mine || (other == mine && g < lane);
-      }
-      const bool in = lane < a.n_group && before < a.topk_group;
-      const uint32_t kept = __ballot_sync(0xffffffffu, in);
+      for (int g = 0; g < a.n_group; ++g) before += __shfl_sync(0xffffffffu, mine, g * group_stride) >= mine + (g >= my_group);
+      const bool in = speaks && before < a.topk_group;
       if (bias || a.pairs) {
         const float low = order_value(__reduce_min_sync(0xffffffffu, in ? mine : 0xffffffffu));
-        const float high = order_value(__reduce_max_sync(0xffffffffu, in ? 0u : mine));
+        const float high = order_value(__reduce_max_sync(0xffffffffu, in || !speaks ? 0u : mine));
         near = !(low - high > 0x1p-18f + 0x1p-21f * fabsf(low));       // two terms, hence twice the bound below
       }
+      if (Groups == 1) {
 #pragma unroll
-      for (int j = 0; j < VPT; ++j) if (!(kept >> group[j] & 1)) key[j] = 0u;
-    }
-    uint32_t chosen = 0, head = key[0];
+        for (int j = 0; j < VPT; ++j) key[j] = in ? key[j] : 0u;
+      } else {
+        const uint32_t kept = __ballot_sync(0xffffffffu, in);
 #pragma unroll
-    for (int j = 1; j < VPT; ++j) head = max(head, key[j]);
-    uint32_t last = 0;
-    for (int c = 0; c < a.k; ++c) {
-      last = __reduce_max_sync(0xffffffffu, head);
-      const int src = __ffs(__ballot_sync(0xffffffffu, head == last)) - 1;
-      if (lane == src) {
-        bool open = true;
-        head = 0;
-#pragma unroll
-        for (int j = 0; j < VPT; ++j) {
-          if (open && key[j] == last) { key[j] = 0; chosen |= 1u << j; open = false; }
-          head = max(head, key[j]);
-        }
+        for (int j = 0; j < VPT; ++j) if (!(kept >> group[j] & 1)) key[j] = 0u;
       }
+    }
+    // The k-th largest value: lanes keep their own sorted, the largest heads leave together until k are gone.
+    uint32_t q[VPT];
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) q[j] = key[j];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+      for (int j = 0; j + 1 < VPT - i; ++j) { const uint32_t hi = max(q[j], q[j + 1]); q[j + 1] = min(q[j], q[j + 1]); q[j] = hi; }
+    uint32_t last = 0;
+#pragma unroll 1
+    for (int gone = 0; gone < a.k;) {
+      last = __reduce_max_sync(0xffffffffu, q[0]);                     // at least 1: topk_group groups hold k experts
+      gone += __popc(__ballot_sync(0xffffffffu, q[0] == last));
+      if (q[0] == last) {
+#pragma unroll
+        for (int j = 0; j + 1 < VPT; ++j) q[j] = q[j + 1];
+        q[VPT - 1] = 0;
+      }
+    }
+    uint32_t chosen = 0, at[VPT];                                      // at[j]: the lanes whose j-th expert is chosen
+    int total = 0;
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      chosen |= (uint32_t)(key[j] >= last) << j;
+      at[j] = __ballot_sync(0xffffffffu, key[j] >= last);
+      total += __popc(at[j]);
     }
     if (bias) {
       // fp32 errors of s: of the exponent |l - m| 2^-24 e^-|l - m|, of exponential, sum and quotient 2^-21 s at most; of the sum with
       // the bias 2^-24 of it.  Twice that between two values, rounded up.
-      const uint32_t after = __reduce_max_sync(0xffffffffu, head);
+      const uint32_t after = __reduce_max_sync(0xffffffffu, q[0]);
       const float low = order_value(last);
-      near = near || (after != 0 && !(low - order_value(after) > 0x1p-19f + 0x1p-22f * fabsf(low)));
+      near = near || total > a.k || (after != 0 && !(low - order_value(after) > 0x1p-19f + 0x1p-22f * fabsf(low)));
     }
-    if (near) chosen = topk_choose_64(logits + t * a.E, bias, a, VPT, scratch[warp]);
-    float sum = 0.f;
+    if (near) {
+      chosen = topk_choose_64(logits + t * a.E, bias, a, VPT, scratch[warp]);
 #pragma unroll
-    for (int j = 0; j < VPT; ++j) if (chosen >> j & 1) sum += s[j];
-    const float f = a.renorm ? a.scale / (warp_sum(sum) + kTopkEps) : a.scale;
+      for (int j = 0; j < VPT; ++j) at[j] = __ballot_sync(0xffffffffu, chosen >> j & 1);
+    } else if (total > a.k) {                                          // equal values at the border: the lowest indices of them stay
+      int spare = a.k, equal = 0;                                      // room for equal ones; those of lower lanes
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) {
+        spare -= __popc(__ballot_sync(0xffffffffu, key[j] > last));
+        equal += __popc(__ballot_sync(0xffffffffu, key[j] == last) & ((1u << lane) - 1u));
+      }
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) {
+        if (key[j] == last && equal++ >= spare) chosen &= ~(1u << j);
+        at[j] = __ballot_sync(0xffffffffu, chosen >> j & 1);
+      }
+    }
+    float f = a.scale;
+    if (a.renorm) {
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) sum += chosen >> j & 1 ? s[j] : 0.f;
+      f = a.scale / (warp_sum(sum) + kTopkEps);
+    }
     // ascending: the chosen of lower lanes, then the lane's own
     int place = 0;
 #pragma unroll
-    for (int j = 0; j < VPT; ++j) place += __popc(__ballot_sync(0xffffffffu, chosen >> j & 1) & ((1u << lane) - 1u));
+    for (int j = 0; j < VPT; ++j) place += __popc(at[j] & ((1u << lane) - 1u));
+    const int64_t row = t * a.k;
 #pragma unroll
     for (int j = 0; j < VPT; ++j)
       if (chosen >> j & 1) {
-        const int64_t at = t * a.k + place++;
-        expert_idx[at] = e0 + j;
-        gate_w[at] = s[j] * f;
+        expert_idx[row + place] = e0 + j;
+        gate_w[row + place] = s[j] * f;
+        ++place;
       }
   }
 }

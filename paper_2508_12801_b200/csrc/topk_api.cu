@@ -61,7 +61,9 @@ maxscore_status maxscore_topk_fwd(maxscore_ctx* c, const float* logits, const fl
     return MAXSCORE_ERR_INVALID_ARG;
   topk_by_width(a.E, [&](auto w) {
     constexpr int V = decltype(w)::value;
-    auto kernel = a.n_group > 1 ? topk_fwd_kernel<V, true> : topk_fwd_kernel<V, false>;
+    const int lanes = a.group_size / V;
+    a.group_lanes = a.group_size % V == 0 && (lanes & (lanes - 1)) == 0 ? lanes : 0;
+    auto kernel = a.n_group == 1 ? topk_fwd_kernel<V, 0> : a.group_lanes ? topk_fwd_kernel<V, 1> : topk_fwd_kernel<V, 2>;
     kernel<<<topk_grid(c), kTopkWarps * 32, 0, (cudaStream_t)stream>>>(logits, bias, scores, expert_idx, gate_w, a);
   });
   MS_LAUNCH_CHECK("topk_fwd_kernel");
