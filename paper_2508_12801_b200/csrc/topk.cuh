@@ -27,37 +27,38 @@ struct TopkArgs {
   float scale;
 };
 
-// Integers in the order of floats: -0 equals 0, NaN equals -inf, and 0 is below them all ("cannot be chosen").
+// Integers in the order of floats, -0 equal to 0, none of them 0, which stands for "cannot be chosen".  (NaN: first or last by its sign.)
 __device__ __forceinline__ uint32_t order_key(float x) {
-  const uint32_t u = __float_as_uint(fmaxf(x, -INFINITY) + 0.f);
+  const uint32_t u = __float_as_uint(x + 0.f);
   return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float order_value(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 
 // e^x for x <= 0: 2^t with t = x log2(e) rounded, then what the rounding left of the exponent as a factor 1 + r ln 2.  Off by 2^-22
-// (the approximation of 2^t) and some 2^-24 (the products) of itself; below 2^-126 it is 0.
+// (the approximation of 2^t) and some 2^-24 (the products) of itself; below 2^-126 it is 0.  NaN stays NaN.
 __device__ __forceinline__ float exp_down(float x) {
   constexpr float log2e = 1.44269504f, rest = 1.92596303e-8f, ln2 = 0.693147181f;      // log2(e) = log2e + rest
-  const float t = fmaxf(x, -1e30f) * log2e;                                             // -inf: t - t would be NaN.  NaN: see the caller
-  const float r = fmaf(x, rest, fmaf(x, log2e, -t));
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(x) : "f"(x), "f"(-126.f));                       // e^-126 is 0 in fp32
+  const float t = x * log2e, r = fmaf(x, rest, fmaf(x, log2e, -t));
   float e;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
-  return x > -126.f ? fmaf(e * ln2, r, e) : e;
+  return fmaf(e * ln2, r, e);
 }
 // sigmoid(l) and 1 - sigmoid(l), both to a few steps of their last bit
 __device__ __forceinline__ void sigmoid_pair(float l, float& s, float& rest) {
   const float t = exp_down(-fabsf(l)), r = __fdividef(1.f, 1.f + t), tr = t * r;
-  s = l < 0.f ? tr : l >= 0.f ? r : l;   // NaN stays NaN
+  s = l < 0.f ? tr : r;
   rest = l < 0.f ? r : tr;
 }
 
-template <int VPT>
+// Full: rows of exactly 32 VPT experts, moved as vectors.
+template <int VPT, bool Full>
 __device__ __forceinline__ void topk_load_row(const float* __restrict__ row, int E, int lane, float (&l)[VPT]) {
   const int e0 = lane * VPT;
-  if (VPT == 4 && E == 128) {
+  if (Full && VPT == 4) {
     const float4 v = __ldg(reinterpret_cast<const float4*>(row) + lane);
     l[0] = v.x; l[1 % VPT] = v.y; l[2 % VPT] = v.z; l[3 % VPT] = v.w;
-  } else if (VPT == 2 && E == 64) {
+  } else if (Full && VPT == 2) {
     const float2 v = __ldg(reinterpret_cast<const float2*>(row) + lane);
     l[0] = v.x; l[1 % VPT] = v.y;
   } else {
@@ -65,11 +66,11 @@ __device__ __forceinline__ void topk_load_row(const float* __restrict__ row, int
     for (int j = 0; j < VPT; ++j) l[j] = e0 + j < E ? __ldg(row + e0 + j) : 0.f;
   }
 }
-template <int VPT>
+template <int VPT, bool Full>
 __device__ __forceinline__ void topk_store_row(float* __restrict__ row, int E, int lane, const float (&v)[VPT]) {
   const int e0 = lane * VPT;
-  if (VPT == 4 && E == 128) reinterpret_cast<float4*>(row)[lane] = make_float4(v[0], v[1 % VPT], v[2 % VPT], v[3 % VPT]);
-  else if (VPT == 2 && E == 64) reinterpret_cast<float2*>(row)[lane] = make_float2(v[0], v[1 % VPT]);
+  if (Full && VPT == 4) reinterpret_cast<float4*>(row)[lane] = make_float4(v[0], v[1 % VPT], v[2 % VPT], v[3 % VPT]);
+  else if (Full && VPT == 2) reinterpret_cast<float2*>(row)[lane] = make_float2(v[0], v[1 % VPT]);
   else {
 #pragma unroll
     for (int j = 0; j < VPT; ++j) if (e0 + j < E) row[e0 + j] = v[j];
@@ -77,7 +78,7 @@ __device__ __forceinline__ void topk_store_row(float* __restrict__ row, int E, i
 }
 
 // s of the row; for the sigmoid 1 - s too
-template <int VPT>
+template <int VPT, bool Full>
 __device__ __forceinline__ void topk_scores(const float (&l)[VPT], int E, int lane, bool sigmoid, float (&s)[VPT], float (&rest)[VPT]) {
   const int e0 = lane * VPT;
   if (sigmoid) {
@@ -87,13 +88,12 @@ __device__ __forceinline__ void topk_scores(const float (&l)[VPT], int E, int la
   }
   uint32_t top = 0;
 #pragma unroll
-  for (int j = 0; j < VPT; ++j) if (e0 + j < E) top = max(top, order_key(l[j]));
+  for (int j = 0; j < VPT; ++j) if (Full || e0 + j < E) top = max(top, order_key(l[j]));
   const float m = order_value(__reduce_max_sync(0xffffffffu, top));
   float sum = 0.f;
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
-    const float x = l[j] - m;                           // NaN for a NaN, and for rows whose largest is infinite
-    s[j] = e0 + j >= E ? 0.f : x == x ? exp_down(x) : x;
+    s[j] = Full || e0 + j < E ? exp_down(l[j] - m) : 0.f;              // NaN where l is, and in rows whose largest is infinite
     sum += s[j];
   }
   const float inv = 1.f / warp_sum(sum);
@@ -156,8 +156,41 @@ __device__ __noinline__ uint32_t topk_choose_64(const float* __restrict__ row, c
   return chosen;
 }
 
+// Choice among equal values at the border: the lowest indices of them stay.  Returns this lane's chosen experts as bits.
+template <int VPT>
+__device__ __noinline__ uint32_t topk_choose_equal(const uint32_t* key, int k) {
+  const int lane = threadIdx.x & 31;
+  uint32_t left[VPT], last = 0;
+#pragma unroll
+  for (int j = 0; j < VPT; ++j) left[j] = key[j];
+  for (int gone = 0; gone < k;) {                                      // all experts of one value leave together
+    uint32_t head = 0;
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) head = max(head, left[j]);
+    last = __reduce_max_sync(0xffffffffu, head);                       // above 0: k experts can be chosen
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      gone += __popc(__ballot_sync(0xffffffffu, left[j] == last));
+      if (left[j] == last) left[j] = 0;
+    }
+  }
+  int spare = k, equal = 0;                                            // room for the equal ones; those of lower lanes
+#pragma unroll
+  for (int j = 0; j < VPT; ++j) {
+    spare -= __popc(__ballot_sync(0xffffffffu, key[j] > last));
+    equal += __popc(__ballot_sync(0xffffffffu, key[j] == last) & ((1u << lane) - 1u));
+  }
+  uint32_t chosen = 0;
+#pragma unroll
+  for (int j = 0; j < VPT; ++j) {
+    if (key[j] > last) chosen |= 1u << j;
+    else if (key[j] == last && equal++ < spare) chosen |= 1u << j;
+  }
+  return chosen;
+}
+
 // Groups: 0 none; 1 of `group_lanes` lanes each, a power of two; 2 of any size.
-template <int VPT, int Groups>
+template <int VPT, int Groups, bool Full>
 __global__ void __launch_bounds__(kTopkWarps * 32)
 topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias, float* __restrict__ scores, int32_t* __restrict__ expert_idx,
                 float* __restrict__ gate_w, TopkArgs a) {
@@ -174,29 +207,37 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
   }
   const int group_stride = Groups == 1 ? a.group_lanes : 1;            // lanes that speak for the groups: g * group_stride
   const int my_group = lane / group_stride;
+  const bool speaks = my_group < a.n_group;
   const int64_t step = gridDim.x * kTopkWarps;
   int64_t t = blockIdx.x * kTopkWarps + warp;
   float next[VPT];
-  if (t < a.T) topk_load_row<VPT>(logits + t * a.E, a.E, lane, next);
+  if (t < a.T) topk_load_row<VPT, Full>(logits + t * a.E, a.E, lane, next);
   for (; t < a.T; t += step) {
     float l[VPT], s[VPT], rest[VPT];
 #pragma unroll
     for (int j = 0; j < VPT; ++j) l[j] = next[j];
-    if (t + step < a.T) topk_load_row<VPT>(logits + (t + step) * a.E, a.E, lane, next);
-    topk_scores<VPT>(l, a.E, lane, a.sigmoid, s, rest);
-    if (scores) topk_store_row<VPT>(scores + t * a.E, a.E, lane, s);
+    if (t + step < a.T) topk_load_row<VPT, Full>(logits + (t + step) * a.E, a.E, lane, next);
+    topk_scores<VPT, Full>(l, a.E, lane, a.sigmoid, s, rest);
+    if (scores) topk_store_row<VPT, Full>(scores + t * a.E, a.E, lane, s);
+    float c[VPT];
     uint32_t key[VPT];
 #pragma unroll
-    for (int j = 0; j < VPT; ++j) key[j] = e0 + j < a.E ? order_key(bias ? s[j] + b[j] : l[j]) : 0u;
+    for (int j = 0; j < VPT; ++j) {
+      c[j] = bias ? s[j] + b[j] : l[j];
+      key[j] = Full || e0 + j < a.E ? order_key(c[j]) : 0u;
+    }
     bool near = false;                                                 // the same in all lanes
     if (Groups) {
-      // the two largest of each group
+      // the two largest of each group (NaN counts as nothing)
+      if (!bias && a.pairs) {
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) c[j] = s[j];
+      }
       float m1 = -INFINITY, m2 = -INFINITY;
       auto take = [&](float x) { m2 = fmaxf(m2, fminf(m1, x)); m1 = fmaxf(m1, x); };
       if (Groups == 1) {
 #pragma unroll
-        for (int j = 0; j < VPT; ++j)
-          if (e0 + j < a.E) take(fmaxf(bias ? s[j] + b[j] : a.pairs ? s[j] : l[j], -INFINITY));       // NaN comes last
+        for (int j = 0; j < VPT; ++j) if (Full || e0 + j < a.E) take(c[j]);
         for (int o = 1; o < a.group_lanes; o <<= 1) {
           const float o1 = __shfl_xor_sync(0xffffffffu, m1, o), o2 = __shfl_xor_sync(0xffffffffu, m2, o);
           m2 = fmaxf(fminf(m1, o1), fmaxf(m2, o2));
@@ -204,21 +245,29 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
         }
       } else {
 #pragma unroll
-        for (int j = 0; j < VPT; ++j)
-          if (e0 + j < a.E) grouped[e0 + j + group[j]] = bias ? s[j] + b[j] : a.pairs ? s[j] : l[j];
+        for (int j = 0; j < VPT; ++j) if (Full || e0 + j < a.E) grouped[e0 + j + group[j]] = c[j];
         __syncwarp();
         if (lane < a.n_group)
-          for (int i = 0; i < a.group_size; ++i) take(fmaxf(grouped[lane * (a.group_size + 1) + i], -INFINITY));
+          for (int i = 0; i < a.group_size; ++i) take(grouped[lane * (a.group_size + 1) + i]);
         __syncwarp();
       }
-      const bool speaks = my_group < a.n_group;
-      const uint32_t mine = order_key(a.pairs && a.group_size > 1 ? m1 + m2 : m1);
-      int before = 0;
-      for (int g = 0; g < a.n_group; ++g) before += __shfl_sync(0xffffffffu, mine, g * group_stride) >= mine + (g >= my_group);
-      const bool in = speaks && before < a.topk_group;
+      const uint32_t mine = speaks ? order_key(a.pairs && a.group_size > 1 ? m1 + m2 : m1) : 0u;
+      // the best leave one by one; where equal ones left together, every group counts those before it instead
+      uint32_t head = mine, worst = 0;
+#pragma unroll 1
+      for (int g = 0; g < a.topk_group; ++g) {
+        worst = __reduce_max_sync(0xffffffffu, head);
+        head = head == worst ? 0u : head;
+      }
+      bool in = speaks && mine >= worst;
+      if (__popc(__ballot_sync(0xffffffffu, in)) != a.topk_group * group_stride) {
+        int before = 0;
+        for (int g = 0; g < a.n_group; ++g) before += __shfl_sync(0xffffffffu, mine, g * group_stride) >= mine + (g >= my_group);
+        in = speaks && before < a.topk_group;
+      }
       if (bias || a.pairs) {
         const float low = order_value(__reduce_min_sync(0xffffffffu, in ? mine : 0xffffffffu));
-        const float high = order_value(__reduce_max_sync(0xffffffffu, in || !speaks ? 0u : mine));
+        const float high = order_value(__reduce_max_sync(0xffffffffu, in ? 0u : mine));
         near = !(low - high > 0x1p-18f + 0x1p-21f * fabsf(low));       // two terms, hence twice the bound below
       }
       if (Groups == 1) {
@@ -230,19 +279,18 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
         for (int j = 0; j < VPT; ++j) if (!(kept >> group[j] & 1)) key[j] = 0u;
       }
     }
-    // The k-th largest value: lanes keep their own sorted, the largest heads leave together until k are gone.
+    // The k-th largest value: lanes keep their own sorted, the largest heads leave.
     uint32_t q[VPT];
 #pragma unroll
     for (int j = 0; j < VPT; ++j) q[j] = key[j];
-#pragma unroll
-    for (int i = 0; i < VPT; ++i)
-#pragma unroll
-      for (int j = 0; j + 1 < VPT - i; ++j) { const uint32_t hi = max(q[j], q[j + 1]); q[j + 1] = min(q[j], q[j + 1]); q[j] = hi; }
+    auto order = [&](int i, int j) { const uint32_t hi = max(q[i], q[j]); q[j] = min(q[i], q[j]); q[i] = hi; };
+    if constexpr (VPT == 4) { order(0, 1); order(2, 3); order(0, 2); order(1, 3); order(1, 2); }
+    else if constexpr (VPT == 3) { order(0, 1); order(1, 2); order(0, 1); }
+    else if constexpr (VPT == 2) order(0, 1);
     uint32_t last = 0;
 #pragma unroll 1
-    for (int gone = 0; gone < a.k;) {
-      last = __reduce_max_sync(0xffffffffu, q[0]);                     // at least 1: topk_group groups hold k experts
-      gone += __popc(__ballot_sync(0xffffffffu, q[0] == last));
+    for (int i = 0; i < a.k; ++i) {
+      last = __reduce_max_sync(0xffffffffu, q[0]);
       if (q[0] == last) {
 #pragma unroll
         for (int j = 0; j + 1 < VPT; ++j) q[j] = q[j + 1];
@@ -250,36 +298,32 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
       }
     }
     uint32_t chosen = 0, at[VPT];                                      // at[j]: the lanes whose j-th expert is chosen
-    int total = 0;
+    auto places = [&] {                                                // how many chosen experts lower lanes have
+      int n = 0;
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) n += __popc(at[j] & ((1u << lane) - 1u));
+      return n;
+    };
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
-      chosen |= (uint32_t)(key[j] >= last) << j;
-      at[j] = __ballot_sync(0xffffffffu, key[j] >= last);
-      total += __popc(at[j]);
+      const bool in = key[j] >= last && key[j] != 0u;
+      chosen |= (uint32_t)in << j;
+      at[j] = __ballot_sync(0xffffffffu, in);
     }
+    int place = places();
+    const bool equal = __shfl_sync(0xffffffffu, place + __popc(chosen), 31) != a.k;      // equal values left together
     if (bias) {
       // fp32 errors of s: of the exponent |l - m| 2^-24 e^-|l - m|, of exponential, sum and quotient 2^-21 s at most; of the sum with
       // the bias 2^-24 of it.  Twice that between two values, rounded up.
       const uint32_t after = __reduce_max_sync(0xffffffffu, q[0]);
       const float low = order_value(last);
-      near = near || total > a.k || (after != 0 && !(low - order_value(after) > 0x1p-19f + 0x1p-22f * fabsf(low)));
+      near = near || equal || (after != 0 && !(low - order_value(after) > 0x1p-19f + 0x1p-22f * fabsf(low)));
     }
-    if (near) {
-      chosen = topk_choose_64(logits + t * a.E, bias, a, VPT, scratch[warp]);
+    if (near || equal) {
+      chosen = near ? topk_choose_64(logits + t * a.E, bias, a, VPT, scratch[warp]) : topk_choose_equal<VPT>(key, a.k);
 #pragma unroll
       for (int j = 0; j < VPT; ++j) at[j] = __ballot_sync(0xffffffffu, chosen >> j & 1);
-    } else if (total > a.k) {                                          // equal values at the border: the lowest indices of them stay
-      int spare = a.k, equal = 0;                                      // room for equal ones; those of lower lanes
-#pragma unroll
-      for (int j = 0; j < VPT; ++j) {
-        spare -= __popc(__ballot_sync(0xffffffffu, key[j] > last));
-        equal += __popc(__ballot_sync(0xffffffffu, key[j] == last) & ((1u << lane) - 1u));
-      }
-#pragma unroll
-      for (int j = 0; j < VPT; ++j) {
-        if (key[j] == last && equal++ >= spare) chosen &= ~(1u << j);
-        at[j] = __ballot_sync(0xffffffffu, chosen >> j & 1);
-      }
+      place = places();
     }
     float f = a.scale;
     if (a.renorm) {
@@ -289,15 +333,13 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
       f = a.scale / (warp_sum(sum) + kTopkEps);
     }
     // ascending: the chosen of lower lanes, then the lane's own
-    int place = 0;
-#pragma unroll
-    for (int j = 0; j < VPT; ++j) place += __popc(at[j] & ((1u << lane) - 1u));
-    const int64_t row = t * a.k;
+    int32_t* idx = expert_idx + t * a.k;
+    float* w = gate_w + t * a.k;
 #pragma unroll
     for (int j = 0; j < VPT; ++j)
       if (chosen >> j & 1) {
-        expert_idx[row + place] = e0 + j;
-        gate_w[row + place] = s[j] * f;
+        idx[place] = e0 + j;
+        w[place] = s[j] * f;
         ++place;
       }
   }
@@ -307,7 +349,7 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
 //   ds_c = scale / (S + eps) (g_c - sum_j g_j s_j / (S + eps)), S the sum of the chosen s;  without renorm scale g_c
 //   softmax: dl = s (ds - sum ds s)      sigmoid: dl = ds s (1 - s)
 // Lanes 0 to k - 1 hold the chosen pairs; rows of shared memory carry s to them and ds back.
-template <int VPT>
+template <int VPT, bool Full>
 __global__ void __launch_bounds__(kTopkWarps * 32)
 topk_bwd_kernel(const float* __restrict__ logits, const int32_t* __restrict__ expert_idx, const float* __restrict__ dgate_w,
                 const float* __restrict__ dscores_col, float* __restrict__ dlogits, TopkArgs a) {
@@ -326,7 +368,7 @@ topk_bwd_kernel(const float* __restrict__ logits, const int32_t* __restrict__ ex
   float next[VPT], next_g = 0.f;
   int next_e = -1;
   auto load = [&](int64_t tok) {
-    topk_load_row<VPT>(logits + tok * a.E, a.E, lane, next);
+    topk_load_row<VPT, Full>(logits + tok * a.E, a.E, lane, next);
     if (lane < a.k) {
       next_e = __ldg(expert_idx + tok * a.k + lane);
       next_g = __ldg(dgate_w + tok * a.k + lane);
@@ -341,7 +383,7 @@ topk_bwd_kernel(const float* __restrict__ logits, const int32_t* __restrict__ ex
     const int e = valid ? next_e : 0;
     float g = valid ? a.scale * next_g : 0.f;
     if (t + step < a.T) load(t + step);
-    topk_scores<VPT>(l, a.E, lane, a.sigmoid, s, rest);
+    topk_scores<VPT, Full>(l, a.E, lane, a.sigmoid, s, rest);
     float dot = 0.f;                                                   // sum of ds s over the row
     if (a.renorm || !a.sigmoid) {
 #pragma unroll
@@ -372,7 +414,7 @@ topk_bwd_kernel(const float* __restrict__ logits, const int32_t* __restrict__ ex
       const float ds = grow[e0 + j] + col[j];
       o[j] = a.sigmoid ? ds * s[j] * rest[j] : s[j] * (ds - dot);
     }
-    topk_store_row<VPT>(dlogits + t * a.E, a.E, lane, o);
+    topk_store_row<VPT, Full>(dlogits + t * a.E, a.E, lane, o);
     __syncwarp();
     if (valid) grow[e] = 0.f;
     __syncwarp();

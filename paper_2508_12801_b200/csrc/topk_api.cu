@@ -36,13 +36,16 @@ maxscore_status topk_args(const maxscore_ctx* c, const maxscore_topk* how, TopkA
 
 int topk_grid(const maxscore_ctx* c) { return (int)std::min<int64_t>(((int64_t)c->p.T + kTopkWarps - 1) / kTopkWarps, (int64_t)c->sm_count * 8); }
 
-// experts of a lane: rows of up to 32, 64, 96 and 128
+// experts of a lane: rows of up to 32, 64, 96 and 128; rows of 64 and 128 are moved as vectors
 template <typename F>
 void topk_by_width(int E, F go) {
-  if (E <= 32) go(std::integral_constant<int, 1>{});
-  else if (E <= 64) go(std::integral_constant<int, 2>{});
-  else if (E <= 96) go(std::integral_constant<int, 3>{});
-  else go(std::integral_constant<int, 4>{});
+  using std::false_type; using std::true_type;
+  if (E <= 32) go(std::integral_constant<int, 1>{}, false_type{});
+  else if (E < 64) go(std::integral_constant<int, 2>{}, false_type{});
+  else if (E == 64) go(std::integral_constant<int, 2>{}, true_type{});
+  else if (E <= 96) go(std::integral_constant<int, 3>{}, false_type{});
+  else if (E < 128) go(std::integral_constant<int, 4>{}, false_type{});
+  else go(std::integral_constant<int, 4>{}, true_type{});
 }
 
 }  // namespace
@@ -59,11 +62,12 @@ maxscore_status maxscore_topk_fwd(maxscore_ctx* c, const float* logits, const fl
   const size_t rows = sizeof(float) * (size_t)a.T * a.E, pairs = sizeof(float) * (size_t)a.T * a.k;
   if (!apart({{scores, rows}, {expert_idx, pairs}, {gate_w, pairs}}, {{logits, rows}, {bias, sizeof(float) * (size_t)a.E}}))
     return MAXSCORE_ERR_INVALID_ARG;
-  topk_by_width(a.E, [&](auto w) {
+  topk_by_width(a.E, [&](auto w, auto whole) {
     constexpr int V = decltype(w)::value;
+    constexpr bool F = decltype(whole)::value;
     const int lanes = a.group_size / V;
     a.group_lanes = a.group_size % V == 0 && (lanes & (lanes - 1)) == 0 ? lanes : 0;
-    auto kernel = a.n_group == 1 ? topk_fwd_kernel<V, 0> : a.group_lanes ? topk_fwd_kernel<V, 1> : topk_fwd_kernel<V, 2>;
+    auto kernel = a.n_group == 1 ? topk_fwd_kernel<V, 0, F> : a.group_lanes ? topk_fwd_kernel<V, 1, F> : topk_fwd_kernel<V, 2, F>;
     kernel<<<topk_grid(c), kTopkWarps * 32, 0, (cudaStream_t)stream>>>(logits, bias, scores, expert_idx, gate_w, a);
   });
   MS_LAUNCH_CHECK("topk_fwd_kernel");
@@ -82,8 +86,8 @@ maxscore_status maxscore_topk_bwd(maxscore_ctx* c, const float* logits, const in
   const size_t rows = sizeof(float) * (size_t)a.T * a.E, pairs = sizeof(float) * (size_t)a.T * a.k;
   if (!apart({{dlogits, rows}}, {{logits, rows}, {expert_idx, pairs}, {dgate_w, pairs}, {dscores_col, sizeof(float) * (size_t)a.E}}))
     return MAXSCORE_ERR_INVALID_ARG;
-  topk_by_width(a.E, [&](auto w) {
-    topk_bwd_kernel<decltype(w)::value><<<topk_grid(c), kTopkWarps * 32, 0, (cudaStream_t)stream>>>(logits, expert_idx, dgate_w, dscores_col,
+  topk_by_width(a.E, [&](auto w, auto whole) {
+    topk_bwd_kernel<decltype(w)::value, decltype(whole)::value><<<topk_grid(c), kTopkWarps * 32, 0, (cudaStream_t)stream>>>(logits, expert_idx, dgate_w, dscores_col,
                                                                                                       dlogits, a);
   });
   MS_LAUNCH_CHECK("topk_bwd_kernel");
