@@ -340,6 +340,61 @@ maxscore_status maxscore_expert_glu_bwd(maxscore_ctx* ctx, const void* dy, const
                                         const int32_t* expert_load, void* dpre, int32_t d_out, int32_t d_ff, int32_t w_layout,
                                         void* cuda_stream);
 
+/* ---- the experts in 8-bit integers (serving; bf16 I/O only) ------------------------------------------- */
+
+/* A row x (of tokens, or the weights of one column) becomes q = rint(x * inv), ties to even, inv = 127 / amax in fp32 and amax its
+ * largest magnitude; it stands for q * scale, scale = amax / 127 in fp32.  Where amax < 2^-118, q and scale are zero; where a value is
+ * not finite, scale is NaN and q zero, and so every product of that row is NaN.
+ * Integers are rows of bytes, [E, C, width], with one fp32 scale per row, [E, C]; weights [E, d_out, d_in] (d_in contiguous) with
+ * one per column of the product, [E, d_out].  Rows in use, rows behind them and overlaps as in the products above.
+ * Products sum the integers exactly (in 32 bits; any signed bytes) and are scaled and rounded to bf16 once.
+ * Reproducible bit for bit.  maxscore_check_internal tells whether a bounded wait gave up.
+ * Errors: NULL or misaligned (16 bytes) pointers, an output that shares memory with another argument, non-positive widths,
+ * w_layout not 0 or 1 -> MAXSCORE_ERR_INVALID_ARG; fp32 I/O, integer rows (d_model, width, d_in) that are no multiple of 16 or not below
+ * 2^17, d_out or d_ff that is no multiple of 8 or too large (2^24, 2^23) -> MAXSCORE_ERR_UNSUPPORTED. */
+
+/* maxscore_dispatch with the rows quantised on the way: dst [E, C, d_model] integers, dst_scale [E, C]; empty slots get zeros. */
+maxscore_status maxscore_dispatch_q8(maxscore_ctx* ctx, const void* src, const int32_t* expert_idx, const int32_t* slot_idx,
+                                     const int32_t* slot_token, int8_t* dst, float* dst_scale, void* cuda_stream);
+
+/* Rows of an expert buffer x [E, C, width] quantised (h, between the two products); zeros behind the load. */
+maxscore_status maxscore_expert_quant(maxscore_ctx* ctx, const void* x, const int32_t* expert_load, int8_t* q, float* q_scale,
+                                      int32_t width, void* cuda_stream);
+
+/* Weights w [E, d_in, d_out] (w_layout 1: [E, d_out, d_in]) quantised per column: wq [E, d_out, d_in], w_scale [E, d_out].
+ * For maxscore_expert_glu_q8 d_out = 2 d_ff, gate columns first.  Once per weight. */
+maxscore_status maxscore_expert_quant_weight(maxscore_ctx* ctx, const void* w, int8_t* wq, float* w_scale, int32_t d_in, int32_t d_out,
+                                             int32_t w_layout, void* cuda_stream);
+
+/* y[e, s, :] = (xq[e, s, :] . wq_e^T) * x_scale[e, s] * w_scale[e, :]        y [E, C, d_out] bf16 */
+maxscore_status maxscore_expert_gemm_q8(maxscore_ctx* ctx, const int8_t* xq, const float* x_scale, const int8_t* wq,
+                                        const float* w_scale, const int32_t* expert_load, void* y, int32_t d_in, int32_t d_out,
+                                        void* cuda_stream);
+
+/* [g | u] the same product with w_up, wq [E, 2 d_ff, d_in]; h = silu(g) * u from the unrounded g and u.   h [E, C, d_ff] bf16 */
+maxscore_status maxscore_expert_glu_q8(maxscore_ctx* ctx, const int8_t* xq, const float* x_scale, const int8_t* wq,
+                                       const float* w_scale, const int32_t* expert_load, void* h, int32_t d_in, int32_t d_ff,
+                                       void* cuda_stream);
+
+/* ---- expert activations kept in 8 bits (training; bf16 I/O only) --------------------------------------- */
+
+/* maxscore_expert_glu and its backward with [g | u] kept in 8 bits instead of bf16, a scale for each 32 columns of a row of g
+ * and of u, quantised as above (columns behind d_ff count as zeros).  keep, 32-byte aligned:
+ *   int8 [E, C, 2, w], w = d_ff rounded up to 32, g first; then, from a multiple of 256 bytes on, fp32 scales [E, 2 w / 32, C], g's first.
+ * Only the rows in use are written, and read again.  1.125 bytes a value instead of 2, and h need not be kept either: the backward call
+ * forms it again.  Other arguments, reproducibility and errors as in maxscore_expert_glu and _glu_bwd; fp32 I/O ->
+ * MAXSCORE_ERR_UNSUPPORTED. */
+maxscore_status maxscore_keep8_bytes(const maxscore_ctx* ctx, int32_t d_ff, size_t* bytes);   /* host only */
+
+maxscore_status maxscore_expert_glu_keep8(maxscore_ctx* ctx, const void* x, const void* w_up, const int32_t* expert_load, void* keep,
+                                          void* h, int32_t d_in, int32_t d_ff, int32_t w_layout, void* cuda_stream);
+
+/* dpre as maxscore_expert_glu_bwd forms it, from the kept g and u; h [E, C, d_ff] out, silu(g) * u of the kept values (for the gradient
+ * of w_down), or NULL. */
+maxscore_status maxscore_expert_glu_bwd_keep8(maxscore_ctx* ctx, const void* dy, const void* w_down, const void* keep,
+                                              const int32_t* expert_load, void* dpre, void* h, int32_t d_out, int32_t d_ff,
+                                              int32_t w_layout, void* cuda_stream);
+
 /* ---- the norms before and after the block ---------------------------------------------------------- */
 
 /* After-norm, gate, scaled residual and before-norm around a block, all steps in one pass over the rows:

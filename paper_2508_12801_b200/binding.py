@@ -61,7 +61,9 @@ EXPORTS = ["maxscore_capacity", "maxscore_workspace_bytes", "maxscore_create", "
            "maxscore_softtopk_bwd_aux", "maxscore_check_internal", "maxscore_launch_count",
            "maxscore_test_raise_internal", "maxscore_assign_iterative", "maxscore_assign_top2_sinkhorn",
            "maxscore_expert_gemm", "maxscore_expert_gemm_dw", "maxscore_expert_glu", "maxscore_expert_glu_bwd",
-           "maxscore_combine_norm", "maxscore_block_norm", "maxscore_block_norm_bwd", "maxscore_topk_fwd", "maxscore_topk_bwd"]
+           "maxscore_combine_norm", "maxscore_block_norm", "maxscore_block_norm_bwd", "maxscore_topk_fwd", "maxscore_topk_bwd",
+           "maxscore_dispatch_q8", "maxscore_expert_quant", "maxscore_expert_quant_weight", "maxscore_expert_gemm_q8", "maxscore_expert_glu_q8",
+           "maxscore_keep8_bytes", "maxscore_expert_glu_keep8", "maxscore_expert_glu_bwd_keep8"]
 
 
 def _load():
@@ -93,6 +95,14 @@ _lib.maxscore_block_norm.argtypes = [_vp] * 7
 _lib.maxscore_block_norm_bwd.argtypes = [_vp] * 12
 _lib.maxscore_topk_fwd.argtypes = [_vp] * 8
 _lib.maxscore_topk_bwd.argtypes = [_vp] * 8
+_lib.maxscore_dispatch_q8.argtypes = [_vp] * 8
+_lib.maxscore_expert_quant.argtypes = [_vp] * 5 + [_i32, _vp]
+_lib.maxscore_expert_quant_weight.argtypes = [_vp] * 4 + [_i32] * 3 + [_vp]
+_lib.maxscore_expert_gemm_q8.argtypes = [_vp] * 7 + [_i32] * 2 + [_vp]
+_lib.maxscore_expert_glu_q8.argtypes = [_vp] * 7 + [_i32] * 2 + [_vp]
+_lib.maxscore_keep8_bytes.argtypes = [_vp, _i32, C.POINTER(C.c_size_t)]
+_lib.maxscore_expert_glu_keep8.argtypes = [_vp] * 6 + [_i32] * 3 + [_vp]
+_lib.maxscore_expert_glu_bwd_keep8.argtypes = [_vp] * 7 + [_i32] * 3 + [_vp]
 
 
 class MaxScoreError(RuntimeError):
@@ -322,6 +332,73 @@ def expert_glu_bwd(ctx, dy, w_down, pre, expert_load, dpre, d_out, d_ff, w_layou
           _need(ctx, "w_down", w_down, io, ctx.params.E * d_ff * d_out), _need(ctx, "pre", pre, io, rows * 2 * d_ff),
           _need(ctx, "expert_load", expert_load, torch.int32, ctx.params.E), _need(ctx, "dpre", dpre, io, rows * 2 * d_ff), d_out, d_ff,
           w_layout, stream=stream)
+
+
+# ---- the experts in 8-bit integers --------------------------------------------------------------------------
+def dispatch_q8(ctx, src, expert_idx, slot_idx, slot_token, dst, dst_scale, stream=None):
+    """dispatch with the rows quantised on the way: int8 rows and one fp32 scale each."""
+    p, i32 = ctx.params, torch.int32
+    rows, pairs = p.E * ctx.capacity, p.T * p.k
+    _call(ctx, "maxscore_dispatch_q8", _lib.maxscore_dispatch_q8, _need(ctx, "src", src, ctx.io_torch, p.T * p.d_model),
+          _need(ctx, "expert_idx", expert_idx, i32, pairs), _need(ctx, "slot_idx", slot_idx, i32, pairs), _need(ctx, "slot_token", slot_token, i32, rows),
+          _need(ctx, "dst", dst, torch.int8, rows * p.d_model), _need(ctx, "dst_scale", dst_scale, torch.float32, rows), stream=stream)
+
+
+def expert_quant(ctx, x, expert_load, q, q_scale, width, stream=None):
+    """Rows of an expert buffer in 8-bit integers, zeros behind the load."""
+    rows = ctx.params.E * ctx.capacity
+    _call(ctx, "maxscore_expert_quant", _lib.maxscore_expert_quant, _need(ctx, "x", x, ctx.io_torch, rows * width),
+          _need(ctx, "expert_load", expert_load, torch.int32, ctx.params.E), _need(ctx, "q", q, torch.int8, rows * width),
+          _need(ctx, "q_scale", q_scale, torch.float32, rows), width, stream=stream)
+
+
+def expert_quant_weight(ctx, w, wq, w_scale, d_in, d_out, w_layout=0, stream=None):
+    """Weights in 8-bit integers [E, d_out, d_in] with a scale per column of the product, once per weight."""
+    E = ctx.params.E
+    _call(ctx, "maxscore_expert_quant_weight", _lib.maxscore_expert_quant_weight, _need(ctx, "w", w, ctx.io_torch, E * d_in * d_out),
+          _need(ctx, "wq", wq, torch.int8, E * d_in * d_out), _need(ctx, "w_scale", w_scale, torch.float32, E * d_out), d_in, d_out, w_layout,
+          stream=stream)
+
+
+def expert_gemm_q8(ctx, xq, x_scale, wq, w_scale, expert_load, y, d_in, d_out, stream=None):
+    """expert_gemm on 8-bit rows and weights: integer sums, scaled by row and column."""
+    E, rows, i8, f32 = ctx.params.E, ctx.params.E * ctx.capacity, torch.int8, torch.float32
+    _call(ctx, "maxscore_expert_gemm_q8", _lib.maxscore_expert_gemm_q8, _need(ctx, "xq", xq, i8, rows * d_in), _need(ctx, "x_scale", x_scale, f32, rows),
+          _need(ctx, "wq", wq, i8, E * d_in * d_out), _need(ctx, "w_scale", w_scale, f32, E * d_out),
+          _need(ctx, "expert_load", expert_load, torch.int32, E), _need(ctx, "y", y, ctx.io_torch, rows * d_out), d_in, d_out, stream=stream)
+
+
+def expert_glu_q8(ctx, xq, x_scale, wq, w_scale, expert_load, h, d_in, d_ff, stream=None):
+    """h = silu(g) u with [g | u] the product of 8-bit rows and weights [E, 2 d_ff, d_in]."""
+    E, rows, i8, f32 = ctx.params.E, ctx.params.E * ctx.capacity, torch.int8, torch.float32
+    _call(ctx, "maxscore_expert_glu_q8", _lib.maxscore_expert_glu_q8, _need(ctx, "xq", xq, i8, rows * d_in), _need(ctx, "x_scale", x_scale, f32, rows),
+          _need(ctx, "wq", wq, i8, E * d_in * 2 * d_ff), _need(ctx, "w_scale", w_scale, f32, E * 2 * d_ff),
+          _need(ctx, "expert_load", expert_load, torch.int32, E), _need(ctx, "h", h, ctx.io_torch, rows * d_ff), d_in, d_ff, stream=stream)
+
+
+# ---- expert activations kept in 8 bits -----------------------------------------------------------------------
+def keep8_bytes(ctx, d_ff) -> int:
+    """Size of the buffer (uint8) in which expert_glu_keep8 leaves [g | u]."""
+    n = C.c_size_t(0)
+    _check(_lib.maxscore_keep8_bytes(ctx.handle, d_ff, C.byref(n)), "maxscore_keep8_bytes")
+    return int(n.value)
+
+
+def expert_glu_keep8(ctx, x, w_up, expert_load, keep, h, d_in, d_ff, w_layout=0, stream=None):
+    """expert_glu with [g | u] kept in 8 bits."""
+    io, rows = ctx.io_torch, ctx.params.E * ctx.capacity
+    _call(ctx, "maxscore_expert_glu_keep8", _lib.maxscore_expert_glu_keep8, _need(ctx, "x", x, io, rows * d_in),
+          _need(ctx, "w_up", w_up, io, ctx.params.E * d_in * 2 * d_ff), _need(ctx, "expert_load", expert_load, torch.int32, ctx.params.E),
+          _need(ctx, "keep", keep, torch.uint8, keep8_bytes(ctx, d_ff)), _need(ctx, "h", h, io, rows * d_ff), d_in, d_ff, w_layout, stream=stream)
+
+
+def expert_glu_bwd_keep8(ctx, dy, w_down, keep, expert_load, dpre, h, d_out, d_ff, w_layout=0, stream=None):
+    """expert_glu_bwd from what expert_glu_keep8 kept; h (may be None) receives silu(g) u formed again."""
+    io, rows = ctx.io_torch, ctx.params.E * ctx.capacity
+    _call(ctx, "maxscore_expert_glu_bwd_keep8", _lib.maxscore_expert_glu_bwd_keep8, _need(ctx, "dy", dy, io, rows * d_out),
+          _need(ctx, "w_down", w_down, io, ctx.params.E * d_ff * d_out), _need(ctx, "keep", keep, torch.uint8, keep8_bytes(ctx, d_ff)),
+          _need(ctx, "expert_load", expert_load, torch.int32, ctx.params.E), _need(ctx, "dpre", dpre, io, rows * 2 * d_ff),
+          _need(ctx, "h", h, io, rows * d_ff, optional=True), d_out, d_ff, w_layout, stream=stream)
 
 
 def make_norm(w_post=None, gate=None, w_pre=None, rows_per_gate=0, eps=1e-5, w_offset=0.0, res_scale=1.0) -> Norm:

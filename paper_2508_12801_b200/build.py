@@ -8,9 +8,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmaxscore.so")
-SOURCES = ["maxscore_api.cu", "blocks_api.cu", "topk_api.cu"]
+SOURCES = ["maxscore_api.cu", "blocks_api.cu", "topk_api.cu", "experts8_api.cu"]
 HEADERS = ["common.cuh", "context.cuh", "tc.cuh", "flow.cuh", "gate.cuh", "move.cuh", "softtopk.cuh", "reroute.cuh", "alg1.cuh", "expert.cuh",
-           "expert_tc.cuh", "expert_few.cuh", "norm.cuh", "topk.cuh",
+           "expert_tc.cuh", "expert_few.cuh", "expert_launch.cuh", "int8.cuh", "rows8.cuh", "norm.cuh", "topk.cuh",
            os.path.join("..", "..", "include", "maxscore.h")]
 
 

@@ -56,7 +56,7 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-constexpr int kRoomyMax = 32;            // more than the kernels that one context's sizes and type can choose
+constexpr int kRoomyMax = 64;            // more than the kernels that one context's sizes and type can choose
 
 }  // namespace msr
 

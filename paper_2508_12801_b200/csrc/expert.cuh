@@ -15,12 +15,18 @@
 namespace msr {
 
 enum ExpertEpi { kEpiPlain = 0, kEpiGlu = 1, kEpiDact = 2, kEpiDw = 3 };
+// kBf16: operands and results in bf16.  kInt8: operands in 8-bit integers with a scale per row and per column.  kKeep8: as kBf16, with
+// [g | u] kept in 8 bits.
+enum ExpertForm { kBf16 = 0, kInt8 = 1, kKeep8 = 2 };
 
 struct ExpertArgs {
   const int32_t* load;      // [E]
   int E, C;
   int M, N, K;              // dW: M = d_in, N = d_out, K per expert; else M per expert, N = columns (d_ff for the gated ones)
   int accumulate;           // dW only
+  const float *x_scale, *w_scale;      // kInt8: [E, C], and a column's in the order of the weights' columns
+  int8_t* keep;             // kKeep8: integers [E, C, 2, keep_width], g first
+  float* keep_scale;        // kKeep8: [E, 2 keep_width / 32, C]
   int a_chunks, b_chunks;   // tensor cores: the operand's map has the 64-column chunks as a dimension of their own
 };
 
@@ -46,7 +52,7 @@ __device__ __forceinline__ void dact(float dh, float g, float u, float& dg, floa
 
 // Rows behind the loads of an [E, C, row] buffer become zero.  `grain`: rows that the tiles of the caller write anyway
 // (their last tile is written whole, zeros behind the load).
-__device__ void expert_zero_behind(const ExpertArgs& a, const int* rows, char* y, size_t row_bytes, int grain, int worker,
+__device__ inline void expert_zero_behind(const ExpertArgs& a, const int* rows, char* y, size_t row_bytes, int grain, int worker,
                                    int workers) {
   const int vecs = (int)(row_bytes / 16);
   for (int e = 0; e < a.E; ++e) {
@@ -59,7 +65,7 @@ __device__ void expert_zero_behind(const ExpertArgs& a, const int* rows, char* y
 }
 
 // The same where rows are few: a warp per row of the whole buffer, so that many experts with next to nothing cost one step.
-__device__ void expert_zero_behind_rows(const ExpertArgs& a, const int* rows, char* y, size_t row_bytes, int warp, int warps) {
+__device__ inline void expert_zero_behind_rows(const ExpertArgs& a, const int* rows, char* y, size_t row_bytes, int warp, int warps) {
   const int vecs = (int)(row_bytes / 16), lane = threadIdx.x & 31;
   for (int r = warp; r < a.E * a.C; r += warps) {
     const int e = r / a.C;

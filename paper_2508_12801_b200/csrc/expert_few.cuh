@@ -36,7 +36,7 @@ __device__ __forceinline__ bool all_epilogue_threads(bool x) {
 }
 
 // W_MN: the weights' columns are contiguous.  tW0 / tW1: weights (gated: gate / up columns); tX: the rows.
-template <int EPI, bool W_MN>
+template <int EPI, bool W_MN, int Form = kBf16>
 __global__ void __launch_bounds__(kFewThreads)
 expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant__ CUtensorMap tW1, const __grid_constant__ CUtensorMap tX,
                   __nv_bfloat16* __restrict__ out, __nv_bfloat16* __restrict__ pre_out, ExpertArgs a, int pad, unsigned* error_flag) {
@@ -46,7 +46,8 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
   float* up = reinterpret_cast<float*>(base + kFewRing);              // [pad][64], gated only
   __shared__ FewSmem sm;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int ntn = (a.N + kCols - 1) / kCols, nkb = (a.K + kXBK - 1) / kXBK;
+  constexpr int kBK = Form == kInt8 ? 2 * kXBK : kXBK, kDepth = kBK / 4;      // depths of a slice (128 bytes) and of an MMA
+  const int ntn = (a.N + kCols - 1) / kCols, nkb = (a.K + kBK - 1) / kBK;
   const int stage_bytes = few_stage_bytes(pad), stages = min(kFewMaxStages, kFewRing / stage_bytes);
   uint32_t tmem_cols = 32;
   while ((int)tmem_cols < 2 * pad) tmem_cols <<= 1;
@@ -78,7 +79,7 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
           if (!ok) break;
           unsigned char* w = base + (size_t)s * stage_bytes;
           const uint32_t sw = smem_u32(w);
-          const int k0 = kb * kXBK;
+          const int k0 = kb * kBK;
           mbar_expect_tx(&sm.full[s], stage_bytes);
           if (EPI == kEpiGlu) {
             if (W_MN) { tma_load_3d(sw, &tW0, n0, k0, e, &sm.full[s]); tma_load_3d(sw + 8192, &tW1, n0, k0, e, &sm.full[s]); }
@@ -97,7 +98,10 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
       if (!ok) sm.failed = 1;
     }
   } else if (warp == 1) {
-    const uint32_t idesc = idesc_bf16_m128(pad) | (W_MN ? 1u << 15 : 0u);
+    const uint32_t idesc = idesc_types(Form) | ((uint32_t)(pad >> 3) << 17) | ((128u >> 4) << 24) | (W_MN ? 1u << 15 : 0u);
+    auto mma = [](uint32_t d, uint64_t wd, uint64_t xd, uint32_t id, uint32_t add) {
+      if constexpr (Form == kInt8) umma_i8(d, wd, xd, id, add); else umma_bf16(d, wd, xd, id, add);
+    };
     constexpr uint32_t kWStep = W_MN ? 128 : 2;
     int s = 0, turn = 0; uint32_t ph = 0; bool ok = true;
     for (int t = blockIdx.x; t < total && ok; t += gridDim.x, ++turn) {
@@ -110,12 +114,12 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
         tc_fence_after();
         const uint32_t sw = smem_u32(base) + (uint32_t)(s * stage_bytes);
         const uint64_t wd = W_MN ? smem_desc_mn128(sw, 8192u) : smem_desc_k128(sw), xd = smem_desc_k128(sw + 16384);
-        const int left = a.K - kb * kXBK;
+        const int left = a.K - kb * kBK;
         if (elect_one()) {
-          umma_bf16(acc, wd, xd, idesc, kb > 0 ? 1u : 0u);
-          if (left > 16) umma_bf16(acc, wd + kWStep, xd + 2, idesc, 1u);
-          if (left > 32) umma_bf16(acc, wd + 2 * kWStep, xd + 4, idesc, 1u);
-          if (left > 48) umma_bf16(acc, wd + 3 * kWStep, xd + 6, idesc, 1u);
+          mma(acc, wd, xd, idesc, kb > 0 ? 1u : 0u);
+          if (left > kDepth) mma(acc, wd + kWStep, xd + 2, idesc, 1u);
+          if (left > 2 * kDepth) mma(acc, wd + 2 * kWStep, xd + 4, idesc, 1u);
+          if (left > 3 * kDepth) mma(acc, wd + 3 * kWStep, xd + 6, idesc, 1u);
           umma_commit(&sm.empty[s]);
           if (kb == nkb - 1) umma_commit(&sm.acc_full[buf]);
         }
@@ -142,10 +146,33 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
       if (EPI == kEpiGlu) ok = all_epilogue_threads(ok);   // (also: the last item's values have been read from `up`)
       if (!ok) break;
       tc_fence_after();
+      float col_scale = 0.f;
+      if (Form == kInt8 && col < a.N) col_scale = __ldg(a.w_scale + (EPI == kEpiGlu ? (size_t)e * 2 * a.N + (q >= 2 ? a.N : 0) : (size_t)e * a.N) + col);
+      // rows c0 to c0 + 15 of the column; 32-bit integers become the values they stand for
+      auto take = [&](int c0, float (&r)[16]) {
+        tmem_ld16(acc + c0, r);
+        if constexpr (Form == kInt8) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            r[j] = c0 + j < rows ? (float)__float_as_int(r[j]) * (__ldg(a.x_scale + row0 + c0 + j) * col_scale) : 0.f;
+        }
+      };
+      // kKeep8: a warp's 32 columns of a row are a block; columns behind d_ff are zero, as the copies filled the weights up
+      auto keep = [&](int c0, const float (&r)[16]) {
+        const int fp = keep_width(a.N), blocks = fp / kKeepBlock, half = q >= 2, first = col - lane;
+        if (first >= a.N) return;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          if (c0 + j >= rows) break;
+          const Step8 st8 = step8(__reduce_max_sync(0xffffffffu, abs_bits(__float_as_uint(r[j]))));
+          a.keep[((row0 + c0 + j) * 2 + half) * fp + col] = st8.inv > 0.f ? (int8_t)round8(r[j], st8.inv) : (int8_t)0;
+          if (lane == 0) a.keep_scale[((size_t)e * 2 * blocks + half * blocks + first / kKeepBlock) * a.C + c0 + j] = st8.scale;
+        }
+      };
       if constexpr (EPI == kEpiPlain) {
         for (int c0 = 0; c0 < rows; c0 += 16) {
           float r[16];
-          tmem_ld16(acc + c0, r);
+          take(c0, r);
           if (col < a.N) {
 #pragma unroll
             for (int j = 0; j < 16; ++j)
@@ -156,7 +183,8 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
         if (q >= 2)
           for (int c0 = 0; c0 < rows; c0 += 16) {
             float r[16];
-            tmem_ld16(acc + c0, r);
+            take(c0, r);
+            if constexpr (Form == kKeep8) keep(c0, r);
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
               up[(c0 + j) * 64 + (q & 1) * 32 + lane] = r[j];
@@ -167,7 +195,8 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
         if (q < 2)
           for (int c0 = 0; c0 < rows; c0 += 16) {
             float r[16];
-            tmem_ld16(acc + c0, r);
+            take(c0, r);
+            if constexpr (Form == kKeep8) keep(c0, r);
             if (col < a.N) {
 #pragma unroll
               for (int j = 0; j < 16; ++j)

@@ -14,6 +14,7 @@
 // shared memory by the producer warp before the pair's MMA may read the slice.
 #pragma once
 #include "expert.cuh"
+#include "int8.cuh"
 
 namespace msr {
 
@@ -77,6 +78,14 @@ __device__ __forceinline__ void umma_bf16_pair(uint32_t tmem_d, uint64_t adesc, 
       "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+__device__ __forceinline__ void umma_i8_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// What differs between the operands' types in an instruction descriptor: bf16 x bf16 -> fp32, or signed bytes -> 32-bit integers.
+__host__ __device__ constexpr uint32_t idesc_types(int form) { return (form == kInt8 ? 2u << 4 : 1u << 4) | (1u << 7) | (1u << 10); }
 __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {     // arrives on the same barrier of both CTAs
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
                "h"((uint16_t)3) : "memory");
@@ -178,14 +187,15 @@ __device__ __forceinline__ void expert_prefix(const ExpertArgs& a, int* rows, in
 // EPI as in expert.cuh.  B_MN: B is stored with its columns contiguous.  dW: both operands run along the rows.
 // Maps: tA; tB0 / tB1 = B of the leading / the other CTA (gate and up columns in the gated form, else the same).
 // Add: dW is added to what is there.  W = 2 with dW: one sum whatever its length, for capacities up to kXPartRows.
-// tO0: y or h; tO1 / tO2: g / u kept (gated).  out: y, h, dpre or dW; pre_out: [g | u] kept or null; pre_in: [g | u] (backward).
-template <int EPI, bool B_MN, int W, bool Add = false>
+// tO0: y or h; tO1 / tO2: g / u kept (gated).  out: y, h, dpre or dW; pre_out: [g | u] kept or null, h or null in the backward of kKeep8;
+// pre_in: [g | u] (backward of kBf16).
+template <int EPI, bool B_MN, int W, bool Add = false, int Form = kBf16>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(x_threads(EPI))
 expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__ CUtensorMap tB0, const __grid_constant__ CUtensorMap tB1,
                  const __grid_constant__ CUtensorMap tO0, const __grid_constant__ CUtensorMap tO1, const __grid_constant__ CUtensorMap tO2,
                  char* __restrict__ out, char* __restrict__ pre_out, const char* __restrict__ pre_in, ExpertArgs a, unsigned* error_flag) {
   constexpr bool kDw = EPI == kEpiDw, kA_MN = kDw, kParts = kDw && W == 1;
-  constexpr int kEpiWarps = x_epi_warps(EPI);
+  constexpr int kEpiWarps = x_epi_warps(EPI), kBK = Form == kInt8 ? 2 * kXBK : kXBK;      // depth of a slice: 128 bytes
   constexpr int kStages = x_stages(EPI, W), kStageBytes = x_stage_bytes(W);
   constexpr int kTileN = EPI == kEpiGlu ? 128 : kXTile;               // output columns of a tile
   extern __shared__ unsigned char xsm_raw[];
@@ -225,7 +235,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
     const CUtensorMap* tB = rank ? &tB1 : &tB0;
     while (ok && walk.next(x)) {
       const int K = kDw ? x.rows : a.K;
-      const int nkb = (K + kXBK - 1) / kXBK;
+      const int nkb = (K + kBK - 1) / kBK;
       const int ax = x.m * kXTile + 128 * rank;
       const int bx = EPI == kEpiGlu ? x.n * 128 : x.n * kXTile + 128 * rank;
       const uint32_t bytes = 16384u * (uint32_t)(1 + x.subs);
@@ -234,7 +244,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
         const uint32_t ph = (uint32_t)((it / kStages) & 1);
         const uint32_t sa = smem_u32(base) + (uint32_t)(s * kStageBytes), sb = sa + 16384;
         const uint32_t full = full0 + 8u * (uint32_t)s;
-        const int k0 = kb * kXBK;
+        const int k0 = kb * kBK;
         const bool masked = kDw && kb == nkb - 1 && (K & 15);          // the load ends inside an MMA's depth
         int good = 1;
         if (lane == 0) {
@@ -297,9 +307,13 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
     // The tensor pipe holds little beyond the MMA it runs, so every clock between a slice's last MMA and the next one's
     // first shows.  The whole warp walks and waits (its values stay in uniform registers, where the MMA wants them), one
     // elected lane issues a slice's four MMAs and its commit in a row.
-    const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (kA_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
+    const uint32_t idesc = idesc_types(Form) | (kA_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
                            ((uint32_t)(kXTile >> 3) << 17) | ((uint32_t)(kXTile >> 4) << 24);
-    constexpr uint32_t kAStep = kA_MN ? 128 : 2, kBStep = B_MN ? 128 : 2;      // 16 deep, in descriptor units of 16 bytes
+    constexpr uint32_t kAStep = kA_MN ? 128 : 2, kBStep = B_MN ? 128 : 2;      // an MMA's depth (32 bytes) in descriptor units of 16 bytes
+    constexpr int kDepth = kBK / 4;
+    auto mma = [](uint32_t d, uint64_t ad, uint64_t bd, uint32_t id, uint32_t add) {
+      if constexpr (Form == kInt8) umma_i8_pair(d, ad, bd, id, add); else umma_bf16_pair(d, ad, bd, id, add);
+    };
     const uint64_t adesc0 = kA_MN ? smem_desc_mn128(smem_u32(base), 8192u) : smem_desc_k128(smem_u32(base));
     const uint64_t bdesc0 = B_MN ? smem_desc_mn128(smem_u32(base) + 16384, 8192u) : smem_desc_k128(smem_u32(base) + 16384);
     XWalk<W> walk(sm, a, ntn, pair, pairs);
@@ -308,7 +322,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
     int s0 = 0, turn = 0; bool ok = true;               // s0: ring position of slice kb
     while (ok && walk.next(x)) {
       const int K = kDw ? x.rows : a.K;
-      const int nkb = (K + kXBK - 1) / kXBK;
+      const int nkb = (K + kBK - 1) / kBK;
       if (nkb == 0) continue;
       // With two column tiles the first and the last slices are multiplied group-wise, the first column tile ahead of the
       // second: its accumulator is complete (and free again) that much earlier, which is what hides the epilogues.
@@ -331,12 +345,12 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
             if (!ok) break;
             tc_fence_after();
             const uint64_t ad = adesc0 + (uint64_t)(s * (kStageBytes / 16)), bd = bdesc0 + (uint64_t)(s * (kStageBytes / 16) + h * 1024);
-            const int left = K - (kb + j) * kXBK;
+            const int left = K - (kb + j) * kBK;
             if (elect_one()) {
-              umma_bf16_pair(acc, ad, bd, idesc, kb + j > begin ? 1u : 0u);
-              if (left > 16) umma_bf16_pair(acc, ad + kAStep, bd + kBStep, idesc, 1u);
-              if (left > 32) umma_bf16_pair(acc, ad + 2 * kAStep, bd + 2 * kBStep, idesc, 1u);
-              if (left > 48) umma_bf16_pair(acc, ad + 3 * kAStep, bd + 3 * kBStep, idesc, 1u);
+              mma(acc, ad, bd, idesc, kb + j > begin ? 1u : 0u);
+              if (left > kDepth) mma(acc, ad + kAStep, bd + kBStep, idesc, 1u);
+              if (left > 2 * kDepth) mma(acc, ad + 2 * kAStep, bd + 2 * kBStep, idesc, 1u);
+              if (left > 3 * kDepth) mma(acc, ad + 3 * kAStep, bd + 3 * kBStep, idesc, 1u);
               if (h == x.subs - 1) umma_commit_pair(&sm.empty[s]);
               if (kb + j == end - 1) umma_commit_pair(&sm.acc_full[buf]);
             }
@@ -357,6 +371,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       const int worker = (blockIdx.x * kEpiWarps + warp - 2) * 32 + lane, workers = gridDim.x * kEpiWarps * 32;
       expert_zero_behind(a, sm.rows, out, 2 * (size_t)(EPI == kEpiDact ? 2 * a.N : a.N), kXTile, worker, workers);
       if (EPI == kEpiGlu && pre_out) expert_zero_behind(a, sm.rows, pre_out, 4 * (size_t)a.N, kXTile, worker, workers);
+      if (EPI == kEpiDact && Form == kKeep8 && pre_out) expert_zero_behind(a, sm.rows, pre_out, 2 * (size_t)a.N, kXTile, worker, workers);
     }
     unsigned char* stage = base + kStages * kStageBytes + (size_t)(warp - 2) * x_box_bytes(EPI);
     const uint32_t acc_empty0 = map_to_rank(smem_u32(&sm.acc_empty[0]), 0);
@@ -432,7 +447,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
     uint32_t acc_ph = 0;                                // bit b: parity to wait for at accumulator b
     int turn = 0; bool ok = true;
     while (ok && walk.next(x)) {
-      const int nkb = ((kDw ? x.rows : a.K) + kXBK - 1) / kXBK;
+      const int nkb = ((kDw ? x.rows : a.K) + kBK - 1) / kBK;
       const int y0 = x.m * kXTile + 128 * rank + 32 * q;              // first row of this warp
       const int rows = min(32, (kDw ? a.M : a.C) - y0);               // rows of the tensor; may be none
       const size_t row0 = (size_t)x.e * (kDw ? a.M : a.C) + y0;
@@ -482,7 +497,35 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
         const int col0 = (x.n + sub) * kTileCols + part * kCols;
         const uint32_t acc = tmem + lanes + (uint32_t)(buf * 256 + part * kCols);
         const bool keep_row = kDw || y0 + lane < x.rows;              // rows behind the load come out as zeros
-        if (EPI == kEpiDact) fetch(row0, rows, col0);
+        float row_scale = 0.f;
+        if (Form == kInt8 && keep_row) row_scale = __ldg(a.x_scale + row0 + lane);
+        // 16 columns from `col` on (of N; the weights' column `of` has column 0) as products of fp32 values: an integer is exact up to 2^24 and
+        // else rounded once
+        auto unscale = [&](uint32_t (&u)[16], int col, const float* of) {
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            const float4 c = col + i < a.N ? __ldg(reinterpret_cast<const float4*>(of + col + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            u[i] = __float_as_uint((float)(int)u[i] * (row_scale * c.x)); u[i + 1] = __float_as_uint((float)(int)u[i + 1] * (row_scale * c.y));
+            u[i + 2] = __float_as_uint((float)(int)u[i + 2] * (row_scale * c.z)); u[i + 3] = __float_as_uint((float)(int)u[i + 3] * (row_scale * c.w));
+          }
+        };
+        uint32_t kg[8] = {}, ku[8] = {};                               // kKeep8: 32 columns of the row's g and u, and their steps
+        float sg = 0.f, su = 0.f;
+        auto fetch8 = [&](int col) {
+          if (keep_row && col < a.N) {
+            const int fp = keep_width(a.N), blocks = fp / kKeepBlock;
+            const int8_t* g = a.keep + (row0 + lane) * 2 * fp + col;
+            auto load = [](uint32_t (&w)[8], const int8_t* p) {
+              asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]),
+                           "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+            };
+            load(kg, g); load(ku, g + fp);
+            const float* st8 = a.keep_scale + ((size_t)x.e * 2 * blocks + col / kKeepBlock) * a.C + y0 + lane;
+            sg = __ldg(st8); su = __ldg(st8 + (size_t)blocks * a.C);
+          }
+          __syncwarp();
+        };
+        if constexpr (EPI == kEpiDact) { if constexpr (Form == kKeep8) fetch8(col0); else fetch(row0, rows, col0); }
         if (nkb > 0) {
           ok = mbar_wait_bounded(&sm.acc_full[buf], (acc_ph >> buf) & 1);
           if (!ok) break;
@@ -514,13 +557,16 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
             tmem_ld_wait();
             unsigned char* to = next_box();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) put16(to, i, u[i], keep_row);
+            for (int i = 0; i < 4; ++i) {
+              if constexpr (Form == kInt8) unscale(u[i], col0 + c0 + 16 * i, a.w_scale + (size_t)x.e * a.N);
+              put16(to, i, u[i], keep_row);
+            }
             box_store(&tO0, col0 + c0, y0, x.e, rows > 0 && col0 + c0 < a.N);
           }
         } else if constexpr (EPI == kEpiGlu) {
           // h, then g and u if they are kept: the accumulator is read again for each rather than held in registers
 #pragma unroll 1
-          for (int what = 0; what < (pre_out ? 3 : 1); ++what) {
+          for (int what = 0; what < (Form == kBf16 && pre_out ? 3 : 1); ++what) {
             unsigned char* to = next_box();
 #pragma unroll 1
             for (int i = 0; i < 4; ++i) {
@@ -528,6 +574,10 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
               tmem_ld16_issue(acc + 16 * i + (what == 2 ? 128 : 0), g);
               if (what == 0) tmem_ld16_issue(acc + 128 + 16 * i, u);
               tmem_ld_wait();
+              if constexpr (Form == kInt8) {
+                const float* of = a.w_scale + (size_t)x.e * 2 * a.N;
+                unscale(g, col0 + 16 * i, of); unscale(u, col0 + 16 * i, of + a.N);
+              }
               if (what == 0) {
 #pragma unroll
                 for (int j = 0; j < 16; ++j) g[j] = __float_as_uint(silu_mul<true>(__uint_as_float(g[j]), __uint_as_float(u[j])));
@@ -536,7 +586,76 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
             }
             box_store(what == 0 ? &tO0 : what == 1 ? &tO1 : &tO2, col0, y0, x.e, rows > 0 && col0 < a.N);
           }
+          if constexpr (Form == kKeep8) {
+            // A lane's 32 columns of its row are a block: 32 bytes, a sector of memory, and the lanes' scales a line.  Columns behind d_ff are
+            // zero in the accumulator (the copies filled the weights up), rows behind the load are left out.
+            const int fp = keep_width(a.N), blocks = fp / kKeepBlock;
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+              const int half = i >> 1, col = col0 + (i & 1) * kKeepBlock;
+              uint32_t u[2][16], m = 0;
+              tmem_ld16_issue(acc + half * 128 + (i & 1) * kKeepBlock, u[0]);
+              tmem_ld16_issue(acc + half * 128 + (i & 1) * kKeepBlock + 16, u[1]);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 32; ++j) m = max(m, abs_bits(u[j >> 4][j & 15]));
+              if (keep_row && col < a.N) {
+                const Step8 st8 = step8(m);
+                uint32_t w[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                  const uint32_t(&v)[16] = u[j >> 2];
+                  const int k = (j & 3) * 4;
+                  w[j] = pack8(round8(__uint_as_float(v[k]), st8.inv), round8(__uint_as_float(v[k + 1]), st8.inv),
+                               round8(__uint_as_float(v[k + 2]), st8.inv), round8(__uint_as_float(v[k + 3]), st8.inv));
+                  if (!(st8.inv > 0.f)) w[j] = 0;
+                }
+                int8_t* to = a.keep + ((row0 + lane) * 2 + half) * fp + col;
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                             "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+                a.keep_scale[((size_t)x.e * 2 * blocks + half * blocks + col / kKeepBlock) * a.C + y0 + lane] = st8.scale;
+              }
+              __syncwarp();
+            }
+          }
         } else {
+          if constexpr (Form == kKeep8) {
+            // as below, with g and u from their integers; h = silu(g) u is formed again on the way, and leaves through the first box
+            // once dg has left it
+#pragma unroll 1
+            for (int c0 = 0; c0 < kCols; c0 += 32) {
+              if (c0) fetch8(col0 + c0);
+              uint32_t h[16];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                uint32_t u[8];
+                tmem_ld8(acc + c0 + 8 * i, u);
+                float dg[8], du[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                  const int w = 2 * i + (j >> 2);
+                  const float g = byte8(kg[w] ^ 0x80808080u, j & 3) * sg, up = byte8(ku[w] ^ 0x80808080u, j & 3) * su;
+                  const float s = sigmoid_f<true>(g), dh = __uint_as_float(u[j]);
+                  dg[j] = keep_row ? dh * up * s * (1.f + g * (1.f - s)) : 0.f;
+                  du[j] = keep_row ? dh * g * s : 0.f;
+                  const float hv = keep_row ? g * s * up : 0.f;
+                  if (j & 1) h[4 * i + (j >> 1)] = pack_bf16(__uint_as_float(h[4 * i + (j >> 1)]), hv);
+                  else h[4 * i + (j >> 1)] = __float_as_uint(hv);
+                }
+                Vec16<__nv_bfloat16>::store(reinterpret_cast<__nv_bfloat16*>(stage + lane * kRow + ((i ^ swz(lane)) << 4)), dg);
+                Vec16<__nv_bfloat16>::store(reinterpret_cast<__nv_bfloat16*>(stage + (32 + lane) * kRow + ((i ^ swz(lane)) << 4)), du);
+              }
+              char* dst = out + (row0 * 2 * a.N + col0 + c0) * 2;
+              const int left = (a.N - col0 - c0) * 2;
+              box_out(stage, dst, (size_t)a.N * 4, rows, left);
+              if (pre_out) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) to_box(stage, i, make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]));
+                box_out(stage, pre_out + (row0 * a.N + col0 + c0) * 2, (size_t)a.N * 2, rows, left);
+              }
+              box_out(stage + 32 * kRow, dst + (size_t)a.N * 2, (size_t)a.N * 4, rows, left);
+            }
+          } else {
           // dh in the accumulator; g and u sit in a pair of boxes, which dg and du then leave from
 #pragma unroll 1
           for (int c0 = 0; c0 < kCols; c0 += 32) {
@@ -565,6 +684,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
             box_out(stage, dst, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 2);
             box_out(stage + 32 * kRow, dst + (size_t)a.N * 2, (size_t)a.N * 4, rows, (a.N - col0 - c0) * 2);
           }
+          }
         }
         if (nkb > 0) {
           tc_fence_before();
@@ -575,7 +695,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       }
       if (!kParts && nkb > 0) ++turn;
     }
-    if (EPI == kEpiDact) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (EPI == kEpiDact && Form != kKeep8) asm volatile("cp.async.wait_group 0;" ::: "memory");
     if (lane == 0) bulk_wait_all<0>();
     if (!ok && lane == 0) sm.failed = 1;
   }
