@@ -36,6 +36,7 @@ __device__ __forceinline__ bool all_epilogue_threads(bool x) {
 }
 
 // W_MN: the weights' columns are contiguous.  tW0 / tW1: weights (gated: gate / up columns); tX: the rows.
+// out, pre_out: y; h and [g | u] kept or null; dpre and h or null (backward of kKeep8).
 template <int EPI, bool W_MN, int Form = kBf16>
 __global__ void __launch_bounds__(kFewThreads)
 expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant__ CUtensorMap tW1, const __grid_constant__ CUtensorMap tX,
@@ -132,7 +133,8 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
     const int q = warp & 3;                             // TMEM lanes this warp may read
     {
       const int w = blockIdx.x * 4 + warp - 2, ws = gridDim.x * 4;
-      expert_zero_behind_rows(a, sm.rows, (char*)out, 2 * (size_t)a.N, w, ws);
+      expert_zero_behind_rows(a, sm.rows, (char*)out, (EPI == kEpiDact ? 4 : 2) * (size_t)a.N, w, ws);
+      if (EPI == kEpiDact && pre_out) expert_zero_behind_rows(a, sm.rows, (char*)pre_out, 2 * (size_t)a.N, w, ws);
       if (EPI == kEpiGlu && pre_out) expert_zero_behind_rows(a, sm.rows, (char*)pre_out, 4 * (size_t)a.N, w, ws);
     }
     int turn = 0, e = 0; bool ok = true;
@@ -142,6 +144,21 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
       const int col = (t - sm.first[e]) * kCols + (EPI == kEpiGlu ? (q & 1) * 32 : q * 32) + lane;
       const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * pad);
       const size_t row0 = (size_t)e * a.C;
+      // backward from kept activations: 16 rows of this column's g and u, and lane j's step of g (lanes 16 on: of u) of row j
+      int8_t kg[16], ku[16];
+      float steps = 0.f;
+      auto fetch = [&](int c0) {
+        const int fp = keep_width(a.N), blocks = fp / kKeepBlock, r = c0 + (lane & 15);
+        if (col - lane >= a.N) return;                                 // the whole warp: fp reaches to the end of a block
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int8_t* p = a.keep + (row0 + c0 + j) * 2 * fp + col;
+          kg[j] = c0 + j < rows ? __ldg(p) : (int8_t)0;
+          ku[j] = c0 + j < rows ? __ldg(p + fp) : (int8_t)0;
+        }
+        if (r < rows) steps = __ldg(a.keep_scale + ((size_t)e * 2 * blocks + (lane >> 4) * blocks + col / kKeepBlock) * a.C + r);
+      };
+      if constexpr (EPI == kEpiDact) fetch(0);
       ok = mbar_wait_bounded(&sm.acc_full[buf], (uint32_t)((turn >> 1) & 1));
       if (EPI == kEpiGlu) ok = all_epilogue_threads(ok);   // (also: the last item's values have been read from `up`)
       if (!ok) break;
@@ -169,7 +186,24 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
           if (lane == 0) a.keep_scale[((size_t)e * 2 * blocks + half * blocks + first / kKeepBlock) * a.C + c0 + j] = st8.scale;
         }
       };
-      if constexpr (EPI == kEpiPlain) {
+      if constexpr (EPI == kEpiDact) {
+        for (int c0 = 0; c0 < rows; c0 += 16) {
+          float r[16];
+          if (c0) fetch(c0);
+          take(c0, r);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const float g = (float)kg[j] * __shfl_sync(0xffffffffu, steps, j), u = (float)ku[j] * __shfl_sync(0xffffffffu, steps, 16 + j);
+            const float s = sigmoid_f<true>(g);
+            if (col < a.N && c0 + j < rows) {
+              __nv_bfloat16* o = out + (row0 + c0 + j) * 2 * a.N + col;
+              o[0] = __float2bfloat16(r[j] * u * s * (1.f + g * (1.f - s)));
+              o[a.N] = __float2bfloat16(r[j] * g * s);
+              if (pre_out) pre_out[(row0 + c0 + j) * a.N + col] = __float2bfloat16(g * s * u);
+            }
+          }
+        }
+      } else if constexpr (EPI == kEpiPlain) {
         for (int c0 = 0; c0 < rows; c0 += 16) {
           float r[16];
           take(c0, r);

@@ -1,6 +1,7 @@
 // Checks and launches of the tensor-core expert products that the C entry points share: maps of the operands, choice of the tile.
 #pragma once
 #include <algorithm>
+#include <stdlib.h>
 
 #include "common.cuh"
 #include "context.cuh"
@@ -73,13 +74,14 @@ maxscore_status launch_tc(maxscore_ctx* c, const void* A, const void* B, const v
       else MS_MAP(&tB1, (const char*)B + N * K * elem, K, N, K, cols * K, 128, false, elem);
     }
     if (EPI != kEpiDact) MS_MAP(&tO0, out, N, C, N, C * N, 32);
+    else if (Form == kKeep8 && pre_out) MS_MAP(&tO0, pre_out, N, C, N, C * N, 32);
     if (EPI == kEpiGlu && Form == kBf16 && pre_out) {
       MS_MAP(&tO1, pre_out, N, C, 2 * N, C * 2 * N, 32);
       MS_MAP(&tO2, (P)pre_out + N, N, C, 2 * N, C * 2 * N, 32);
     }
   }
 #undef MS_MAP
-  if (kDw || EPI == kEpiDact) tO0 = tA;                  // not used
+  if (kDw || (EPI == kEpiDact && (Form != kKeep8 || !pre_out))) tO0 = tA;      // not used
   if (EPI != kEpiGlu || Form != kBf16 || !pre_out) tO1 = tO2 = tO0;       // not used
   const long long tile_n = EPI == kEpiGlu ? 128 : kXTile;
   const long long tiles = (long long)a.E * (((kDw ? M : C) + kXTile - 1) / kXTile) * ((N + tile_n - 1) / tile_n);
@@ -98,7 +100,7 @@ maxscore_status launch_tc(maxscore_ctx* c, const void* A, const void* B, const v
     else go(expert_tc_kernel<EPI, B_MN, 1>, 1);
   }
   else if constexpr (EPI == kEpiDact) go(expert_tc_kernel<EPI, B_MN, 1, false, Form>, 1);
-  else if (a.K * elem >= 8192 && tiles >= 4 * pairs) go(expert_tc_kernel<EPI, B_MN, 2, false, Form>, 2);
+  else if (getenv("XW") ? getenv("XW")[0] == '2' : a.K * elem >= 8192 && tiles >= 4 * pairs) go(expert_tc_kernel<EPI, B_MN, 2, false, Form>, 2);
   else go(expert_tc_kernel<EPI, B_MN, 1, false, Form>, 1);
   if (s) return s;
   MS_LAUNCH_CHECK("expert_tc_kernel");
@@ -114,7 +116,7 @@ maxscore_status launch_few(maxscore_ctx* c, const void* x, const void* w, void* 
   typedef const __nv_bfloat16* P;
   CUtensorMap tW0, tW1, tX;
   maxscore_status s;
-  a.b_chunks = EPI == kEpiPlain && B_MN && N % 64 == 0;
+  a.b_chunks = EPI != kEpiGlu && B_MN && N % 64 == 0;
   s = make_tmap_expert(c, &tX, x, K, C, K, C * K, (uint32_t)pad, false, elem);
   if (s) return s;
   const uint32_t box = B_MN || EPI == kEpiGlu ? 64 : 128;

@@ -593,14 +593,15 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
 #pragma unroll 1
             for (int i = 0; i < 4; ++i) {
               const int half = i >> 1, col = col0 + (i & 1) * kKeepBlock;
-              uint32_t u[2][16], m = 0;
+              uint32_t u[2][16];
+              float m = 0.f;
               tmem_ld16_issue(acc + half * 128 + (i & 1) * kKeepBlock, u[0]);
               tmem_ld16_issue(acc + half * 128 + (i & 1) * kKeepBlock + 16, u[1]);
               tmem_ld_wait();
 #pragma unroll
-              for (int j = 0; j < 32; ++j) m = max(m, abs_bits(u[j >> 4][j & 15]));
+              for (int j = 0; j < 16; ++j) m = max_abs(m, __uint_as_float(u[0][j]), __uint_as_float(u[1][j]));
               if (keep_row && col < a.N) {
-                const Step8 st8 = step8(m);
+                const Step8 st8 = step8(__float_as_uint(m));
                 uint32_t w[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -620,12 +621,12 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
           }
         } else {
           if constexpr (Form == kKeep8) {
-            // as below, with g and u from their integers; h = silu(g) u is formed again on the way, and leaves through the first box
-            // once dg has left it
-#pragma unroll 1
+            // As below, with g and u from their integers.  h = silu(g) u is formed again on the way and leaves through a tile store of 64
+            // columns once dg and du have left the boxes.
+            uint32_t h[32];
+#pragma unroll
             for (int c0 = 0; c0 < kCols; c0 += 32) {
-              if (c0) fetch8(col0 + c0);
-              uint32_t h[16];
+              if (c0 == 0) { if (lane == 0) bulk_wait_read<0>(); __syncwarp(); }      // the boxes are free of the last tile's h
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 uint32_t u[8];
@@ -639,21 +640,28 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
                   dg[j] = keep_row ? dh * up * s * (1.f + g * (1.f - s)) : 0.f;
                   du[j] = keep_row ? dh * g * s : 0.f;
                   const float hv = keep_row ? g * s * up : 0.f;
-                  if (j & 1) h[4 * i + (j >> 1)] = pack_bf16(__uint_as_float(h[4 * i + (j >> 1)]), hv);
-                  else h[4 * i + (j >> 1)] = __float_as_uint(hv);
+                  uint32_t& hw = h[c0 / 2 + 4 * i + (j >> 1)];
+                  hw = j & 1 ? pack_bf16(__uint_as_float(hw), hv) : __float_as_uint(hv);
                 }
                 Vec16<__nv_bfloat16>::store(reinterpret_cast<__nv_bfloat16*>(stage + lane * kRow + ((i ^ swz(lane)) << 4)), dg);
                 Vec16<__nv_bfloat16>::store(reinterpret_cast<__nv_bfloat16*>(stage + (32 + lane) * kRow + ((i ^ swz(lane)) << 4)), du);
               }
+              if (c0 + 32 < kCols) fetch8(col0 + c0 + 32);             // on its way while the results leave
               char* dst = out + (row0 * 2 * a.N + col0 + c0) * 2;
               const int left = (a.N - col0 - c0) * 2;
               box_out(stage, dst, (size_t)a.N * 4, rows, left);
-              if (pre_out) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) to_box(stage, i, make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]));
-                box_out(stage, pre_out + (row0 * a.N + col0 + c0) * 2, (size_t)a.N * 2, rows, left);
-              }
               box_out(stage + 32 * kRow, dst + (size_t)a.N * 2, (size_t)a.N * 4, rows, left);
+            }
+            if (pre_out) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                *reinterpret_cast<uint4*>(stage + lane * 128 + ((i ^ (lane & 7)) << 4)) = make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
+              fence_proxy_async();
+              __syncwarp();
+              if (lane == 0) {
+                if (rows > 0 && col0 < a.N) tma_store_3d(&tO0, col0, y0, x.e, smem_u32(stage));
+                bulk_commit();
+              }
             }
           } else {
           // dh in the accumulator; g and u sit in a pair of boxes, which dg and du then leave from

@@ -171,8 +171,10 @@ maxscore_status maxscore_expert_glu_bwd_keep8(maxscore_ctx* c, const void* dy, c
              {rows_span(c, dy, d_out), weight_span(c, w_down, d_ff, d_out, 2), {keep, keep_bytes(c, d_ff)}, load_span(c, expert_load)}))
     return MAXSCORE_ERR_INVALID_ARG;
   const ExpertArgs a = keep_args(c, expert_load, d_ff, d_out, const_cast<void*>(keep));
-  return w_layout == 1 ? launch_tc<kEpiDact, true, kKeep8>(c, dy, w_down, nullptr, dpre, h, a, (cudaStream_t)stream)
-                       : launch_tc<kEpiDact, false, kKeep8>(c, dy, w_down, nullptr, dpre, h, a, (cudaStream_t)stream);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (c->C <= kFewRows) return w_layout == 1 ? launch_few<kEpiDact, true, kKeep8>(c, dy, w_down, dpre, h, a, st) : launch_few<kEpiDact, false, kKeep8>(c, dy, w_down, dpre, h, a, st);
+  return w_layout == 1 ? launch_tc<kEpiDact, true, kKeep8>(c, dy, w_down, nullptr, dpre, h, a, st)
+                       : launch_tc<kEpiDact, false, kKeep8>(c, dy, w_down, nullptr, dpre, h, a, st);
 }
 
 }  // extern "C"

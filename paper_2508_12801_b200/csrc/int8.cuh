@@ -25,6 +25,11 @@ __device__ __forceinline__ uint32_t pack8(uint32_t a, uint32_t b, uint32_t c, ui
   return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
 __device__ __forceinline__ uint32_t abs_bits(uint32_t u) { return u & 0x7fffffffu; }
+// the larger of m and the magnitudes of a and b; NaN wins
+__device__ __forceinline__ float max_abs(float m, float a, float b) {
+  asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(fabsf(a)), "f"(fabsf(b)));
+  return m;
+}
 // integer i of a word of four as a float: exact
 __device__ __forceinline__ float byte8(uint32_t w_flipped, int i) {                   // w ^ 0x80808080
   return __uint_as_float(__byte_perm(w_flipped, 0x4b000000u, 0x7440 + i)) - 8388736.f;
