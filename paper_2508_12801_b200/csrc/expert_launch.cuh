@@ -1,7 +1,6 @@
 // Checks and launches of the tensor-core expert products that the C entry points share: maps of the operands, choice of the tile.
 #pragma once
 #include <algorithm>
-#include <stdlib.h>
 
 #include "common.cuh"
 #include "context.cuh"
@@ -93,14 +92,15 @@ maxscore_status launch_tc(maxscore_ctx* c, const void* A, const void* B, const v
   // Two column tiles at a time read a quarter less per flop, but their epilogues hide less well.  Long runs, 256 x 512 against
   // 256 x 256: y at C 4096, K 4096 1 248 / 1 234 TFLOP/s, at C 1024, K 2048 1 150 / 1 145, K 1024 1 041 / 1 055, K 512 853 / 904;
   // h 1 286 / 1 257 at K 4096, 1 125 / 1 178 at K 2048.  dW takes them where one accumulator holds its sum (E 64, C 128, 2048 x 1024:
-  // 112 us / 136 us); the backward of the activation loses at every size (1 022 / 1 058 at K 4096, 561 / 705 at 1024).
+  // 112 us / 136 us).  Integers, twice as fast on the same slices, never gain (TOPS, h: 2 612 / 2 812 at K 4096, 2 071 / 2 622 at 2048; y: 1 912 / 2 154
+  // at K 1024).  The backward of the activation loses at every size (1 022 / 1 058 at K 4096, 561 / 705 at 1024).
   if constexpr (kDw) {
     if (a.C <= kXPartRows) { if (a.accumulate) go(expert_tc_kernel<EPI, B_MN, 2, true>, 2); else go(expert_tc_kernel<EPI, B_MN, 2>, 2); }
     else if (a.accumulate) go(expert_tc_kernel<EPI, B_MN, 1, true>, 1);
     else go(expert_tc_kernel<EPI, B_MN, 1>, 1);
   }
-  else if constexpr (EPI == kEpiDact) go(expert_tc_kernel<EPI, B_MN, 1, false, Form>, 1);
-  else if (getenv("XW") ? getenv("XW")[0] == '2' : a.K * elem >= 8192 && tiles >= 4 * pairs) go(expert_tc_kernel<EPI, B_MN, 2, false, Form>, 2);
+  else if constexpr (EPI == kEpiDact || Form == kInt8) go(expert_tc_kernel<EPI, B_MN, 1, false, Form>, 1);
+  else if (a.K >= 4096 && tiles >= 4 * pairs) go(expert_tc_kernel<EPI, B_MN, 2, false, Form>, 2);
   else go(expert_tc_kernel<EPI, B_MN, 1, false, Form>, 1);
   if (s) return s;
   MS_LAUNCH_CHECK("expert_tc_kernel");
