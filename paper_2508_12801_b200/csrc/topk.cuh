@@ -8,10 +8,11 @@
 // l, which fp32 compares exactly.  With one (and for sums of two scores) a row whose last accepted and first refused value lie closer
 // than fp32 can tell apart is chosen again in 64 bits, by the whole warp; about one row in 2 000 of 128 experts.
 //
-// A warp owns a token, a lane VPT consecutive experts (so the lowest lane holds the lowest index and a ballot settles ties).  The k
-// largest come out one by one: a warp-wide maximum of order-preserving integers, a ballot, and the owner takes the next of its own.
-// The row is read once and what is written is k pairs (and the scores, if they are wanted); next to 4 E bytes of logits the
-// instructions count (see the figures at the launch).
+// Two forms.  In the usual one eight lanes own a token and a warp four: next to 4 E bytes of logits the instructions count, and what a
+// token needs once (sums, maxima, the k rounds) costs a quarter of what it does with a warp per token.  Each lane sorts the values of
+// its consecutive experts, keeps the eight largest, and in k rounds the largest heads leave.  Groups that are not whole lanes, a power of two of them, take the
+// other form, a warp per token with the groups' values in shared memory.
+// T 65536, E 128, k 8: see the figures at the launch.
 #pragma once
 #include "common.cuh"
 
@@ -22,7 +23,8 @@ constexpr float kTopkEps = 1e-20f;     // in the denominator of the weights: a r
 
 struct TopkArgs {
   int T, E, k;
-  int n_group, topk_group, group_size, group_lanes;      // group_lanes: lanes of a group where that is a power of two, else 0
+  int n_group, topk_group, group_size;
+  int group_shift;       // eight lanes a token: a group has 1 << group_shift of them
   int sigmoid, pairs, renorm;
   float scale;
 };
@@ -189,10 +191,10 @@ __device__ __noinline__ uint32_t topk_choose_equal(const uint32_t* key, int k) {
   return chosen;
 }
 
-// Groups: 0 none; 1 of `group_lanes` lanes each, a power of two; 2 of any size.
-template <int VPT, int Groups, bool Full>
+// A warp per token, groups of any size.
+template <int VPT, bool Full>
 __global__ void __launch_bounds__(kTopkWarps * 32)
-topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias, float* __restrict__ scores, int32_t* __restrict__ expert_idx,
+topk_fwd_scan_kernel(const float* __restrict__ logits, const float* __restrict__ bias, float* __restrict__ scores, int32_t* __restrict__ expert_idx,
                 float* __restrict__ gate_w, TopkArgs a) {
   __shared__ __align__(16) double scratch[kTopkWarps][kMaxE];          // 64-bit values of a row; its fp32 values, group by group, before
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e0 = lane * VPT;
@@ -203,11 +205,9 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
     b[j] = bias && e0 + j < a.E ? __ldg(bias + e0 + j) : 0.f;
-    group[j] = Groups == 2 ? min((e0 + j) / a.group_size, kTopkMaxGroups - 1) : 0;
+    group[j] = min((e0 + j) / a.group_size, kTopkMaxGroups - 1);
   }
-  const int group_stride = Groups == 1 ? a.group_lanes : 1;            // lanes that speak for the groups: g * group_stride
-  const int my_group = lane / group_stride;
-  const bool speaks = my_group < a.n_group;
+  const bool speaks = lane < a.n_group;                                // a lane per group
   const int64_t step = gridDim.x * kTopkWarps;
   int64_t t = blockIdx.x * kTopkWarps + warp;
   float next[VPT];
@@ -227,57 +227,34 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
       key[j] = Full || e0 + j < a.E ? order_key(c[j]) : 0u;
     }
     bool near = false;                                                 // the same in all lanes
-    if (Groups) {
+    {
       // the two largest of each group (NaN counts as nothing)
       if (!bias && a.pairs) {
 #pragma unroll
         for (int j = 0; j < VPT; ++j) c[j] = s[j];
       }
       float m1 = -INFINITY, m2 = -INFINITY;
-      auto take = [&](float x) { m2 = fmaxf(m2, fminf(m1, x)); m1 = fmaxf(m1, x); };
-      if (Groups == 1) {
 #pragma unroll
-        for (int j = 0; j < VPT; ++j) if (Full || e0 + j < a.E) take(c[j]);
-        for (int o = 1; o < a.group_lanes; o <<= 1) {
-          const float o1 = __shfl_xor_sync(0xffffffffu, m1, o), o2 = __shfl_xor_sync(0xffffffffu, m2, o);
-          m2 = fmaxf(fminf(m1, o1), fmaxf(m2, o2));
-          m1 = fmaxf(m1, o1);
+      for (int j = 0; j < VPT; ++j) if (Full || e0 + j < a.E) grouped[e0 + j + group[j]] = c[j];
+      __syncwarp();
+      if (speaks)
+        for (int i = 0; i < a.group_size; ++i) {
+          const float x = grouped[lane * (a.group_size + 1) + i];
+          m2 = fmaxf(m2, fminf(m1, x)); m1 = fmaxf(m1, x);
         }
-      } else {
-#pragma unroll
-        for (int j = 0; j < VPT; ++j) if (Full || e0 + j < a.E) grouped[e0 + j + group[j]] = c[j];
-        __syncwarp();
-        if (lane < a.n_group)
-          for (int i = 0; i < a.group_size; ++i) take(grouped[lane * (a.group_size + 1) + i]);
-        __syncwarp();
-      }
+      __syncwarp();
       const uint32_t mine = speaks ? order_key(a.pairs && a.group_size > 1 ? m1 + m2 : m1) : 0u;
-      // the best leave one by one; where equal ones left together, every group counts those before it instead
-      uint32_t head = mine, worst = 0;
-#pragma unroll 1
-      for (int g = 0; g < a.topk_group; ++g) {
-        worst = __reduce_max_sync(0xffffffffu, head);
-        head = head == worst ? 0u : head;
-      }
-      bool in = speaks && mine >= worst;
-      if (__popc(__ballot_sync(0xffffffffu, in)) != a.topk_group * group_stride) {
-        int before = 0;
-        for (int g = 0; g < a.n_group; ++g) before += __shfl_sync(0xffffffffu, mine, g * group_stride) >= mine + (g >= my_group);
-        in = speaks && before < a.topk_group;
-      }
+      int before = 0;
+      for (int g = 0; g < a.n_group; ++g) before += __shfl_sync(0xffffffffu, mine, g) >= mine + (g >= lane);
+      const bool in = speaks && before < a.topk_group;
       if (bias || a.pairs) {
         const float low = order_value(__reduce_min_sync(0xffffffffu, in ? mine : 0xffffffffu));
         const float high = order_value(__reduce_max_sync(0xffffffffu, in ? 0u : mine));
         near = !(low - high > 0x1p-18f + 0x1p-21f * fabsf(low));       // two terms, hence twice the bound below
       }
-      if (Groups == 1) {
+      const uint32_t kept = __ballot_sync(0xffffffffu, in);
 #pragma unroll
-        for (int j = 0; j < VPT; ++j) key[j] = in ? key[j] : 0u;
-      } else {
-        const uint32_t kept = __ballot_sync(0xffffffffu, in);
-#pragma unroll
-        for (int j = 0; j < VPT; ++j) if (!(kept >> group[j] & 1)) key[j] = 0u;
-      }
+      for (int j = 0; j < VPT; ++j) if (!(kept >> group[j] & 1)) key[j] = 0u;
     }
     // The k-th largest value: lanes keep their own sorted, the largest heads leave.
     uint32_t q[VPT];
@@ -342,6 +319,224 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
         w[place] = s[j] * f;
         ++place;
       }
+  }
+}
+
+// ---- eight lanes a token ---------------------------------------------------------------------------------------------------
+__device__ __forceinline__ float seg_max(float v) {
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+__device__ __forceinline__ uint32_t seg_max(uint32_t v) {
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ T seg_sum(T v) {
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ int seg_before(int v, int lane8) {          // sum over the lower lanes of the token
+  int incl = v;
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, incl, o, 8);
+    if (lane8 >= o) incl += x;
+  }
+  return incl - v;
+}
+__device__ __forceinline__ void descend(uint32_t& a, uint32_t& b) { const uint32_t hi = max(a, b); b = min(a, b); a = hi; }
+// q[At .. At + N) in descending order
+template <int N, int At, int M>
+__device__ __forceinline__ void sort_keys(uint32_t (&q)[M]) {
+  auto ce = [&](int i, int j) { descend(q[At + i], q[At + j]); };
+  if constexpr (N == 2) ce(0, 1);
+  else if constexpr (N == 4) { ce(0, 1); ce(2, 3); ce(0, 2); ce(1, 3); ce(1, 2); }
+  else {
+    static_assert(N == 8, "2, 4 or 8");
+    ce(0, 1); ce(2, 3); ce(4, 5); ce(6, 7); ce(0, 2); ce(1, 3); ce(4, 6); ce(5, 7); ce(1, 2); ce(5, 6); ce(0, 4); ce(3, 7); ce(1, 5); ce(2, 6);
+    ce(1, 4); ce(3, 6); ce(2, 4); ce(3, 5); ce(3, 4);
+  }
+}
+
+// V: experts of a lane.  Groups: whether there are any, of whole lanes.  Full: E = 8 V.
+template <int V, bool Groups, bool Full>
+__global__ void __launch_bounds__(kTopkWarps * 32)
+topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias, float* __restrict__ scores, int32_t* __restrict__ expert_idx,
+                float* __restrict__ gate_w, TopkArgs a) {
+  constexpr int Q = V < kMaxK ? V : kMaxK;                             // at most k of a lane's experts are chosen
+  __shared__ double scratch[kTopkWarps][kMaxE];                        // values of a row that is chosen in 64 bits
+  __shared__ uint32_t marks[kTopkWarps][4];                            // and its experts
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, lane8 = lane & 7, e0 = lane8 * V;
+  const uint32_t seg = 0xffu << (lane & 24);
+  const int my_group = lane8 >> a.group_shift;
+  const bool speaks = my_group < a.n_group;
+  auto there = [&](int j) { return Full || e0 + j < a.E; };
+  const int64_t step = (int64_t)gridDim.x * kTopkWarps * 4;
+  for (int64_t t0 = ((int64_t)blockIdx.x * kTopkWarps + warp) * 4; t0 < a.T; t0 += step) {
+    const int64_t t = min(t0 + (lane >> 3), (int64_t)a.T - 1);         // behind the last token: computed again, not written
+    const bool valid = t0 + (lane >> 3) < a.T;
+    const float* row = logits + t * a.E + e0;
+    float s[V];
+    uint32_t key[V];
+    auto load = [&](float (&x)[V], const float* p) {
+      if constexpr (Full && V % 4 == 0) {
+#pragma unroll
+        for (int j = 0; j < V; j += 4) {
+          const float4 v = __ldg(reinterpret_cast<const float4*>(p + j));
+          x[j] = v.x; x[j + 1] = v.y; x[j + 2] = v.z; x[j + 3] = v.w;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = there(j) ? __ldg(p + j) : 0.f;
+      }
+    };
+    float l[V];
+    load(l, row);
+    if (a.sigmoid) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) { float rest; sigmoid_pair(l[j], s[j], rest); }
+    } else {
+      float m = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < V; ++j) if (there(j)) m = fmaxf(m, l[j]);
+      m = seg_max(m);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        s[j] = there(j) ? exp_down(l[j] - m) : 0.f;                    // NaN where l is, and in rows whose largest is infinite
+        sum += s[j];
+      }
+      const float inv = 1.f / seg_sum(sum);
+#pragma unroll
+      for (int j = 0; j < V; ++j) s[j] *= inv;
+    }
+    if (scores && valid) {
+      float* to = scores + t * a.E + e0;
+      if constexpr (Full && V % 4 == 0) {
+#pragma unroll
+        for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(to + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) if (there(j)) to[j] = s[j];
+      }
+    }
+    if (bias) {
+      float b[V];
+      load(b, bias + e0);
+#pragma unroll
+      for (int j = 0; j < V; ++j) l[j] = s[j] + b[j];
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) key[j] = there(j) ? order_key(l[j]) : 0u;
+    bool near = false;                                                 // the same in a token's lanes
+    if constexpr (Groups) {
+      // the two largest of each group (NaN counts as nothing)
+      float m1 = -INFINITY, m2 = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (there(j)) {
+          const float x = !bias && a.pairs ? s[j] : l[j];
+          m2 = fmaxf(m2, fminf(m1, x)); m1 = fmaxf(m1, x);
+        }
+      for (int o = 1; o < 1 << a.group_shift; o <<= 1) {
+        const float o1 = __shfl_xor_sync(0xffffffffu, m1, o), o2 = __shfl_xor_sync(0xffffffffu, m2, o);
+        m2 = fmaxf(fminf(m1, o1), fmaxf(m2, o2));
+        m1 = fmaxf(m1, o1);
+      }
+      const uint32_t mine = speaks ? order_key(a.pairs && a.group_size > 1 ? m1 + m2 : m1) : 0u;
+      int before = 0;                                                  // lanes of better groups: of equal ones the lower
+#pragma unroll
+      for (int o = 1; o < 8; ++o) before += __shfl_xor_sync(0xffffffffu, mine, o) >= mine + ((lane8 ^ o) >> a.group_shift >= my_group);
+      const bool in = speaks && before < a.topk_group << a.group_shift;
+      if (bias || a.pairs) {
+        const float low = order_value(~seg_max(in ? ~mine : 0u)), high = order_value(seg_max(in ? 0u : mine));
+        near = !(low - high > 0x1p-18f + 0x1p-21f * fabsf(low));       // two terms, hence twice the bound below
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) key[j] = in ? key[j] : 0u;
+    }
+    // The lane's largest in order, then k rounds (or fewer, where equal ones leave together).
+    uint32_t q[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) q[j] = key[j];
+    if constexpr (V == 16) {
+      sort_keys<8, 0>(q); sort_keys<8, 8>(q);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) q[j] = max(q[j], q[15 - j]);         // the eight largest, rising and falling
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) if (!(j & o)) descend(q[j], q[j + o]);
+    } else sort_keys<V, 0>(q);
+    uint32_t last = 0;                                                 // the k-th largest value
+    int gone = 0;
+#pragma unroll 1
+    for (int i = 0; i < a.k; ++i) {
+      const uint32_t m = seg_max(q[0]);
+      const bool open = gone < a.k, leaves = open && q[0] == m;
+      if (open) last = m;
+      gone += __popc(__ballot_sync(0xffffffffu, leaves) & seg);
+      if (leaves) {
+#pragma unroll
+        for (int j = 0; j + 1 < Q; ++j) q[j] = q[j + 1];
+        q[Q - 1] = 0;
+      }
+    }
+    uint32_t chosen = 0;
+#pragma unroll
+    for (int j = 0; j < V; ++j) chosen |= (uint32_t)(key[j] >= last) << j;               // last is above 0: k experts can be chosen
+    int place = seg_before(__popc(chosen), lane8);
+    const bool equal = __shfl_sync(0xffffffffu, place + __popc(chosen), lane | 7) != a.k;
+    if (bias) {
+      // fp32 errors of s: of the exponent |l - m| 2^-24 e^-|l - m|, of exponential, sum and quotient 2^-21 s at most; of the sum with
+      // the bias 2^-24 of it.  Twice that between two values, rounded up.
+      uint32_t after = 0;
+#pragma unroll
+      for (int j = 0; j < V; ++j) after = max(after, chosen >> j & 1 ? 0u : key[j]);
+      after = seg_max(after);
+      const float low = order_value(last);
+      near = near || equal || (after != 0 && !(low - order_value(after) > 0x1p-19f + 0x1p-22f * fabsf(low)));
+    }
+    if (__any_sync(0xffffffffu, equal || near)) {
+      // equal values at the border: the lowest indices of them stay (a token without any keeps its experts)
+      int above = 0, same = 0;
+#pragma unroll
+      for (int j = 0; j < V; ++j) { above += key[j] > last; same += key[j] == last; }
+      int room = a.k - seg_sum(above) - seg_before(same, lane8);
+#pragma unroll
+      for (int j = 0; j < V; ++j) if (key[j] == last && room-- <= 0) chosen &= ~(1u << j);
+      // rows that fp32 cannot decide, one by one
+      for (uint32_t left = __ballot_sync(0xffffffffu, near && lane8 == 0); left; left &= left - 1) {
+        const int first = __ffs(left) - 1, vpt = (a.E + 31) / 32;
+        const uint32_t bits = topk_choose_64(logits + min(t0 + (first >> 3), (int64_t)a.T - 1) * a.E, bias, a, vpt, scratch[warp]);
+        if (lane < 4) marks[warp][lane] = 0;
+        __syncwarp();
+        for (int j = 0; j < vpt; ++j) if (bits >> j & 1) atomicOr(&marks[warp][(lane * vpt + j) >> 5], 1u << ((lane * vpt + j) & 31));
+        __syncwarp();
+        if ((lane & 24) == first) chosen = marks[warp][e0 >> 5] >> (e0 & 31) & (V == 32 ? 0xffffffffu : (1u << V) - 1u);
+        __syncwarp();
+      }
+      place = seg_before(__popc(chosen), lane8);
+    }
+    float f = a.scale;
+    if (a.renorm) {
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum += chosen >> j & 1 ? s[j] : 0.f;
+      f = a.scale / (seg_sum(sum) + kTopkEps);
+    }
+    // ascending: the chosen of lower lanes, then the lane's own
+    int32_t* idx = expert_idx + t * a.k + place;
+    float* w = gate_w + t * a.k + place;
+    if (valid) {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (chosen >> j & 1) { *idx++ = e0 + j; *w++ = s[j] * f; }
+    }
+    __syncwarp();
   }
 }
 

@@ -34,7 +34,11 @@ maxscore_status topk_args(const maxscore_ctx* c, const maxscore_topk* how, TopkA
   return MAXSCORE_OK;
 }
 
-int topk_grid(const maxscore_ctx* c) { return (int)std::min<int64_t>(((int64_t)c->p.T + kTopkWarps - 1) / kTopkWarps, (int64_t)c->sm_count * 8); }
+// tokens: of a warp
+int topk_grid(const maxscore_ctx* c, int tokens) {
+  const int64_t each = (int64_t)kTopkWarps * tokens;
+  return (int)std::min<int64_t>((c->p.T + each - 1) / each, (int64_t)c->sm_count * 8);
+}
 
 // experts of a lane: rows of up to 32, 64, 96 and 128; rows of 64 and 128 are moved as vectors
 template <typename F>
@@ -62,14 +66,26 @@ maxscore_status maxscore_topk_fwd(maxscore_ctx* c, const float* logits, const fl
   const size_t rows = sizeof(float) * (size_t)a.T * a.E, pairs = sizeof(float) * (size_t)a.T * a.k;
   if (!apart({{scores, rows}, {expert_idx, pairs}, {gate_w, pairs}}, {{logits, rows}, {bias, sizeof(float) * (size_t)a.E}}))
     return MAXSCORE_ERR_INVALID_ARG;
-  topk_by_width(a.E, [&](auto w, auto whole) {
-    constexpr int V = decltype(w)::value;
-    constexpr bool F = decltype(whole)::value;
-    const int lanes = a.group_size / V;
-    a.group_lanes = a.group_size % V == 0 && (lanes & (lanes - 1)) == 0 ? lanes : 0;
-    auto kernel = a.n_group == 1 ? topk_fwd_kernel<V, 0, F> : a.group_lanes ? topk_fwd_kernel<V, 1, F> : topk_fwd_kernel<V, 2, F>;
-    kernel<<<topk_grid(c), kTopkWarps * 32, 0, (cudaStream_t)stream>>>(logits, bias, scores, expert_idx, gate_w, a);
-  });
+  const int v = a.E <= 16 ? 2 : a.E <= 32 ? 4 : a.E <= 64 ? 8 : 16, lanes = a.group_size / v;       // experts of a lane of eight
+  if (a.n_group == 1 || (a.group_size % v == 0 && (lanes & (lanes - 1)) == 0)) {
+    while (a.n_group > 1 && 1 << a.group_shift < lanes) ++a.group_shift;
+    auto go = [&](auto per_lane, auto whole) {
+      constexpr int V = decltype(per_lane)::value;
+      constexpr bool F = decltype(whole)::value;
+      auto kernel = a.n_group == 1 ? topk_fwd_kernel<V, false, F> : topk_fwd_kernel<V, true, F>;
+      kernel<<<topk_grid(c, 4), kTopkWarps * 32, 0, (cudaStream_t)stream>>>(logits, bias, scores, expert_idx, gate_w, a);
+    };
+    auto by = [&](auto per_lane) { if (a.E == 8 * decltype(per_lane)::value) go(per_lane, std::true_type{}); else go(per_lane, std::false_type{}); };
+    if (v == 2) by(std::integral_constant<int, 2>{});
+    else if (v == 4) by(std::integral_constant<int, 4>{});
+    else if (v == 8) by(std::integral_constant<int, 8>{});
+    else by(std::integral_constant<int, 16>{});
+  } else {
+    topk_by_width(a.E, [&](auto w, auto whole) {
+      topk_fwd_scan_kernel<decltype(w)::value, decltype(whole)::value><<<topk_grid(c, 1), kTopkWarps * 32, 0, (cudaStream_t)stream>>>(
+          logits, bias, scores, expert_idx, gate_w, a);
+    });
+  }
   MS_LAUNCH_CHECK("topk_fwd_kernel");
   c->launches += 1;
   return MAXSCORE_OK;
@@ -87,7 +103,7 @@ maxscore_status maxscore_topk_bwd(maxscore_ctx* c, const float* logits, const in
   if (!apart({{dlogits, rows}}, {{logits, rows}, {expert_idx, pairs}, {dgate_w, pairs}, {dscores_col, sizeof(float) * (size_t)a.E}}))
     return MAXSCORE_ERR_INVALID_ARG;
   topk_by_width(a.E, [&](auto w, auto whole) {
-    topk_bwd_kernel<decltype(w)::value, decltype(whole)::value><<<topk_grid(c), kTopkWarps * 32, 0, (cudaStream_t)stream>>>(logits, expert_idx, dgate_w, dscores_col,
+    topk_bwd_kernel<decltype(w)::value, decltype(whole)::value><<<topk_grid(c, 1), kTopkWarps * 32, 0, (cudaStream_t)stream>>>(logits, expert_idx, dgate_w, dscores_col,
                                                                                                       dlogits, a);
   });
   MS_LAUNCH_CHECK("topk_bwd_kernel");
