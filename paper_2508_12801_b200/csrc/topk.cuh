@@ -48,7 +48,10 @@ __device__ __forceinline__ float exp_down(float x) {
 }
 // sigmoid(l) and 1 - sigmoid(l), both to a few steps of their last bit
 __device__ __forceinline__ void sigmoid_pair(float l, float& s, float& rest) {
-  const float t = exp_down(-fabsf(l)), r = __fdividef(1.f, 1.f + t), tr = t * r;
+  const float t = exp_down(-fabsf(l));
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + t));                          // of 1 to 2, to the last bit or so
+  const float tr = t * r;
   s = l < 0.f ? tr : r;
   rest = l < 0.f ? r : tr;
 }
@@ -370,32 +373,40 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
   constexpr int Q = V < kMaxK ? V : kMaxK;                             // at most k of a lane's experts are chosen
   __shared__ double scratch[kTopkWarps][kMaxE];                        // values of a row that is chosen in 64 bits
   __shared__ uint32_t marks[kTopkWarps][4];                            // and its experts
+  constexpr int kPad = V >= 8 ? 4 : 0;                                 // between lanes' parts, so that 16-byte stores do not meet in a bank
+  __shared__ __align__(16) float held[kTopkWarps][4][8 * (V + kPad)];  // s of the warp's four tokens
+  __shared__ __align__(16) float held_bias[8 * (V + kPad)];            // laid out as they are
+  __shared__ int picks[kTopkWarps][4][kMaxK];                          // the chosen of each, ascending
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, lane8 = lane & 7, e0 = lane8 * V;
   const uint32_t seg = 0xffu << (lane & 24);
   const int my_group = lane8 >> a.group_shift;
   const bool speaks = my_group < a.n_group;
   auto there = [&](int j) { return Full || e0 + j < a.E; };
-  const int64_t step = (int64_t)gridDim.x * kTopkWarps * 4;
-  for (int64_t t0 = ((int64_t)blockIdx.x * kTopkWarps + warp) * 4; t0 < a.T; t0 += step) {
-    const int64_t t = min(t0 + (lane >> 3), (int64_t)a.T - 1);         // behind the last token: computed again, not written
+  float* mine_s = held[warp][lane >> 3];
+  int* mine_e = picks[warp][lane >> 3];
+  auto load = [&](float (&x)[V], const float* p) {
+    if constexpr (Full && V % 4 == 0) {
+#pragma unroll
+      for (int j = 0; j < V; j += 4) {
+        const float4 v = __ldg(reinterpret_cast<const float4*>(p + j));
+        x[j] = v.x; x[j + 1] = v.y; x[j + 2] = v.z; x[j + 3] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) x[j] = there(j) ? __ldg(p + j) : 0.f;
+    }
+  };
+  for (int e = threadIdx.x; e < 8 * V; e += kTopkWarps * 32) held_bias[e + e / V * kPad] = bias && e < a.E ? __ldg(bias + e) : 0.f;
+  __syncthreads();
+  const int64_t step = (int64_t)gridDim.x * kTopkWarps * 4, end = (int64_t)a.T - 1;
+  float l[V];                                                          // a row; then the next one, on its way during the rounds
+  int64_t t0 = ((int64_t)blockIdx.x * kTopkWarps + warp) * 4;
+  if (t0 < a.T) load(l, logits + min(t0 + (lane >> 3), end) * a.E + e0);
+  for (; t0 < a.T; t0 += step) {
+    const int64_t t = min(t0 + (lane >> 3), end);                      // behind the last token: computed again, not written
     const bool valid = t0 + (lane >> 3) < a.T;
-    const float* row = logits + t * a.E + e0;
     float s[V];
     uint32_t key[V];
-    auto load = [&](float (&x)[V], const float* p) {
-      if constexpr (Full && V % 4 == 0) {
-#pragma unroll
-        for (int j = 0; j < V; j += 4) {
-          const float4 v = __ldg(reinterpret_cast<const float4*>(p + j));
-          x[j] = v.x; x[j + 1] = v.y; x[j + 2] = v.z; x[j + 3] = v.w;
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = there(j) ? __ldg(p + j) : 0.f;
-      }
-    };
-    float l[V];
-    load(l, row);
     if (a.sigmoid) {
 #pragma unroll
       for (int j = 0; j < V; ++j) { float rest; sigmoid_pair(l[j], s[j], rest); }
@@ -413,21 +424,28 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
 #pragma unroll
       for (int j = 0; j < V; ++j) s[j] *= inv;
     }
-    if (scores && valid) {
-      float* to = scores + t * a.E + e0;
-      if constexpr (Full && V % 4 == 0) {
 #pragma unroll
-        for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(to + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
+    for (int j = 0; j < V; j += (V % 4 == 0 ? 4 : 2)) {
+      if constexpr (V % 4 == 0) *reinterpret_cast<float4*>(mine_s + e0 + lane8 * kPad + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
+      else *reinterpret_cast<float2*>(mine_s + e0 + j) = make_float2(s[j], s[j + 1]);
+    }
+    if (scores) {
+      __syncwarp();
+      if constexpr (Full && V >= 4) {
+        // from shared memory in whole lines: lane i of a row of V 2 chunks
+#pragma unroll
+        for (int i = lane; i < 4 * V * 2; i += 32) {
+          const int r = i / (V * 2), e = i % (V * 2) * 4;
+          if (t0 + r < a.T) *reinterpret_cast<float4*>(scores + (t0 + r) * a.E + e) = *reinterpret_cast<const float4*>(&held[warp][r][e + e / V * kPad]);
+        }
       } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) if (there(j)) to[j] = s[j];
+        for (int r = 0; r < 4 && t0 + r < a.T; ++r)
+          for (int e = lane; e < a.E; e += 32) scores[(t0 + r) * a.E + e] = held[warp][r][e + e / V * kPad];
       }
     }
     if (bias) {
-      float b[V];
-      load(b, bias + e0);
 #pragma unroll
-      for (int j = 0; j < V; ++j) l[j] = s[j] + b[j];
+      for (int j = 0; j < V; ++j) l[j] = s[j] + held_bias[e0 + lane8 * kPad + j];
     }
 #pragma unroll
     for (int j = 0; j < V; ++j) key[j] = there(j) ? order_key(l[j]) : 0u;
@@ -458,6 +476,7 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
 #pragma unroll
       for (int j = 0; j < V; ++j) key[j] = in ? key[j] : 0u;
     }
+    if (t0 + step < a.T) load(l, logits + min(t0 + step + (lane >> 3), end) * a.E + e0);
     // The lane's largest in order, then k rounds (or fewer, where equal ones leave together).
     uint32_t q[V];
 #pragma unroll
@@ -493,12 +512,10 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
     if (bias) {
       // fp32 errors of s: of the exponent |l - m| 2^-24 e^-|l - m|, of exponential, sum and quotient 2^-21 s at most; of the sum with
       // the bias 2^-24 of it.  Twice that between two values, rounded up.
-      uint32_t after = 0;
-#pragma unroll
-      for (int j = 0; j < V; ++j) after = max(after, chosen >> j & 1 ? 0u : key[j]);
-      after = seg_max(after);
+      const uint32_t after = seg_max(q[0]);
       const float low = order_value(last);
-      near = near || equal || (after != 0 && !(low - order_value(after) > 0x1p-19f + 0x1p-22f * fabsf(low)));
+      const bool blind = V > Q && seg_max((uint32_t)__popc(chosen)) >= Q;              // a lane whose list has run out
+      near = near || equal || blind || (after != 0 && !(low - order_value(after) > 0x1p-19f + 0x1p-22f * fabsf(low)));
     }
     if (__any_sync(0xffffffffu, equal || near)) {
       // equal values at the border: the lowest indices of them stay (a token without any keeps its experts)
@@ -521,20 +538,16 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
       }
       place = seg_before(__popc(chosen), lane8);
     }
-    float f = a.scale;
-    if (a.renorm) {
-      float sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < V; ++j) sum += chosen >> j & 1 ? s[j] : 0.f;
-      f = a.scale / (seg_sum(sum) + kTopkEps);
-    }
-    // ascending: the chosen of lower lanes, then the lane's own
-    int32_t* idx = expert_idx + t * a.k + place;
-    float* w = gate_w + t * a.k + place;
-    if (valid) {
-#pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (chosen >> j & 1) { *idx++ = e0 + j; *w++ = s[j] * f; }
+    // ascending: the chosen of lower lanes, then the lane's own; each of the token's first k lanes then takes one
+    for (uint32_t left = chosen; left; left &= left - 1) mine_e[place++] = e0 + __ffs(left) - 1;
+    __syncwarp();
+    const bool takes = lane8 < a.k;
+    const int e = mine_e[takes ? lane8 : 0];
+    const float v = takes ? mine_s[e + e / V * kPad] : 0.f;
+    const float f = a.renorm ? a.scale / (seg_sum(v) + kTopkEps) : a.scale;
+    if (takes && valid) {
+      expert_idx[t * a.k + lane8] = e;
+      gate_w[t * a.k + lane8] = v * f;
     }
     __syncwarp();
   }
