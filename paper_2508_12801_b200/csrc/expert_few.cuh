@@ -14,10 +14,13 @@
 
 namespace msr {
 
-constexpr int kFewRows = 128, kFewThreads = 192, kFewRing = 196608;       // bytes of the operand ring
+constexpr int kFewRows = 128, kFewThreads = 192;
+// Bytes of the operand ring, and of each epilogue warp's staging (8-bit forms: three boxes of 16 rows of 64 bytes, and 16 of kept g and u)
+__host__ __device__ constexpr int few_ring(int form) { return form == kBf16 ? 196608 : 180224; }
+__host__ __device__ constexpr int few_box(int form) { return form == kBf16 ? 0 : 4096; }
 __host__ __device__ constexpr int few_pad(int rows) { return (rows + 15) / 16 * 16; }
 __host__ __device__ constexpr int few_stage_bytes(int pad) { return 16384 + pad * 128; }
-__host__ __device__ constexpr int few_smem(int epi, int pad) { return kFewRing + (epi == kEpiGlu ? pad * 256 : 0) + 1024; }
+__host__ __device__ constexpr int few_smem(int epi, int pad, int form) { return few_ring(form) + (epi == kEpiGlu ? pad * 256 : 0) + 4 * few_box(form) + 1024; }
 constexpr int kFewMaxStages = 10;
 
 struct FewSmem {
@@ -44,12 +47,12 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
   constexpr int kCols = EPI == kEpiGlu ? 64 : 128;                    // output columns of an item
   extern __shared__ unsigned char fsm_raw[];
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(fsm_raw) + 1023) & ~(uintptr_t)1023);
-  float* up = reinterpret_cast<float*>(base + kFewRing);              // [pad][64], gated only
+  float* up = reinterpret_cast<float*>(base + few_ring(Form));        // [pad][64], gated only
   __shared__ FewSmem sm;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr int kBK = Form == kInt8 ? 2 * kXBK : kXBK, kDepth = kBK / 4;      // depths of a slice (128 bytes) and of an MMA
   const int ntn = (a.N + kCols - 1) / kCols, nkb = (a.K + kBK - 1) / kBK;
-  const int stage_bytes = few_stage_bytes(pad), stages = min(kFewMaxStages, kFewRing / stage_bytes);
+  const int stage_bytes = few_stage_bytes(pad), stages = min(kFewMaxStages, few_ring(Form) / stage_bytes);
   uint32_t tmem_cols = 32;
   while ((int)tmem_cols < 2 * pad) tmem_cols <<= 1;
 
@@ -144,19 +147,17 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
       const int col = (t - sm.first[e]) * kCols + (EPI == kEpiGlu ? (q & 1) * 32 : q * 32) + lane;
       const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * pad);
       const size_t row0 = (size_t)e * a.C;
-      // backward from kept activations: 16 rows of this column's g and u, and lane j's step of g (lanes 16 on: of u) of row j
-      int8_t kg[16], ku[16];
+      const int first = col - lane;                                    // of the warp's 32 columns: a block of kept activations
+      // backward from kept activations: a lane brings 16 bytes of g and of u, and lane j the step of g (lanes 16 on: of u) of row j
+      uint4 kg, ku;
       float steps = 0.f;
       auto fetch = [&](int c0) {
         const int fp = keep_width(a.N), blocks = fp / kKeepBlock, r = c0 + (lane & 15);
-        if (col - lane >= a.N) return;                                 // the whole warp: fp reaches to the end of a block
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const int8_t* p = a.keep + (row0 + c0 + j) * 2 * fp + col;
-          kg[j] = c0 + j < rows ? __ldg(p) : (int8_t)0;
-          ku[j] = c0 + j < rows ? __ldg(p + fp) : (int8_t)0;
-        }
-        if (r < rows) steps = __ldg(a.keep_scale + ((size_t)e * 2 * blocks + (lane >> 4) * blocks + col / kKeepBlock) * a.C + r);
+        const bool in = first < a.N && c0 + (lane >> 1) < rows;
+        const uint4* p = reinterpret_cast<const uint4*>(a.keep + (row0 + c0 + (lane >> 1)) * 2 * fp + first + (lane & 1) * 16);
+        kg = in ? __ldg(p) : make_uint4(0, 0, 0, 0);
+        ku = in ? __ldg(p + fp / 16) : make_uint4(0, 0, 0, 0);
+        if (first < a.N && r < rows) steps = __ldg(a.keep_scale + ((size_t)e * 2 * blocks + (lane >> 4) * blocks + first / kKeepBlock) * a.C + r);
       };
       if constexpr (EPI == kEpiDact) fetch(0);
       ok = mbar_wait_bounded(&sm.acc_full[buf], (uint32_t)((turn >> 1) & 1));
@@ -165,48 +166,119 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
       tc_fence_after();
       float col_scale = 0.f;
       if (Form == kInt8 && col < a.N) col_scale = __ldg(a.w_scale + (EPI == kEpiGlu ? (size_t)e * 2 * a.N + (q >= 2 ? a.N : 0) : (size_t)e * a.N) + col);
-      // rows c0 to c0 + 15 of the column; 32-bit integers become the values they stand for
-      auto take = [&](int c0, float (&r)[16]) {
-        tmem_ld16(acc + c0, r);
-        if constexpr (Form == kInt8) {
+      if constexpr (Form != kBf16) {
+        // What a row costs here bounds these forms from a few dozen rows on.  Results pass through 16-row boxes so that they leave as
+        // 16-byte stores, and what belongs to a row (its scale, a block's step) is read or worked out once, by one lane.
+        unsigned char* box = base + few_ring(Form) + (EPI == kEpiGlu ? pad * 256 : 0) + (warp - 2) * few_box(Form);
+        auto take = [&](int c0, float (&r)[16]) {                      // 16 rows of the column; integers become the values they stand for
+          const float xs = Form == kInt8 && c0 + (lane & 15) < rows ? __ldg(a.x_scale + row0 + c0 + (lane & 15)) : 0.f;
+          __syncwarp();
+          tmem_ld16(acc + c0, r);
+          if constexpr (Form == kInt8) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j)
-            r[j] = c0 + j < rows ? (float)__float_as_int(r[j]) * (__ldg(a.x_scale + row0 + c0 + j) * col_scale) : 0.f;
-        }
-      };
-      // kKeep8: a warp's 32 columns of a row are a block; columns behind d_ff are zero, as the copies filled the weights up
-      auto keep = [&](int c0, const float (&r)[16]) {
-        const int fp = keep_width(a.N), blocks = fp / kKeepBlock, half = q >= 2, first = col - lane;
-        if (first >= a.N) return;
+            for (int j = 0; j < 16; ++j) r[j] = (float)__float_as_int(r[j]) * (__shfl_sync(0xffffffffu, xs, j) * col_scale);
+          }
+        };
+        auto put = [&](int b, int j, float v) { reinterpret_cast<__nv_bfloat16*>(box + b * 1024 + j * 64)[lane] = __float2bfloat16(v); };
+        auto flush = [&](int b, __nv_bfloat16* dst, size_t stride, int c0) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          if (c0 + j >= rows) break;
-          const Step8 st8 = step8(__reduce_max_sync(0xffffffffu, abs_bits(__float_as_uint(r[j]))));
-          a.keep[((row0 + c0 + j) * 2 + half) * fp + col] = st8.inv > 0.f ? (int8_t)round8(r[j], st8.inv) : (int8_t)0;
-          if (lane == 0) a.keep_scale[((size_t)e * 2 * blocks + half * blocks + first / kKeepBlock) * a.C + c0 + j] = st8.scale;
-        }
-      };
-      if constexpr (EPI == kEpiDact) {
-        for (int c0 = 0; c0 < rows; c0 += 16) {
-          float r[16];
-          if (c0) fetch(c0);
-          take(c0, r);
+          for (int i = 0; i < 2; ++i) {
+            const int r = i * 8 + (lane >> 2), c = first + (lane & 3) * 8;
+            if (c0 + r < rows && c < a.N)
+              *reinterpret_cast<uint4*>(dst + (row0 + c0 + r) * stride + c) = *reinterpret_cast<const uint4*>(box + b * 1024 + r * 64 + (lane & 3) * 16);
+          }
+        };
+        // columns behind d_ff are zero, as the copies filled the weights up
+        auto keep = [&](int c0, const float (&r)[16]) {
+          const int fp = keep_width(a.N), blocks = fp / kKeepBlock, half = q >= 2;
+          uint32_t amax = 0;
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
-            const float g = (float)kg[j] * __shfl_sync(0xffffffffu, steps, j), u = (float)ku[j] * __shfl_sync(0xffffffffu, steps, 16 + j);
-            const float s = sigmoid_f<true>(g);
-            if (col < a.N && c0 + j < rows) {
-              __nv_bfloat16* o = out + (row0 + c0 + j) * 2 * a.N + col;
-              o[0] = __float2bfloat16(r[j] * u * s * (1.f + g * (1.f - s)));
-              o[a.N] = __float2bfloat16(r[j] * g * s);
-              if (pre_out) pre_out[(row0 + c0 + j) * a.N + col] = __float2bfloat16(g * s * u);
+            const uint32_t m = __reduce_max_sync(0xffffffffu, abs_bits(__float_as_uint(r[j])));
+            if ((lane & 15) == j) amax = m;
+          }
+          const Step8 st8 = step8(amax);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const float inv = __shfl_sync(0xffffffffu, st8.inv, j);
+            box[j * 32 + lane] = inv > 0.f ? (unsigned char)round8(r[j], inv) : (unsigned char)0;
+          }
+          __syncwarp();
+          if (first < a.N) {
+            if (c0 + (lane >> 1) < rows)
+              *reinterpret_cast<uint4*>(a.keep + ((row0 + c0 + (lane >> 1)) * 2 + half) * fp + first + (lane & 1) * 16) = *reinterpret_cast<const uint4*>(box + lane * 16);
+            if (lane < 16 && c0 + lane < rows) a.keep_scale[((size_t)e * 2 * blocks + half * blocks + first / kKeepBlock) * a.C + c0 + lane] = st8.scale;
+          }
+          __syncwarp();
+        };
+        if constexpr (EPI == kEpiPlain) {
+          for (int c0 = 0; c0 < rows; c0 += 16) {
+            float r[16];
+            take(c0, r);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) put(0, j, r[j]);
+            __syncwarp();
+            flush(0, out, a.N, c0);
+            __syncwarp();
+          }
+        } else if constexpr (EPI == kEpiDact) {
+          const unsigned char* kept = box + 3072;
+          for (int c0 = 0; c0 < rows; c0 += 16) {
+            *reinterpret_cast<uint4*>(box + 3072 + lane * 16) = kg;
+            *reinterpret_cast<uint4*>(box + 3584 + lane * 16) = ku;
+            const float now = steps;
+            __syncwarp();
+            if (c0 + 16 < rows) fetch(c0 + 16);
+            float r[16];
+            take(c0, r);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const float g = (float)(int8_t)kept[j * 32 + lane] * __shfl_sync(0xffffffffu, now, j);
+              const float u = (float)(int8_t)kept[512 + j * 32 + lane] * __shfl_sync(0xffffffffu, now, 16 + j);
+              const float s = sigmoid_f<true>(g);
+              put(0, j, r[j] * u * s * (1.f + g * (1.f - s)));
+              put(1, j, r[j] * g * s);
+              put(2, j, g * s * u);
             }
+            __syncwarp();
+            flush(0, out, 2 * (size_t)a.N, c0);
+            flush(1, out + a.N, 2 * (size_t)a.N, c0);
+            if (pre_out) flush(2, pre_out, a.N, c0);
+            __syncwarp();
+          }
+        } else {
+          // The lower rows' u goes over to the warps that hold g, the upper rows' g to those that hold u: each half forms its part of h.
+          const bool gate = q < 2;
+          const int mid = (rows + 31) / 32 * 16;
+          for (int c0 = 0; c0 < rows; c0 += 16) {
+            const bool give = gate == (c0 >= mid);
+            if (Form != kKeep8 && !give) continue;
+            float r[16];
+            take(c0, r);
+            if constexpr (Form == kKeep8) keep(c0, r);
+            if (give) {
+#pragma unroll
+              for (int j = 0; j < 16; ++j) up[(c0 + j) * 64 + (q & 1) * 32 + lane] = r[j];
+            }
+          }
+          asm volatile("bar.sync 1, 128;" ::: "memory");
+          for (int c0 = gate ? 0 : mid; c0 < (gate ? min(mid, rows) : rows); c0 += 16) {
+            float r[16];
+            take(c0, r);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const float o = up[(c0 + j) * 64 + (q & 1) * 32 + lane];
+              put(0, j, gate ? silu_mul<true>(r[j], o) : silu_mul<true>(o, r[j]));
+            }
+            __syncwarp();
+            flush(0, out, a.N, c0);
+            __syncwarp();
           }
         }
       } else if constexpr (EPI == kEpiPlain) {
         for (int c0 = 0; c0 < rows; c0 += 16) {
           float r[16];
-          take(c0, r);
+          tmem_ld16(acc + c0, r);
           if (col < a.N) {
 #pragma unroll
             for (int j = 0; j < 16; ++j)
@@ -217,8 +289,7 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
         if (q >= 2)
           for (int c0 = 0; c0 < rows; c0 += 16) {
             float r[16];
-            take(c0, r);
-            if constexpr (Form == kKeep8) keep(c0, r);
+            tmem_ld16(acc + c0, r);
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
               up[(c0 + j) * 64 + (q & 1) * 32 + lane] = r[j];
@@ -229,8 +300,7 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
         if (q < 2)
           for (int c0 = 0; c0 < rows; c0 += 16) {
             float r[16];
-            take(c0, r);
-            if constexpr (Form == kKeep8) keep(c0, r);
+            tmem_ld16(acc + c0, r);
             if (col < a.N) {
 #pragma unroll
               for (int j = 0; j < 16; ++j)

@@ -129,9 +129,9 @@ maxscore_status launch_few(maxscore_ctx* c, const void* x, const void* w, void* 
   }
   const long long items = (long long)a.E * ((a.N + (EPI == kEpiGlu ? 63 : 127)) / (EPI == kEpiGlu ? 64 : 128));
   const int grid = (int)std::min<long long>(c->sm_count, items);
-  s = room_for(c, expert_few_kernel<EPI, B_MN, Form>, few_smem(EPI, kFewRows));
+  s = room_for(c, expert_few_kernel<EPI, B_MN, Form>, few_smem(EPI, kFewRows, Form));
   if (s) return s;
-  expert_few_kernel<EPI, B_MN, Form><<<grid, kFewThreads, few_smem(EPI, pad), st>>>(tW0, tW1, tX, (__nv_bfloat16*)out, (__nv_bfloat16*)pre_out, a,
+  expert_few_kernel<EPI, B_MN, Form><<<grid, kFewThreads, few_smem(EPI, pad, Form), st>>>(tW0, tW1, tX, (__nv_bfloat16*)out, (__nv_bfloat16*)pre_out, a,
                                                                                    pad, error_flag_of(c));
   MS_LAUNCH_CHECK("expert_few_kernel");
   c->launches += 1;

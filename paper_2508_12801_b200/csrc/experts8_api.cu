@@ -47,7 +47,9 @@ maxscore_status launch_int8(maxscore_ctx* c, const int8_t* xq, const float* xs, 
                             int32_t d_in, int32_t d_out, cudaStream_t st) {
   ExpertArgs a = expert_args(c, load, 0, d_out, d_in);
   a.x_scale = xs; a.w_scale = ws;
-  if (c->C <= kFewRows) return launch_few<EPI, false, kInt8>(c, xq, wq, out, nullptr, a, st);
+  // Few rows: weights on the MMA's M side, read once.  us, against the 256-row tiles: gated, 2048 -> 1024, E 64: C 16 49 / 55, 64 53 / 56,
+  // 96 60 / 57, 128 72 / 59; 1024 -> 2048: C 16 26 / 37, 64 33 / 38, 96 41 / 39, 128 48 / 40; E 128, 2320 -> 400 and back: C 96 58 / 64, 70 / 78.
+  if (c->C <= 80) return launch_few<EPI, false, kInt8>(c, xq, wq, out, nullptr, a, st);
   return launch_tc<EPI, false, kInt8>(c, xq, wq, nullptr, out, nullptr, a, st);
 }
 
@@ -155,7 +157,9 @@ maxscore_status maxscore_expert_glu_keep8(maxscore_ctx* c, const void* x, const 
     return MAXSCORE_ERR_INVALID_ARG;
   const ExpertArgs a = keep_args(c, expert_load, d_ff, d_in, keep);
   cudaStream_t st = (cudaStream_t)stream;
-  if (c->C <= kFewRows)
+  // Few rows against the 256-row tiles, us: the former while the weights' bytes count for more than what each row costs in the epilogue.
+  // C 64: 248 -> 288 19 / 20, 1024 -> 512 11 / 12, 2048 -> 1024 90 / 102;  C 128: 32 / 20, 16 / 13, 102 / 110, 2320 -> 400 109 / 123.
+  if (c->C <= 64 || (c->C <= kFewRows && d_in >= 2048))
     return w_layout == 0 ? launch_few<kEpiGlu, true, kKeep8>(c, x, w_up, h, nullptr, a, st) : launch_few<kEpiGlu, false, kKeep8>(c, x, w_up, h, nullptr, a, st);
   return w_layout == 0 ? launch_tc<kEpiGlu, true, kKeep8>(c, x, w_up, nullptr, h, nullptr, a, st)
                        : launch_tc<kEpiGlu, false, kKeep8>(c, x, w_up, nullptr, h, nullptr, a, st);
@@ -172,7 +176,9 @@ maxscore_status maxscore_expert_glu_bwd_keep8(maxscore_ctx* c, const void* dy, c
     return MAXSCORE_ERR_INVALID_ARG;
   const ExpertArgs a = keep_args(c, expert_load, d_ff, d_out, const_cast<void*>(keep));
   cudaStream_t st = (cudaStream_t)stream;
-  if (c->C <= kFewRows) return w_layout == 1 ? launch_few<kEpiDact, true, kKeep8>(c, dy, w_down, dpre, h, a, st) : launch_few<kEpiDact, false, kKeep8>(c, dy, w_down, dpre, h, a, st);
+  // us, against the 256-row tiles, C 16: 248 -> 288 10 / 33, 1024 -> 512 8.5 / 17, 2048 -> 1024 51 / 67;  C 128: 36 / 39, 21 / 21, 89 / 91.
+  if (c->C <= kFewRows)
+    return w_layout == 1 ? launch_few<kEpiDact, true, kKeep8>(c, dy, w_down, dpre, h, a, st) : launch_few<kEpiDact, false, kKeep8>(c, dy, w_down, dpre, h, a, st);
   return w_layout == 1 ? launch_tc<kEpiDact, true, kKeep8>(c, dy, w_down, nullptr, dpre, h, a, st)
                        : launch_tc<kEpiDact, false, kKeep8>(c, dy, w_down, nullptr, dpre, h, a, st);
 }
