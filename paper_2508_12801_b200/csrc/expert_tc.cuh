@@ -522,6 +522,10 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
             load(kg, g); load(ku, g + fp);
             const float* st8 = a.keep_scale + ((size_t)x.e * 2 * blocks + col / kKeepBlock) * a.C + y0 + lane;
             sg = __ldg(st8); su = __ldg(st8 + (size_t)blocks * a.C);
+          } else {                                                     // rows behind the load, columns behind d_ff: g = u = 0
+            sg = su = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) kg[j] = ku[j] = 0;
           }
           __syncwarp();
         };
@@ -631,20 +635,27 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
               for (int i = 0; i < 4; ++i) {
                 uint32_t u[8];
                 tmem_ld8(acc + c0 + 8 * i, u);
-                float dg[8], du[8];
+                uint32_t dg[4], du[4];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                  const int w = 2 * i + (j >> 2);
-                  const float g = byte8(kg[w] ^ 0x80808080u, j & 3) * sg, up = byte8(ku[w] ^ 0x80808080u, j & 3) * su;
-                  const float s = sigmoid_f<true>(g), dh = __uint_as_float(u[j]);
-                  dg[j] = keep_row ? dh * up * s * (1.f + g * (1.f - s)) : 0.f;
-                  du[j] = keep_row ? dh * g * s : 0.f;
-                  const float hv = keep_row ? g * s * up : 0.f;
-                  uint32_t& hw = h[c0 / 2 + 4 * i + (j >> 1)];
-                  hw = j & 1 ? pack_bf16(__uint_as_float(hw), hv) : __float_as_uint(hv);
+                for (int p = 0; p < 4; ++p) {                          // columns 2 p and 2 p + 1 of the eight, packed
+                  const uint32_t gw = kg[2 * i + (p >> 1)] ^ 0x80808080u, uw = ku[2 * i + (p >> 1)] ^ 0x80808080u;
+                  const int b = (p & 1) * 2;
+                  const float2 g = mul2(add2(make_float2(byte8_raw(gw, b), byte8_raw(gw, b + 1)), both(-kByte8Zero)), both(sg));
+                  const float2 up = mul2(add2(make_float2(byte8_raw(uw, b), byte8_raw(uw, b + 1)), both(-kByte8Zero)), both(su));
+                  const float2 dh = make_float2(keep_row ? __uint_as_float(u[2 * p]) : 0.f, keep_row ? __uint_as_float(u[2 * p + 1]) : 0.f);
+                  float2 t = mul2(g, both(-1.44269504f)), s;           // s = 1 / (1 + 2^t), as sigmoid_f<true>
+                  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t.x) : "f"(t.x));
+                  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t.y) : "f"(t.y));
+                  t = add2(t, both(1.f));
+                  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.x) : "f"(t.x));
+                  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.y) : "f"(t.y));
+                  const float2 gs = mul2(g, s), slope = fma2(g, fma2(s, both(-1.f), both(1.f)), both(1.f));
+                  const float2 a = mul2(mul2(mul2(dh, up), s), slope), c = mul2(dh, gs), hv = mul2(gs, up);
+                  dg[p] = pack_bf16(a.x, a.y); du[p] = pack_bf16(c.x, c.y);
+                  h[c0 / 2 + 4 * i + p] = pack_bf16(hv.x, hv.y);
                 }
-                Vec16<__nv_bfloat16>::store(reinterpret_cast<__nv_bfloat16*>(stage + lane * kRow + ((i ^ swz(lane)) << 4)), dg);
-                Vec16<__nv_bfloat16>::store(reinterpret_cast<__nv_bfloat16*>(stage + (32 + lane) * kRow + ((i ^ swz(lane)) << 4)), du);
+                *reinterpret_cast<uint4*>(stage + lane * kRow + ((i ^ swz(lane)) << 4)) = make_uint4(dg[0], dg[1], dg[2], dg[3]);
+                *reinterpret_cast<uint4*>(stage + (32 + lane) * kRow + ((i ^ swz(lane)) << 4)) = make_uint4(du[0], du[1], du[2], du[3]);
               }
               if (c0 + 32 < kCols) fetch8(col0 + c0 + 32);             // on its way while the results leave
               char* dst = out + (row0 * 2 * a.N + col0 + c0) * 2;

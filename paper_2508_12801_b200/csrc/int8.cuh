@@ -30,9 +30,8 @@ __device__ __forceinline__ float max_abs(float m, float a, float b) {
   asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(fabsf(a)), "f"(fabsf(b)));
   return m;
 }
-// integer i of a word of four as a float: exact
-__device__ __forceinline__ float byte8(uint32_t w_flipped, int i) {                   // w ^ 0x80808080
-  return __uint_as_float(__byte_perm(w_flipped, 0x4b000000u, 0x7440 + i)) - 8388736.f;
-}
+// Integer i of a word of four, plus kByte8Zero, as a float: exact.  The word comes with its sign bits flipped (^ 0x80808080).
+constexpr float kByte8Zero = 8388736.f;              // 2^23 + 128
+__device__ __forceinline__ float byte8_raw(uint32_t flipped, int i) { return __uint_as_float(__byte_perm(flipped, 0x4b000000u, 0x7440 + i)); }
 
 }  // namespace msr
