@@ -10,8 +10,8 @@
 //
 // Two forms.  In the usual one eight lanes own a token and a warp four: next to 4 E bytes of logits the instructions count, and what a
 // token needs once (sums, maxima, the k rounds) costs a quarter of what it does with a warp per token.  Each lane sorts the values of
-// its consecutive experts, keeps the eight largest, and in k rounds the largest heads leave.  Groups that are not whole lanes, a power of two of them, take the
-// other form, a warp per token with the groups' values in shared memory.
+// its consecutive experts, keeps the eight largest, and in k rounds the largest heads leave.  Few tokens, which a warp each serves sooner, and groups that are not
+// whole lanes, a power of two of them, take the other form, a warp per token with the groups' values in shared memory.
 // T 65536, E 128, k 8: see the figures at the launch.
 #pragma once
 #include "common.cuh"
@@ -109,32 +109,47 @@ __device__ __forceinline__ void topk_scores(const float (&l)[VPT], int E, int la
 // The choice in 64 bits, for rows that fp32 cannot decide.  Returns this lane's chosen experts as bits.  `d`: E doubles of the warp's own.
 __device__ __noinline__ uint32_t topk_choose_64(const float* __restrict__ row, const float* __restrict__ bias, TopkArgs a, int vpt, double* d) {
   const int lane = threadIdx.x & 31, e0 = lane * vpt;
-  double m = -INFINITY, sum = 0.0;
-  if (!a.sigmoid) {
-    for (int j = 0; j < vpt; ++j) if (e0 + j < a.E) m = fmax(m, (double)__ldg(row + e0 + j));
+  double l[4], v[4];                                                  // four chains side by side: this is a matter of latency
+  bool in[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    in[j] = j < vpt && e0 + j < a.E;
+    l[j] = in[j] ? (double)__ldg(row + e0 + j) : -INFINITY;
+  }
+  if (a.sigmoid) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = 1.0 / (1.0 + exp(-l[j]));
+  } else {
+    double m = fmax(fmax(l[0], l[1]), fmax(l[2], l[3])), sum = 0.0;
     for (int o = 16; o > 0; o >>= 1) m = fmax(m, __shfl_xor_sync(0xffffffffu, m, o));
-    for (int j = 0; j < vpt; ++j) if (e0 + j < a.E) sum += exp((double)__ldg(row + e0 + j) - m);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { v[j] = exp(l[j] - m); sum += in[j] ? v[j] : 0.0; }
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] /= sum;
   }
   auto order = [](double x) { return x == x ? x : -INFINITY; };      // NaN comes last
   __syncwarp();
-  for (int j = 0; j < vpt; ++j)
-    if (e0 + j < a.E) {
-      const double l = (double)__ldg(row + e0 + j);
-      const double s = a.sigmoid ? 1.0 / (1.0 + exp(-l)) : exp(l - m) / sum;
-      d[e0 + j] = order(bias ? s + (double)__ldg(bias + e0 + j) : s);
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (in[j]) {
+      v[j] = order(bias ? v[j] + (double)__ldg(bias + e0 + j) : v[j]);
+      d[e0 + j] = v[j];
     }
   __syncwarp();
   uint32_t kept = 1u;
   if (a.n_group > 1) {
     double m1 = -INFINITY, m2 = -INFINITY;
-    if (lane < a.n_group)
+    if (lane < a.n_group) {
+#pragma unroll 4
       for (int i = 0; i < a.group_size; ++i) {
         const double x = d[lane * a.group_size + i];
-        if (x > m1) { m2 = m1; m1 = x; } else if (x > m2) m2 = x;
+        m2 = fmax(m2, fmin(m1, x)); m1 = fmax(m1, x);
       }
+    }
     const double value = order(a.pairs && a.group_size > 1 ? m1 + m2 : m1);
     int before = 0;
+#pragma unroll 4
     for (int g = 0; g < a.n_group; ++g) {
       const double other = __shfl_sync(0xffffffffu, value, g);
       before += other > value || (other == value && g < lane);
@@ -143,20 +158,23 @@ __device__ __noinline__ uint32_t topk_choose_64(const float* __restrict__ row, c
   }
   if (!bias) {                                          // the experts themselves by their logits, as in fp32
     __syncwarp();
-    for (int j = 0; j < vpt; ++j) if (e0 + j < a.E) d[e0 + j] = order((double)__ldg(row + e0 + j));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) if (in[j]) { v[j] = order(l[j]); d[e0 + j] = v[j]; }
     __syncwarp();
   }
-  uint32_t chosen = 0;
-  for (int j = 0; j < vpt; ++j) {
-    const int e = e0 + j;
-    if (e >= a.E || !(kept >> (e / a.group_size) & 1)) continue;
-    int before = 0;
-    for (uint32_t rest = kept; rest; rest &= rest - 1) {
-      const int first = (__ffs(rest) - 1) * a.group_size;
-      for (int i = first; i < first + a.group_size; ++i) before += d[i] > d[e] || (d[i] == d[e] && i < e);
+  int before[4] = {};
+  for (uint32_t rest = kept; rest; rest &= rest - 1) {
+    const int first = (__ffs(rest) - 1) * a.group_size;
+#pragma unroll 4
+    for (int i = first; i < first + a.group_size; ++i) {
+      const double x = d[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) before[j] += x > v[j] || (x == v[j] && i < e0 + j);
     }
-    if (before < a.k) chosen |= 1u << j;
   }
+  uint32_t chosen = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) if (in[j] && (kept >> ((e0 + j) / a.group_size) & 1) && before[j] < a.k) chosen |= 1u << j;
   __syncwarp();
   return chosen;
 }
@@ -194,7 +212,7 @@ __device__ __noinline__ uint32_t topk_choose_equal(const uint32_t* key, int k) {
   return chosen;
 }
 
-// A warp per token, groups of any size.
+// A warp per token, groups of any size or none.
 template <int VPT, bool Full>
 __global__ void __launch_bounds__(kTopkWarps * 32)
 topk_fwd_scan_kernel(const float* __restrict__ logits, const float* __restrict__ bias, float* __restrict__ scores, int32_t* __restrict__ expert_idx,
@@ -230,7 +248,7 @@ topk_fwd_scan_kernel(const float* __restrict__ logits, const float* __restrict__
       key[j] = Full || e0 + j < a.E ? order_key(c[j]) : 0u;
     }
     bool near = false;                                                 // the same in all lanes
-    {
+    if (a.n_group > 1) {
       // the two largest of each group (NaN counts as nothing)
       if (!bias && a.pairs) {
 #pragma unroll

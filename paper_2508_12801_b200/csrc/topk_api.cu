@@ -67,7 +67,10 @@ maxscore_status maxscore_topk_fwd(maxscore_ctx* c, const float* logits, const fl
   if (!apart({{scores, rows}, {expert_idx, pairs}, {gate_w, pairs}}, {{logits, rows}, {bias, sizeof(float) * (size_t)a.E}}))
     return MAXSCORE_ERR_INVALID_ARG;
   const int v = a.E <= 16 ? 2 : a.E <= 32 ? 4 : a.E <= 64 ? 8 : 16, lanes = a.group_size / v;       // experts of a lane of eight
-  if (a.n_group == 1 || (a.group_size % v == 0 && (lanes & (lanes - 1)) == 0)) {
+  // Eight lanes a token, or a warp where its tokens are resident at once.  us, E 128, k 8 (with groups, bias and scores): T 1 2.7 / 2.2 (3.8 / 2.9),
+  // 1024 3.7 / 2.6, 2048 3.8 / 3.0, 4096 3.8 / 4.5, 16384 6.8 / 10.3 (16.5 / 21.0).
+  const bool many = c->p.T > 16 * c->sm_count;
+  if (many && (a.n_group == 1 || (a.group_size % v == 0 && (lanes & (lanes - 1)) == 0))) {
     while (a.n_group > 1 && 1 << a.group_shift < lanes) ++a.group_shift;
     auto go = [&](auto per_lane, auto whole) {
       constexpr int V = decltype(per_lane)::value;

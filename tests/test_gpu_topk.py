@@ -170,6 +170,72 @@ def test_rows_that_are_not_finite(ms, bad):
             assert torch.equal(idx[keep_rows], choose64(l, bias, 8, False, groups, keep, True)[keep_rows]) and w[keep_rows].isfinite().all()
 
 
+# From some 2 400 tokens on eight lanes own a token instead of a warp (where groups are whole lanes): the same again with rows enough for that.
+MANY = 2601          # no multiple of the four tokens of a warp
+
+
+def many(l):
+    return l.repeat(-(-MANY // l.shape[0]), 1)[:MANY].contiguous()
+
+
+@pytest.mark.parametrize("E, k, groups, keep", [(1, 1, 1, 1), (2, 2, 1, 1), (8, 2, 2, 1), (12, 3, 3, 2), (16, 8, 4, 3), (16, 2, 8, 1), (32, 8, 4, 1), (31, 8, 1, 1),
+                                                (33, 5, 1, 1), (40, 6, 5, 3), (64, 8, 8, 4), (64, 1, 2, 1), (96, 8, 3, 2), (100, 7, 1, 1), (127, 8, 1, 1),
+                                                (128, 8, 8, 4), (128, 6, 4, 1), (128, 8, 2, 1), (128, 8, 1, 1)])
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("with_bias", [False, True])
+def test_many_tokens(ms, E, k, groups, keep, sigmoid, with_bias):
+    g = torch.Generator().manual_seed(E * 7 + k)
+    l = torch.randn(MANY, E, generator=g) * 2
+    l[:200] = torch.randint(-1, 2, (200, E), generator=g).float()            # ties
+    l[200:210] = 0.5
+    l[210:300][torch.rand(90, E, generator=g) < 0.4] = -math.inf
+    l[210:300, E // 2] = 1.0                                              # something is left in every row
+    bias = (torch.randn(E, generator=g) * 0.05 if E % 3 else torch.randint(0, 2, (E,), generator=g) * 0.25) if with_bias else None
+    for pairs in ([False, True] if groups > 1 else [False]):
+        check(ms, l, bias, k, sigmoid, True, 2.5, groups, keep, pairs)
+    check(ms, l, bias, k, sigmoid, False, 1.0, groups, keep)
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_many_tokens_that_only_64_bits_tell_apart(ms, sigmoid):
+    g = torch.Generator().manual_seed(5)
+    E, k = 128, 8
+    l = (torch.randn(1, E, generator=g) * 2).expand(40, E).contiguous() + torch.randn(40, 1, generator=g) * (0.0 if sigmoid else 1.0)
+    bias = (1.0 - scores64(l[:1], sigmoid)[0]).float()
+    check(ms, many(l), bias, k, sigmoid)
+    check(ms, many(l), bias, k, sigmoid, groups=8, keep=3, pairs=True)
+    l = torch.randint(0, 3, (300, 64), generator=g).float() + torch.randint(0, 4, (300, 64), generator=g) * 2.0 ** -22
+    check(ms, many(l), None, 8, sigmoid, groups=8, keep=3, pairs=True)
+    # the ten largest in one lane's consecutive experts, the ninth as near to the eighth as 64 bits see it
+    l = torch.randn(300, E, generator=g) - 8
+    l[:, 32:42] = torch.linspace(1.0, 2.0, 10).flip(0)
+    l[:, 41] = l[:, 40]
+    bias = torch.zeros(E)
+    bias[41] = 2.0 ** -40
+    check(ms, many(l), bias, 8, sigmoid)
+    l[:, 40] = l[:, 39]
+    bias[39] = 2.0 ** -41
+    check(ms, many(l), bias, 8, sigmoid)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_many_rows_that_are_not_finite(ms, bad):
+    g = torch.Generator().manual_seed(9)
+    for E, groups, keep in ((128, 1, 1), (128, 8, 4), (33, 1, 1), (64, 4, 2)):
+        l = torch.randn(MANY, E, generator=g)
+        rows = torch.arange(0, MANY, 3)
+        l[rows, torch.randint(0, E, (len(rows),), generator=g)] = bad
+        l[6] = -math.nan
+        l[9] = -math.inf
+        for bias in (None, torch.zeros(E)):
+            _, idx, w = run(ms, l, bias, 8, ms.make_topk(ms.SOFTMAX, groups, keep, True))
+            assert (idx >= 0).all() and (idx < E).all() and (idx[:, 1:] > idx[:, :-1]).all()
+            assert w[rows].isnan().all()
+            fine = torch.ones(MANY, dtype=torch.bool)
+            fine[rows] = False
+            assert torch.equal(idx[fine], choose64(l, bias, 8, False, groups, keep, True)[fine]) and w[fine].isfinite().all()
+
+
 def dl64(l, idx, dw, col, sigmoid, renorm, scale):
     l = l.to(F64).requires_grad_(True)
     s = torch.sigmoid(l) if sigmoid else torch.softmax(l, 1)
