@@ -29,6 +29,8 @@ __device__ __forceinline__ uint4 quant16(const uint4& lo, const uint4& hi, float
   return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
+// Bound by DRAM: two bytes read and one written a value (dispatch: k written).  Rows of 4096 in expert buffers 6.4 TB/s, of 1024 5.5; dispatch at T 65536,
+// d 4096, k 8 460 us, 5.8 TB/s.
 // A warp quantises a row of `chunks` 16-element chunks into its `n` destinations.  V: chunks that a lane holds from one pass to the next; 0: any
 // number, read twice (the second time from the caches).
 template <int V, typename Put>

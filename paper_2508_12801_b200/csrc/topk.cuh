@@ -12,7 +12,8 @@
 // token needs once (sums, maxima, the k rounds) costs a quarter of what it does with a warp per token.  Each lane sorts the values of
 // its consecutive experts, keeps the eight largest, and in k rounds the largest heads leave.  Few tokens, which a warp each serves sooner, and groups that are not
 // whole lanes, a power of two of them, take the other form, a warp per token with the groups' values in shared memory.
-// T 65536, E 128, k 8: see the figures at the launch.
+// T 65536, E 128, k 8: 33 us with groups, bias and scores written (a warp per token 49), 19 to 21 without any (31); the bytes take 11 and 6.  300
+// instructions a token (580 with a warp for each), issued in 66 to 72 % of the clocks.
 #pragma once
 #include "common.cuh"
 
@@ -574,7 +575,8 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
 // dl from the gradient of the weights and, if given, one of the scores that all tokens share (the balance loss).
 //   ds_c = scale / (S + eps) (g_c - sum_j g_j s_j / (S + eps)), S the sum of the chosen s;  without renorm scale g_c
 //   softmax: dl = s (ds - sum ds s)      sigmoid: dl = ds s (1 - s)
-// Lanes 0 to k - 1 hold the chosen pairs; rows of shared memory carry s to them and ds back.
+// Lanes 0 to k - 1 hold the chosen pairs; rows of shared memory carry s to them and ds back.  T 65536, E 128, k 8: 18 us, of 11 by the bytes; 190
+// instructions a token, issued in 77 % of the clocks.
 template <int VPT, bool Full>
 __global__ void __launch_bounds__(kTopkWarps * 32)
 topk_bwd_kernel(const float* __restrict__ logits, const int32_t* __restrict__ expert_idx, const float* __restrict__ dgate_w,
