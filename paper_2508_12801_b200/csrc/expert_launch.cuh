@@ -73,21 +73,20 @@ maxscore_status launch_tc(maxscore_ctx* c, const void* A, const void* B, const v
       else MS_MAP(&tB1, (const char*)B + N * K * elem, K, N, K, cols * K, 128, false, elem);
     }
     if (EPI != kEpiDact) MS_MAP(&tO0, out, N, C, N, C * N, 32);
-    else if (Form == kKeep8 && pre_out) MS_MAP(&tO0, pre_out, N, C, N, C * N, 32);
     if (EPI == kEpiGlu && Form == kBf16 && pre_out) {
       MS_MAP(&tO1, pre_out, N, C, 2 * N, C * 2 * N, 32);
       MS_MAP(&tO2, (P)pre_out + N, N, C, 2 * N, C * 2 * N, 32);
     }
   }
 #undef MS_MAP
-  if (kDw || (EPI == kEpiDact && (Form != kKeep8 || !pre_out))) tO0 = tA;      // not used
+  if (kDw || EPI == kEpiDact) tO0 = tA;                  // not used
   if (EPI != kEpiGlu || Form != kBf16 || !pre_out) tO1 = tO2 = tO0;       // not used
   const long long tile_n = EPI == kEpiGlu ? 128 : kXTile;
   const long long tiles = (long long)a.E * (((kDw ? M : C) + kXTile - 1) / kXTile) * ((N + tile_n - 1) / tile_n);
   const int pairs = (int)std::min<long long>(c->sm_count / 2, tiles);
   auto go = [&](auto kernel, int w) {
-    s = room_for(c, kernel, x_smem(EPI, w));
-    if (!s) kernel<<<2 * pairs, x_threads(EPI), x_smem(EPI, w), st>>>(tA, tB0, tB1, tO0, tO1, tO2, (char*)out, (char*)pre_out, (const char*)pre_in, a, error_flag_of(c));
+    s = room_for(c, kernel, x_smem(EPI, w, Form));
+    if (!s) kernel<<<2 * pairs, x_threads(EPI), x_smem(EPI, w, Form), st>>>(tA, tB0, tB1, tO0, tO1, tO2, (char*)out, (char*)pre_out, (const char*)pre_in, a, error_flag_of(c));
   };
   // Two column tiles at a time read a quarter less per flop, but their epilogues hide less well.  Long runs, 256 x 512 against
   // 256 x 256: y at C 4096, K 4096 1 248 / 1 234 TFLOP/s, at C 1024, K 2048 1 150 / 1 145, K 1024 1 041 / 1 055, K 512 853 / 904;

@@ -17,9 +17,9 @@
 // loads from the L2 reach 67.  E 32, C 4096: h at K 4096 3 000 TOPS (tensor pipe 90 % active), y at K 1024 2 400 (69 %, the results' stores on
 // top of the loads); long runs at E 128 2 700 to 2 800 and 2 050 to 2 150.  What a sum stands for is worked out in the epilogue.
 // Form kKeep8: h as ever, then g and u block by block from the accumulator into 8 bits (E 128, C 4096, 4096 -> 1024: 7.0 to 7.9 ms, as when they are
-// kept in bf16; 6.3 without).  The backward pass reads them straight into registers, a sector a lane, one step ahead of its use, and forms h again:
-// E 64, C 2560, 2048 -> 1000 650 to 680 us, 810 TFLOP/s, where the bf16 form without h takes 580 to 630.  Switching parts off: without its stores 560, without
-// its loads 580, without its arithmetic 650; latency in the epilogue is what is left.
+// kept in bf16; 6.3 without).  The backward pass takes them into registers, a sector a lane, one step ahead of its use, and forms h again: E 64, C 2560,
+// 2048 -> 1000 640 to 680 us, 810 TFLOP/s, where the bf16 form without h takes 580 to 630.  Its epilogue is 18 000 clocks a tile of the 27 000 that a tile takes
+// in long runs at 1.2 GHz, under the power cap.
 #pragma once
 #include "expert.cuh"
 #include "int8.cuh"
@@ -114,11 +114,12 @@ __host__ __device__ constexpr int x_stage_bytes(int w) { return 16384 * (1 + w);
 // operands in, two results out, an exponential and a quotient each) is what bounds it up to K of a few thousand.
 __host__ __device__ constexpr int x_epi_warps(int epi) { return epi == kEpiDact ? 16 : 8; }
 __host__ __device__ constexpr int x_threads(int epi) { return 64 + 32 * x_epi_warps(epi); }
-// Staging of an epilogue warp: boxes of 32 rows of 128 bytes (64 bytes in the backward), one for dW, a pair for the others.
-__host__ __device__ constexpr int x_box_bytes(int epi) { return epi == kEpiDw || epi == kEpiDact ? 4096 : 8192; }
-__host__ __device__ constexpr int x_stages(int epi, int w) { return (w == 2 ? 3 : 5) + (epi == kEpiDw ? 1 : 0); }
-__host__ __device__ constexpr int x_smem(int epi, int w) {
-  return x_stages(epi, w) * x_stage_bytes(w) + x_epi_warps(epi) * x_box_bytes(epi) + 1024;
+// Staging of an epilogue warp: boxes of 32 rows of 128 bytes (64 bytes in the backward), one for dW, a pair for the others, three for the
+// backward of kept activations (its third result, held in registers until a box was free, made it spill: 35 000 clocks a tile instead of 18 000).
+__host__ __device__ constexpr int x_box_bytes(int epi, int form) { return epi == kEpiDact && form == kKeep8 ? 6144 : epi == kEpiDw || epi == kEpiDact ? 4096 : 8192; }
+__host__ __device__ constexpr int x_stages(int epi, int w, int form) { return (w == 2 ? 3 : 5) + (epi == kEpiDw ? 1 : 0) - (epi == kEpiDact && form == kKeep8 ? 1 : 0); }
+__host__ __device__ constexpr int x_smem(int epi, int w, int form) {
+  return x_stages(epi, w, form) * x_stage_bytes(w) + x_epi_warps(epi) * x_box_bytes(epi, form) + 1024;
 }
 
 struct XSmem {
@@ -204,7 +205,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
                  char* __restrict__ out, char* __restrict__ pre_out, const char* __restrict__ pre_in, ExpertArgs a, unsigned* error_flag) {
   constexpr bool kDw = EPI == kEpiDw, kA_MN = kDw, kParts = kDw && W == 1;
   constexpr int kEpiWarps = x_epi_warps(EPI), kBK = Form == kInt8 ? 2 * kXBK : kXBK;      // depth of a slice: 128 bytes
-  constexpr int kStages = x_stages(EPI, W), kStageBytes = x_stage_bytes(W);
+  constexpr int kStages = x_stages(EPI, W, Form), kStageBytes = x_stage_bytes(W);
   constexpr int kTileN = EPI == kEpiGlu ? 128 : kXTile;               // output columns of a tile
   extern __shared__ unsigned char xsm_raw[];
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(xsm_raw) + 1023) & ~(uintptr_t)1023);
@@ -381,7 +382,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
       if (EPI == kEpiGlu && pre_out) expert_zero_behind(a, sm.rows, pre_out, 4 * (size_t)a.N, kXTile, worker, workers);
       if (EPI == kEpiDact && Form == kKeep8 && pre_out) expert_zero_behind(a, sm.rows, pre_out, 2 * (size_t)a.N, kXTile, worker, workers);
     }
-    unsigned char* stage = base + kStages * kStageBytes + (size_t)(warp - 2) * x_box_bytes(EPI);
+    unsigned char* stage = base + kStages * kStageBytes + (size_t)(warp - 2) * x_box_bytes(EPI, Form);
     const uint32_t acc_empty0 = map_to_rank(smem_u32(&sm.acc_empty[0]), 0);
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
     // A lane computes 128 bytes of its own row; a box of 32 such rows turns them into whole lines for memory.  16-byte chunk c
@@ -633,23 +634,28 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
           }
         } else {
           if constexpr (Form == kKeep8) {
-            // As below, with g and u from their integers.  h = silu(g) u is formed again on the way and leaves through a tile store of 64
-            // columns once dg and du have left the boxes.
-            uint32_t h[32];
-#pragma unroll
+            // As below, with g and u from their integers: a lane lays them into its row of the third box, eight of g and of u to 16 bytes, which h =
+            // silu(g) u, formed again on the way, then takes over.
+#pragma unroll 1
             for (int c0 = 0; c0 < kCols; c0 += 32) {
-              if (c0 == 0) { if (lane == 0) bulk_wait_read<0>(); __syncwarp(); }      // the boxes are free of the last tile's h
+              unsigned char* row = stage + lane * kRow;
 #pragma unroll
+              for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<uint4*>(row + 64 * kRow + ((i ^ swz(lane)) << 4)) = make_uint4(kg[2 * i], kg[2 * i + 1], ku[2 * i], ku[2 * i + 1]);
+              const float2 step_g = both(sg), step_u = both(su);
+              if (c0 + 32 < kCols) fetch8(col0 + c0 + 32);             // on its way from here on
+#pragma unroll 1
               for (int i = 0; i < 4; ++i) {
-                uint32_t u[8];
+                uint32_t u[8], dg[4], du[4], h[4];
+                uint4* at = reinterpret_cast<uint4*>(row + ((i ^ swz(lane)) << 4));
+                const uint4 kept = at[64 * kRow / 16];
                 tmem_ld8(acc + c0 + 8 * i, u);
-                uint32_t dg[4], du[4];
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {                          // columns 2 p and 2 p + 1 of the eight, packed
-                  const uint32_t gw = kg[2 * i + (p >> 1)] ^ 0x80808080u, uw = ku[2 * i + (p >> 1)] ^ 0x80808080u;
+                  const uint32_t gw = (p < 2 ? kept.x : kept.y) ^ 0x80808080u, uw = (p < 2 ? kept.z : kept.w) ^ 0x80808080u;
                   const int b = (p & 1) * 2;
-                  const float2 g = mul2(add2(make_float2(byte8_raw(gw, b), byte8_raw(gw, b + 1)), both(-kByte8Zero)), both(sg));
-                  const float2 up = mul2(add2(make_float2(byte8_raw(uw, b), byte8_raw(uw, b + 1)), both(-kByte8Zero)), both(su));
+                  const float2 g = mul2(add2(make_float2(byte8_raw(gw, b), byte8_raw(gw, b + 1)), both(-kByte8Zero)), step_g);
+                  const float2 up = mul2(add2(make_float2(byte8_raw(uw, b), byte8_raw(uw, b + 1)), both(-kByte8Zero)), step_u);
                   const float2 dh = make_float2(keep_row ? __uint_as_float(u[2 * p]) : 0.f, keep_row ? __uint_as_float(u[2 * p + 1]) : 0.f);
                   float2 t = mul2(g, both(-1.44269504f)), s;           // s = 1 / (1 + 2^t), as sigmoid_f<true>
                   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t.x) : "f"(t.x));
@@ -660,27 +666,17 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
                   const float2 gs = mul2(g, s), slope = fma2(g, fma2(s, both(-1.f), both(1.f)), both(1.f));
                   const float2 a = mul2(mul2(mul2(dh, up), s), slope), c = mul2(dh, gs), hv = mul2(gs, up);
                   dg[p] = pack_bf16(a.x, a.y); du[p] = pack_bf16(c.x, c.y);
-                  h[c0 / 2 + 4 * i + p] = pack_bf16(hv.x, hv.y);
+                  h[p] = pack_bf16(hv.x, hv.y);
                 }
-                *reinterpret_cast<uint4*>(stage + lane * kRow + ((i ^ swz(lane)) << 4)) = make_uint4(dg[0], dg[1], dg[2], dg[3]);
-                *reinterpret_cast<uint4*>(stage + (32 + lane) * kRow + ((i ^ swz(lane)) << 4)) = make_uint4(du[0], du[1], du[2], du[3]);
+                at[0] = make_uint4(dg[0], dg[1], dg[2], dg[3]);
+                at[32 * kRow / 16] = make_uint4(du[0], du[1], du[2], du[3]);
+                at[64 * kRow / 16] = make_uint4(h[0], h[1], h[2], h[3]);
               }
-              if (c0 + 32 < kCols) fetch8(col0 + c0 + 32);             // on its way while the results leave
               char* dst = out + (row0 * 2 * a.N + col0 + c0) * 2;
               const int left = (a.N - col0 - c0) * 2;
               box_out(stage, dst, (size_t)a.N * 4, rows, left);
               box_out(stage + 32 * kRow, dst + (size_t)a.N * 2, (size_t)a.N * 4, rows, left);
-            }
-            if (pre_out) {
-#pragma unroll
-              for (int i = 0; i < 8; ++i)
-                *reinterpret_cast<uint4*>(stage + lane * 128 + ((i ^ (lane & 7)) << 4)) = make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
-              fence_proxy_async();
-              __syncwarp();
-              if (lane == 0) {
-                if (rows > 0 && col0 < a.N) tma_store_3d(&tO0, col0, y0, x.e, smem_u32(stage));
-                bulk_commit();
-              }
+              if (pre_out) box_out(stage + 64 * kRow, pre_out + (row0 * a.N + col0 + c0) * 2, (size_t)a.N * 2, rows, left);
             }
           } else {
           // dh in the accumulator; g and u sit in a pair of boxes, which dg and du then leave from
