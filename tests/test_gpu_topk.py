@@ -253,7 +253,8 @@ def backward(ms, l, idx, dw, col, how):
     return dl.cpu().to(F64)
 
 
-@pytest.mark.parametrize("T, E, k, groups, keep", SHAPES)
+@pytest.mark.parametrize("T, E, k, groups, keep", SHAPES + [(MANY, E, k, 1, 1) for E, k in ((1, 1), (2, 2), (8, 2), (12, 3), (16, 8), (32, 8), (31, 8), (33, 5), (40, 6),
+                                                                                            (64, 8), (96, 1), (100, 7), (127, 8), (128, 8))])
 @pytest.mark.parametrize("sigmoid", [False, True])
 @pytest.mark.parametrize("aux", [False, True])
 def test_backward(ms, T, E, k, groups, keep, sigmoid, aux):
@@ -306,13 +307,20 @@ def test_backward_skips_empty_pairs(ms):
     g = torch.Generator().manual_seed(4)
     l, dw = torch.randn(20, 16, generator=g), torch.randn(20, 3, generator=g)
     idx = torch.rand(20, 16, generator=g).topk(3, 1).indices.sort(1).values
+    empty_pairs(ms, l, dw, idx, lambda got: got)
+    tile = lambda t: t.repeat(131, 1)  # noqa: E731
+    for j in (0, 7, 130):
+        empty_pairs(ms, l, dw, idx, lambda all_rows: all_rows.view(131, 20, 16)[j], tile)
+
+
+def empty_pairs(ms, l, dw, idx, part, tile=lambda t: t):
     short = idx.clone()
     short[:, 2] = -1
     short[5] = -1
     short[6, 1] = 16
     for sigmoid in (False, True):
         how = ms.make_topk(ms.SIGMOID if sigmoid else ms.SOFTMAX)
-        got = backward(ms, l, short, dw, None, how)
+        got = part(backward(ms, tile(l), tile(short), tile(dw), None, how))
         want = dl64(l, idx[:, :2], dw[:, :2], None, sigmoid, True, 1.0)
         rows = [i for i in range(20) if i not in (5, 6)]
         assert (got[rows] - want[rows]).abs().max() <= 1e-5 * want.abs().max()
