@@ -435,3 +435,56 @@ def test_int8_experts_approach_the_bf16_experts(ms):
     # of 3 to 4 rms, of 128 gated values up to 9: at most 1 %, 1 %, 2 % and 1 % of the rms of x, w_up, h and w_down; x and w_up reach h
     # twice (g and u, each with a slope below 1.1).  Independent: the root of the squares' sum is below 3.5 %.
     assert (y.float() - y16.float()).norm() <= 0.035 * y16.float().norm()
+
+
+@pytest.mark.parametrize("C", [5, 300])
+@pytest.mark.parametrize("load", [0, -2])
+def test_no_rows_at_all(ms, C, load):
+    """Every expert without a row: zeros out, nothing of the kept buffer touched."""
+    E, K, f = 3, 64, 40
+    ctx = context(ms, E, C)
+    n = torch.full((E,), load, dtype=torch.int32, device=DEV)
+    nan = lambda *s, dtype=BF16: torch.full(s, float("nan"), dtype=dtype, device=DEV)  # noqa: E731
+    q = lambda *s: torch.full(s, 5, dtype=torch.int8, device=DEV)  # noqa: E731
+    w = torch.ones(E, K, 2 * f, dtype=BF16, device=DEV)
+    y, h, dpre, h2 = nan(E, C, f), nan(E, C, f), nan(E, C, 2 * f), nan(E, C, f)
+    keep = torch.full((ms.keep8_bytes(ctx, f),), 77, dtype=torch.uint8, device=DEV)
+    ms.expert_gemm_q8(ctx, q(E, C, K), nan(E, C, dtype=torch.float32), q(E, f, K), nan(E, f, dtype=torch.float32), n, y, K, f)
+    assert (y == 0).all()
+    ms.expert_glu_q8(ctx, q(E, C, K), nan(E, C, dtype=torch.float32), q(E, 2 * f, K), nan(E, 2 * f, dtype=torch.float32), n, h, K, f)
+    assert (h == 0).all()
+    h.fill_(float("nan"))
+    ms.expert_glu_keep8(ctx, nan(E, C, K), w, n, keep, h, K, f)
+    ms.expert_glu_bwd_keep8(ctx, nan(E, C, K), torch.ones(E, f, K, dtype=BF16, device=DEV), keep, n, dpre, h2, K, f)
+    assert (h == 0).all() and (dpre == 0).all() and (h2 == 0).all() and (keep == 77).all()
+    out, s = q(E, C, K), nan(E, C, dtype=torch.float32)
+    ms.expert_quant(ctx, nan(E, C, K), n, out, s, K)
+    assert (out == 0).all() and (s == 0).all() and ms.check_internal(ctx) == 0
+
+
+def test_one_call_after_another_on_dirty_shared_memory(ms):
+    """The same products again and again, between products of other sizes and forms: bit for bit the same."""
+    E, C, K, f = 4, 300, 272, 104
+    g = torch.Generator().manual_seed(8)
+    ctx = context(ms, E, C)
+    few = context(ms, E, 20)
+    load, few_load = torch.tensor([300, 129, 0, 77], dtype=torch.int32, device=DEV), torch.tensor([20, 1, 0, 17], dtype=torch.int32, device=DEV)
+    x, w, wd = (torch.randn(*s, generator=g).to(BF16).to(DEV) for s in ((E, C, K), (E, K, 2 * f), (E, f, K)))
+    xq, wq = ints(g, E, C, K).to(DEV), ints(g, E, 2 * f, K).to(DEV)
+    xs, ws = torch.rand(E, C, generator=g).to(DEV), (torch.rand(E, 2 * f, generator=g) * 1e-3).to(DEV)
+
+    def once(c, n, ld):
+        new = lambda *s: torch.full(s, float("nan"), dtype=BF16, device=DEV)  # noqa: E731
+        rows = lambda t: t[:, :n].contiguous()  # noqa: E731
+        keep = torch.zeros(ms.keep8_bytes(c, f), dtype=torch.uint8, device=DEV)
+        h, dpre, h2, hq = new(E, n, f), new(E, n, 2 * f), new(E, n, f), new(E, n, f)
+        ms.expert_glu_keep8(c, rows(x), w, ld, keep, h, K, f)
+        ms.expert_glu_q8(c, rows(xq), rows(xs), wq, ws, ld, hq, K, f)
+        ms.expert_glu_bwd_keep8(c, rows(x), wd, keep, ld, dpre, h2, K, f)
+        return h, hq, dpre, h2, keep
+
+    want, few_want = once(ctx, C, load), once(few, 20, few_load)
+    for _ in range(20):
+        for c, n, ld, ref in ((few, 20, few_load, few_want), (ctx, C, load, want)):
+            assert all(torch.equal(a, b) for a, b in zip(once(c, n, ld), ref))
+    assert ms.check_internal(ctx) == 0 and ms.check_internal(few) == 0
