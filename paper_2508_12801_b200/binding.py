@@ -384,19 +384,25 @@ def keep8_bytes(ctx, d_ff) -> int:
     return int(n.value)
 
 
+def _keep8_numel(ctx, d_ff):
+    """keep8_bytes without the call: integers [E, C, 2, w], from a multiple of 256 on the scales [E, 2 w / 32, C]."""
+    rows, w = ctx.params.E * ctx.capacity, (d_ff + 31) // 32 * 32
+    return (rows * 2 * w + 255) // 256 * 256 + rows * (w // 4)
+
+
 def expert_glu_keep8(ctx, x, w_up, expert_load, keep, h, d_in, d_ff, w_layout=0, stream=None):
     """expert_glu with [g | u] kept in 8 bits."""
     io, rows = ctx.io_torch, ctx.params.E * ctx.capacity
     _call(ctx, "maxscore_expert_glu_keep8", _lib.maxscore_expert_glu_keep8, _need(ctx, "x", x, io, rows * d_in),
           _need(ctx, "w_up", w_up, io, ctx.params.E * d_in * 2 * d_ff), _need(ctx, "expert_load", expert_load, torch.int32, ctx.params.E),
-          _need(ctx, "keep", keep, torch.uint8, keep8_bytes(ctx, d_ff)), _need(ctx, "h", h, io, rows * d_ff), d_in, d_ff, w_layout, stream=stream)
+          _need(ctx, "keep", keep, torch.uint8, _keep8_numel(ctx, d_ff)), _need(ctx, "h", h, io, rows * d_ff), d_in, d_ff, w_layout, stream=stream)
 
 
 def expert_glu_bwd_keep8(ctx, dy, w_down, keep, expert_load, dpre, h, d_out, d_ff, w_layout=0, stream=None):
     """expert_glu_bwd from what expert_glu_keep8 kept; h (may be None) receives silu(g) u formed again."""
     io, rows = ctx.io_torch, ctx.params.E * ctx.capacity
     _call(ctx, "maxscore_expert_glu_bwd_keep8", _lib.maxscore_expert_glu_bwd_keep8, _need(ctx, "dy", dy, io, rows * d_out),
-          _need(ctx, "w_down", w_down, io, ctx.params.E * d_ff * d_out), _need(ctx, "keep", keep, torch.uint8, keep8_bytes(ctx, d_ff)),
+          _need(ctx, "w_down", w_down, io, ctx.params.E * d_ff * d_out), _need(ctx, "keep", keep, torch.uint8, _keep8_numel(ctx, d_ff)),
           _need(ctx, "expert_load", expert_load, torch.int32, ctx.params.E), _need(ctx, "dpre", dpre, io, rows * 2 * d_ff),
           _need(ctx, "h", h, io, rows * d_ff, optional=True), d_out, d_ff, w_layout, stream=stream)
 

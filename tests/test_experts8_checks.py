@@ -104,6 +104,12 @@ def test_kept_scales_count_as_the_buffer():
     assert ms._lib.maxscore_keep8_bytes(host_ctx(io_dtype=ms.F32), 40, C.byref(n)) == UNSUPPORTED
 
 
+@pytest.mark.parametrize("E, T, k, d_ff", [(4, 8, 2, 40), (1, 1, 1, 8), (128, 65536, 8, 1024), (33, 777, 5, 1000), (3, 100, 3, 31 * 8)])
+def test_size_of_a_kept_buffer(E, T, k, d_ff):
+    ctx = types.SimpleNamespace(handle=host_ctx(E=E, T=T, k=k), params=ms.make_params(T, 64, E, k), capacity=ms.capacity(ms.make_params(T, 64, E, k)))
+    assert ms._keep8_numel(ctx, d_ff) == ms.keep8_bytes(ctx, d_ff)
+
+
 def test_binding_checks_tensors():
     ctx = types.SimpleNamespace(device_index=-1, device="cpu", params=ms.make_params(8, 64, 4, 2), capacity=4, io_torch=torch.bfloat16, handle=None)
     x = torch.zeros(4, 4, 64, dtype=torch.bfloat16)
