@@ -162,18 +162,25 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
         if (first < a.N && r < rows) steps = __ldg(a.keep_scale + ((size_t)e * 2 * blocks + (lane >> 4) * blocks + first / kKeepBlock) * a.C + r);
       };
       if constexpr (EPI == kEpiDact) fetch(0);
+      // integers: the column's scale and the scales of 16 rows, those of the first rows ahead of the accumulator too
+      float col_scale = 0.f, first_rows = 0.f;
+      auto row_scales = [&](int c0) { return c0 + (lane & 15) < rows ? __ldg(a.x_scale + row0 + c0 + (lane & 15)) : 0.f; };
+      if constexpr (Form == kInt8) {
+        if (col < a.N) col_scale = __ldg(a.w_scale + (EPI == kEpiGlu ? (size_t)e * 2 * a.N + (q >= 2 ? a.N : 0) : (size_t)e * a.N) + col);
+        first_rows = row_scales(0);
+        __syncwarp();
+      }
       ok = mbar_wait_bounded(&sm.acc_full[buf], (uint32_t)((turn >> 1) & 1));
       if (EPI == kEpiGlu) ok = all_epilogue_threads(ok);   // (also: the last item's values have been read from `up`)
       if (!ok) break;
       tc_fence_after();
-      float col_scale = 0.f;
-      if (Form == kInt8 && col < a.N) col_scale = __ldg(a.w_scale + (EPI == kEpiGlu ? (size_t)e * 2 * a.N + (q >= 2 ? a.N : 0) : (size_t)e * a.N) + col);
       if constexpr (Form != kBf16) {
         // What a row costs here bounds these forms from a few dozen rows on.  Results pass through 16-row boxes so that they leave as
         // 16-byte stores, and what belongs to a row (its scale, a block's step) is read or worked out once, by one lane.
         unsigned char* box = base + few_ring(Form) + (EPI == kEpiGlu ? pad * 256 : 0) + (warp - 2) * few_box(Form);
         auto take = [&](int c0, float (&r)[16]) {                      // 16 rows of the column; integers become the values they stand for
-          const float xs = Form == kInt8 && c0 + (lane & 15) < rows ? __ldg(a.x_scale + row0 + c0 + (lane & 15)) : 0.f;
+          float xs = first_rows;
+          if (Form == kInt8 && c0 > 0) xs = row_scales(c0);
           __syncwarp();
           tmem_ld16(acc + c0, r);
           if constexpr (Form == kInt8) {
