@@ -30,6 +30,7 @@ struct FewSmem {
   uint32_t tmem;
   int failed;
   int rows[kMaxE], first[kMaxE + 1];     // rows in use; items before each expert
+  int start;                             // expert of the CTA's first item
 };
 
 // Whether a condition holds on all 128 epilogue threads; a barrier for them too.
@@ -67,7 +68,7 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
     fence_barrier_init();
   }
   if (warp == 1) tmem_alloc(&sm.tmem, tmem_cols);
-  if (warp == 2) expert_prefix(a, sm.rows, sm.first, [&](int r) { return r > 0 ? ntn : 0; });
+  if (warp == 2) expert_prefix(a, sm.rows, sm.first, blockIdx.x, &sm.start, [&](int r) { return r > 0 ? ntn : 0; });
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -76,7 +77,7 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
 
   if (warp == 0) {
     if (lane == 0) {
-      int s = 0, e = 0; uint32_t ph = 1; bool ok = true;
+      int s = 0, e = sm.start; uint32_t ph = 1; bool ok = true;
       for (int t = blockIdx.x; t < total && ok; t += gridDim.x) {
         while (t >= sm.first[e + 1]) ++e;
         const int n0 = (t - sm.first[e]) * kCols;
@@ -142,7 +143,7 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
       if (EPI == kEpiDact && pre_out) expert_zero_behind_rows(a, sm.rows, (char*)pre_out, 2 * (size_t)a.N, w, ws);
       if (EPI == kEpiGlu && pre_out) expert_zero_behind_rows(a, sm.rows, (char*)pre_out, 4 * (size_t)a.N, w, ws);
     }
-    int turn = 0, e = 0; bool ok = true;
+    int turn = 0, e = sm.start; bool ok = true;
     for (int t = blockIdx.x; t < total; t += gridDim.x, ++turn) {
       while (t >= sm.first[e + 1]) ++e;
       const int rows = sm.rows[e], buf = turn & 1;

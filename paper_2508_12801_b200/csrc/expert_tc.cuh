@@ -127,6 +127,7 @@ struct XSmem {
   uint32_t tmem;
   int failed;
   int rows[kMaxE], first[kMaxE + 1];     // rows in use; tiles before each expert
+  int start;                             // expert of the pair's first tile
 };
 
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&u)[8]) {
@@ -153,7 +154,7 @@ template <int W>
 struct XWalk {
   const XSmem& sm; const ExpertArgs& a; int ntn, ntw; int t, step, e;
   __device__ XWalk(const XSmem& s, const ExpertArgs& args, int ntn_, int t0, int step_)
-      : sm(s), a(args), ntn(ntn_), ntw((ntn_ + W - 1) / W), t(t0), step(step_), e(0) {}
+      : sm(s), a(args), ntn(ntn_), ntw((ntn_ + W - 1) / W), t(t0), step(step_), e(s.start) {}
   __device__ bool next(XTile& x) {
     if (t >= sm.first[a.E]) return false;
     while (t >= sm.first[e + 1]) ++e;
@@ -164,9 +165,10 @@ struct XWalk {
   }
 };
 
-// Rows in use and tile counts of every expert, by the first warp; `per` = tiles of an expert with rows r.
+// Rows in use and tile counts of every expert, by one warp; `per` = tiles of an expert with rows r.  start: the expert of tile t0 (stepping there from
+// the first expert costs a microsecond where few of many experts have rows).
 template <typename F>
-__device__ __forceinline__ void expert_prefix(const ExpertArgs& a, int* rows, int* first, F per) {
+__device__ __forceinline__ void expert_prefix(const ExpertArgs& a, int* rows, int* first, int t0, int* start, F per) {
   const int lane = threadIdx.x & 31;
   int mine[kMaxE / 32], sum = 0;
 #pragma unroll
@@ -183,13 +185,16 @@ __device__ __forceinline__ void expert_prefix(const ExpertArgs& a, int* rows, in
     const int v = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += v;
   }
-  int run = incl - sum;
+  int run = incl - sum, before = 0;
 #pragma unroll
   for (int i = 0; i < kMaxE / 32; ++i) {
     const int e = lane * (kMaxE / 32) + i;
     if (e <= a.E) first[e] = run;
     run += mine[i];
+    before += e < a.E && run <= t0;
   }
+  before = __reduce_add_sync(0xffffffffu, before);
+  if (lane == 0) *start = before;
   if (lane == 31 && a.E == kMaxE) first[kMaxE] = run;
 }
 
@@ -227,7 +232,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   if (warp == 2)
-    expert_prefix(a, sm.rows, sm.first, [&](int r) { return (kDw ? ntm_dw : (r + kXTile - 1) / kXTile) * ((ntn + W - 1) / W); });
+    expert_prefix(a, sm.rows, sm.first, blockIdx.x >> 1, &sm.start, [&](int r) { return (kDw ? ntm_dw : (r + kXTile - 1) / kXTile) * ((ntn + W - 1) / W); });
   tc_fence_before();
   __syncwarp();
   cluster_sync();                                       // barriers of both CTAs are ready, shared memory written above is seen
