@@ -10,7 +10,7 @@
 // E 64, 2048 -> 2048): those would be half empty.
 // Gated form: 64 gate and 64 up columns share a tile; the up half passes through shared memory to the threads of the gate half.
 // 8-bit forms (integers; kept activations, forward and backward): half the weight bytes or all of them, and epilogues of their own.
-// E 64, 2048 -> 1024: integers, gated, 16 rows 49 us (5.5 TB/s), one token of eight experts 12; kept, 16 rows 88, its backward 51 (5.4 TB/s).
+// E 64, 2048 -> 1024: integers, gated, 16 rows 49 us (5.5 TB/s), one token of eight experts 10; kept, 16 rows 88, its backward 51 (5.4 TB/s).
 #pragma once
 #include "expert_tc.cuh"
 
@@ -232,10 +232,10 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
             __syncwarp();
           }
         } else if constexpr (EPI == kEpiDact) {
-          const unsigned char* kept = box + 3072;
+          const unsigned char* kept = box + 3 * 1024;
           for (int c0 = 0; c0 < rows; c0 += 16) {
-            *reinterpret_cast<uint4*>(box + 3072 + lane * 16) = kg;
-            *reinterpret_cast<uint4*>(box + 3584 + lane * 16) = ku;
+            *reinterpret_cast<uint4*>(box + 3 * 1024 + lane * 16) = kg;
+            *reinterpret_cast<uint4*>(box + 3 * 1024 + 512 + lane * 16) = ku;
             const float now = steps;
             __syncwarp();
             if (c0 + 16 < rows) fetch(c0 + 16);
