@@ -117,6 +117,18 @@ __device__ __noinline__ uint32_t topk_choose_64(const float* __restrict__ row, c
     in[j] = j < vpt && e0 + j < a.E;
     l[j] = in[j] ? (double)__ldg(row + e0 + j) : -INFINITY;
   }
+  // a row of one value with one bias (padded tokens, and early training): the lowest groups, and of them the lowest experts
+  const double first_l = __shfl_sync(0xffffffffu, l[0], 0);
+  const float first_b = bias ? __ldg(bias) : 0.f;
+  bool even = true;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) even = even && (!in[j] || (l[j] == first_l && (!bias || __ldg(bias + e0 + j) == first_b)));
+  if (__all_sync(0xffffffffu, even)) {
+    uint32_t lowest = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) if (in[j] && e0 + j < a.k) lowest |= 1u << j;
+    return lowest;
+  }
   if (a.sigmoid) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = 1.0 / (1.0 + exp(-l[j]));

@@ -196,6 +196,23 @@ def test_many_tokens(ms, E, k, groups, keep, sigmoid, with_bias):
     check(ms, l, bias, k, sigmoid, False, 1.0, groups, keep)
 
 
+@pytest.mark.parametrize("T", [130, MANY])
+@pytest.mark.parametrize("E, groups, keep", [(128, 8, 4), (33, 3, 2), (64, 1, 1), (8, 4, 1)])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_rows_of_one_value(ms, T, E, groups, keep, sigmoid):
+    """Padded tokens: every expert has the same logit; between them ordinary rows and rows that differ in the last bit of one expert."""
+    g = torch.Generator().manual_seed(E)
+    l = torch.randn(T, E, generator=g)
+    l[::2] = torch.randn(len(l[::2]), 1, generator=g)
+    l[4::10, E // 2] = torch.nextafter(l[4::10, E // 2], torch.tensor(9.0))
+    l[6::10] = 0.0
+    l[6::10, ::3] = -0.0
+    k = min(8, E // groups * keep)
+    for bias in (None, torch.zeros(E), torch.full((E,), 0.3), torch.randn(E, generator=g) * 0.05):
+        for pairs in ([False, True] if groups > 1 else [False]):
+            check(ms, l, bias, k, sigmoid, groups=groups, keep=keep, pairs=pairs)
+
+
 @pytest.mark.parametrize("sigmoid", [False, True])
 def test_many_tokens_that_only_64_bits_tell_apart(ms, sigmoid):
     g = torch.Generator().manual_seed(5)
