@@ -172,6 +172,7 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
         __syncwarp();
       }
       ok = mbar_wait_bounded(&sm.acc_full[buf], (uint32_t)((turn >> 1) & 1));
+      if (EPI != kEpiGlu && Form != kBf16) ok = __all_sync(0xffffffffu, ok);      // a wait that gave up ends the whole warp's work
       if (EPI == kEpiGlu) ok = all_epilogue_threads(ok);   // (also: the last item's values have been read from `up`)
       if (!ok) break;
       tc_fence_after();

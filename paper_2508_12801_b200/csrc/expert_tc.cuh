@@ -546,6 +546,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
         if constexpr (EPI == kEpiDact) { if constexpr (Form == kKeep8) fetch8(col0); else fetch(row0, rows, col0); }
         if (nkb > 0) {
           ok = mbar_wait_bounded(&sm.acc_full[buf], (acc_ph >> buf) & 1);
+          if constexpr (Form != kBf16) ok = __all_sync(0xffffffffu, ok);      // a wait that gave up ends the whole warp's work
           if (!ok) break;
           tc_fence_after();
         }
