@@ -603,6 +603,7 @@ topk_bwd_kernel(const float* __restrict__ logits, const int32_t* __restrict__ ex
     col[j] = dscores_col && e0 + j < a.E ? __ldg(dscores_col + e0 + j) : 0.f;
     grow[e0 + j] = 0.f;
   }
+  __syncwarp();                                                        // before a first token's gradients: sigmoid without renorm has no other barrier ahead of them
   const int64_t step = gridDim.x * kTopkWarps;
   int64_t t = blockIdx.x * kTopkWarps + warp;
   float next[VPT], next_g = 0.f;
