@@ -41,10 +41,20 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t phase) {
       : "memory");
   return ok != 0;
 }
-// Bounded wait: gives up after `limit` polls and reports false, so that no kernel can spin forever.
+// Bounded wait of one lane: gives up after `limit` polls and reports false, so that no kernel can spin forever.
 __device__ __forceinline__ bool mbar_wait_bounded(uint64_t* bar, uint32_t phase, uint32_t limit = 1u << 22) {
   for (uint32_t it = 0; it < limit; ++it) {
     if (mbar_try_wait(bar, phase)) return true;
+    if (it > 64) __nanosleep(32);
+  }
+  return false;
+}
+// The same by a whole warp, with one answer for all its lanes: when the limit runs out some lanes may have seen the phase end and others not,
+// and what follows (tcgen05.ld, elect.sync, a barrier of the warp) needs all of them or none.  The vote is the loop's branch: behind the loop it
+// cost 17 ns a wait.
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t phase, uint32_t limit = 1u << 22) {
+  for (uint32_t it = 0; it < limit; ++it) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, phase))) return true;
     if (it > 64) __nanosleep(32);
   }
   return false;

@@ -114,9 +114,9 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
     for (int t = blockIdx.x; t < total && ok; t += gridDim.x, ++turn) {
       const int buf = turn & 1;
       const uint32_t acc = tmem + (uint32_t)(buf * pad);
-      ok = mbar_wait_bounded(&sm.acc_empty[buf], (uint32_t)(((turn >> 1) & 1) ^ 1));
+      ok = mbar_wait_warp(&sm.acc_empty[buf], (uint32_t)(((turn >> 1) & 1) ^ 1));
       for (int kb = 0; kb < nkb && ok; ++kb) {
-        ok = mbar_wait_bounded(&sm.full[s], ph);
+        ok = mbar_wait_warp(&sm.full[s], ph);
         if (!ok) break;
         tc_fence_after();
         const uint32_t sw = smem_u32(base) + (uint32_t)(s * stage_bytes);
@@ -171,8 +171,7 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
         first_rows = row_scales(0);
         __syncwarp();
       }
-      ok = mbar_wait_bounded(&sm.acc_full[buf], (uint32_t)((turn >> 1) & 1));
-      if (EPI != kEpiGlu && Form != kBf16) ok = __all_sync(0xffffffffu, ok);      // a wait that gave up ends the whole warp's work
+      ok = mbar_wait_warp(&sm.acc_full[buf], (uint32_t)((turn >> 1) & 1));
       if (EPI == kEpiGlu) ok = all_epilogue_threads(ok);   // (also: the last item's values have been read from `up`)
       if (!ok) break;
       tc_fence_after();

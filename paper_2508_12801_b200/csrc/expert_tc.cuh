@@ -291,8 +291,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
         if (kDw && masked) {
           // this CTA's copies land on its own barrier; rows from the load to the next multiple of 16 become zero
           good = __shfl_sync(0xffffffffu, good, 0);
-          if (good) good = mbar_wait_bounded(&sm.tail, tail_phase);
-          good = __all_sync(0xffffffffu, good);
+          if (good) good = mbar_wait_warp(&sm.tail, tail_phase);
           tail_phase ^= 1;
           if (good) {
             const int r0 = K - k0, r1 = (r0 + 15) & ~15;               // a row is 128 bytes of a box, whatever the swizzle
@@ -351,11 +350,11 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
           if (h >= x.subs) break;
           const uint32_t buf = W == 2 ? h : turn & 1;
           const uint32_t acc = tmem + buf * 256;
-          if (kb == begin) { ok = ok && mbar_wait_bounded(&sm.acc_empty[buf], (acc_ph >> buf) & 1); acc_ph ^= 1u << buf; }
+          if (kb == begin) { ok = ok && mbar_wait_warp(&sm.acc_empty[buf], (acc_ph >> buf) & 1); acc_ph ^= 1u << buf; }
           s = s0;
           uint32_t ph = full_ph;
           for (int j = 0; j < n; ++j) {
-            if (h == 0) ok = ok && mbar_wait_bounded(&sm.full[s], ph);
+            if (h == 0) ok = ok && mbar_wait_warp(&sm.full[s], ph);
             if (!ok) break;
             tc_fence_after();
             const uint64_t ad = adesc0 + (uint64_t)(s * (kStageBytes / 16)), bd = bdesc0 + (uint64_t)(s * (kStageBytes / 16) + h * 1024);
@@ -475,7 +474,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
         for (int kb = 0; kb < nkb; kb += kXPartKb, ++turn) {
           const int buf = turn & 1;
           const uint32_t acc = tmem + lanes + (uint32_t)(buf * 256 + part * kCols);
-          ok = mbar_wait_bounded(&sm.acc_full[buf], (acc_ph >> buf) & 1);
+          ok = mbar_wait_warp(&sm.acc_full[buf], (acc_ph >> buf) & 1);
           if (!ok) break;
           tc_fence_after();
 #pragma unroll
@@ -545,8 +544,7 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
         };
         if constexpr (EPI == kEpiDact) { if constexpr (Form == kKeep8) fetch8(col0); else fetch(row0, rows, col0); }
         if (nkb > 0) {
-          ok = mbar_wait_bounded(&sm.acc_full[buf], (acc_ph >> buf) & 1);
-          if constexpr (Form != kBf16) ok = __all_sync(0xffffffffu, ok);      // a wait that gave up ends the whole warp's work
+          ok = mbar_wait_warp(&sm.acc_full[buf], (acc_ph >> buf) & 1);
           if (!ok) break;
           tc_fence_after();
         }

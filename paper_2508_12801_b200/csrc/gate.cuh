@@ -81,9 +81,9 @@ gate_gemm_tc_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_consta
   }
   __syncwarp();
   // ---- epilogue: warp w reads TMEM lanes [32w, 32w+32), i.e. tokens m0 + 32w + lane ------------------
-  const bool got = mbar_wait_bounded(&sm.accum, 0);
+  const bool got = mbar_wait_warp(&sm.accum, 0) && __all_sync(0xffffffffu, !sm.failed);
   tc_fence_after();
-  if (got && !sm.failed) {
+  if (got) {
     const int row = m0 + warp * 32 + lane;
     for (int c0 = 0; c0 < Npad; c0 += 16) {
       float r[16];
@@ -103,7 +103,7 @@ gate_gemm_tc_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_consta
         }
       }
     }
-  } else if (threadIdx.x == 0) {
+  } else if (lane == 0) {
     atomicOr(error_flag, 4u);
   }
   tc_fence_before();
@@ -373,7 +373,7 @@ gate_bwd_dh_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
     bool ok = true;
     for (int nt = 0; nt < n_tiles && ok; ++nt) {
       const int buf = nt & 1;
-      ok = mbar_wait_bounded(&sm.acc_full[buf], (uint32_t)((nt >> 1) & 1));
+      ok = mbar_wait_warp(&sm.acc_full[buf], (uint32_t)((nt >> 1) & 1));
       if (!ok) break;
       tc_fence_after();
       // Staging for the TMA tile store: per warp and column half a 32-row x 128-byte box in the 128-byte
@@ -504,9 +504,9 @@ gate_bwd_dw_tc_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_cons
     umma_commit(&sm.accum);
   }
   __syncwarp();
-  const bool got = mbar_wait_bounded(&sm.accum, 0);
+  const bool got = mbar_wait_warp(&sm.accum, 0) && __all_sync(0xffffffffu, !sm.failed);
   tc_fence_after();
-  if (got && !sm.failed && num_kb > 0) {
+  if (got && num_kb > 0) {
     const int row = m0 + warp * 32 + lane;              // row of dW = column of H
     float* out = partial + ((size_t)blockIdx.y * d + row) * E;
     for (int c0 = 0; c0 < Kpad; c0 += 16) {
@@ -519,7 +519,7 @@ gate_bwd_dw_tc_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_cons
   } else if (num_kb <= 0) {
     const int row = m0 + warp * 32 + lane;
     if (row < d) for (int j = 0; j < E; ++j) partial[((size_t)blockIdx.y * d + row) * E + j] = 0.f;
-  } else if (threadIdx.x == 0) {
+  } else if (lane == 0) {
     atomicOr(error_flag, 4u);
   }
   tc_fence_before();

@@ -314,7 +314,7 @@ norm_fwd_kernel(const T* y_in, const T* src, const int32_t* __restrict__ expert_
       }
     }
   }
-  norm_ring_end(group.ok, error_flag);
+  norm_ring_end(__all_sync(0xffffffffu, group.ok), error_flag);
 }
 
 // Backward.  Tokens are cut into units that stay within one gate row; a CTA walks units with a fixed stride and keeps the
@@ -472,7 +472,7 @@ norm_bwd_kernel(const T* dr_out, const T* dh, const T* y, const T* r_out, T* __r
         if (part_pre) *reinterpret_cast<float2*>(part_pre + at) = apre[j][i];
       }
   }
-  norm_ring_end(group.ok, error_flag);
+  norm_ring_end(__all_sync(0xffffffffu, group.ok), error_flag);
 }
 
 // Column sums of up to 2 + gates partial matrices: blockIdx.y picks one (0: w_post, 1: w_pre, 2..: gate rows), a CTA 32
