@@ -347,7 +347,8 @@ maxscore_status maxscore_expert_glu_bwd(maxscore_ctx* ctx, const void* dy, const
  * not finite, scale is NaN and q zero, and so every product of that row is NaN.
  * Integers are rows of bytes, [E, C, width], with one fp32 scale per row, [E, C]; weights [E, d_out, d_in] (d_in contiguous) with
  * one per column of the product, [E, d_out].  Rows in use, rows behind them and overlaps as in the products above.
- * Products sum the integers exactly (in 32 bits; any signed bytes) and are scaled and rounded to bf16 once.
+ * Products sum the integers exactly (in 32 bits; any signed bytes), are scaled in fp32 (sums above 2^24, the two scales' product and the result
+ * round there; a product of scales outside fp32's range is no loss where the result is inside it) and rounded to bf16 once.
  * Reproducible bit for bit.  maxscore_check_internal tells whether a bounded wait gave up.
  * Errors: NULL or misaligned (16 bytes) pointers, an output that shares memory with another argument, non-positive widths,
  * w_layout not 0 or 1 -> MAXSCORE_ERR_INVALID_ARG; fp32 I/O, integer rows (d_model, width, d_in) that are no multiple of 16 or not below

@@ -185,8 +185,13 @@ expert_few_kernel(const __grid_constant__ CUtensorMap tW0, const __grid_constant
           __syncwarp();
           tmem_ld16(acc + c0, r);
           if constexpr (Form == kInt8) {
+            if (__any_sync(0xffffffffu, far8(xs) || far8(col_scale))) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) r[j] = (float)__float_as_int(r[j]) * (__shfl_sync(0xffffffffu, xs, j) * col_scale);
+              for (int j = 0; j < 16; ++j) r[j] = value8(__float_as_int(r[j]), __shfl_sync(0xffffffffu, xs, j), col_scale);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 16; ++j) r[j] = (float)__float_as_int(r[j]) * (__shfl_sync(0xffffffffu, xs, j) * col_scale);
+            }
           }
         };
         auto put = [&](int b, int j, float v) { reinterpret_cast<__nv_bfloat16*>(box + b * 1024 + j * 64)[lane] = __float2bfloat16(v); };

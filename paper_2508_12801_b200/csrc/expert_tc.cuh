@@ -512,16 +512,27 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
         const bool keep_row = kDw || y0 + lane < x.rows;              // rows behind the load come out as zeros
         float row_scale = 0.f;
         if (Form == kInt8 && keep_row) row_scale = __ldg(a.x_scale + row0 + lane);
+        // whether any scale of the warp's rows and columns lies far from 1; asked for ahead of the accumulator
+        bool far = false;
+        if constexpr (Form == kInt8) {
+          constexpr int kHalf = EPI == kEpiGlu ? 16 : 32;             // lanes for the columns, four each; gated: g's, then u's
+          static_assert(kCols == 4 * kHalf, "a lane looks at four columns");
+          const int col = col0 + (lane % kHalf) * 4;
+          const float* of = a.w_scale + (size_t)x.e * (EPI == kEpiGlu ? 2 * a.N : a.N) + (lane / kHalf) * (size_t)a.N;
+          const bool mine = far8(row_scale) || (col < a.N && far8(__ldg(reinterpret_cast<const float4*>(of + col))));
+          far = __any_sync(0xffffffffu, mine);
+        }
         // 16 columns from `col` on (of N; the weights' column `of` has column 0) as products of fp32 values: an integer is exact up to 2^24 and
         // else rounded once
-        auto unscale = [&](uint32_t (&u)[16], int col, const float* of) {
+        auto unscale = [&](uint32_t (&u)[16], int col, const float* of, auto product) {
 #pragma unroll
           for (int i = 0; i < 16; i += 4) {
             const float4 c = col + i < a.N ? __ldg(reinterpret_cast<const float4*>(of + col + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
-            u[i] = __float_as_uint((float)(int)u[i] * (row_scale * c.x)); u[i + 1] = __float_as_uint((float)(int)u[i + 1] * (row_scale * c.y));
-            u[i + 2] = __float_as_uint((float)(int)u[i + 2] * (row_scale * c.z)); u[i + 3] = __float_as_uint((float)(int)u[i + 3] * (row_scale * c.w));
+            u[i] = product(u[i], c.x); u[i + 1] = product(u[i + 1], c.y); u[i + 2] = product(u[i + 2], c.z); u[i + 3] = product(u[i + 3], c.w);
           }
         };
+        auto near_1 = [&](uint32_t u, float c) { return __float_as_uint((float)(int)u * (row_scale * c)); };
+        auto anywhere = [&](uint32_t u, float c) { return __float_as_uint(value8((int)u, row_scale, c)); };
         uint32_t kg[8] = {}, ku[8] = {};                               // kKeep8: 32 columns of the row's g and u, and their steps
         float sg = 0.f, su = 0.f;
         auto fetch8 = [&](int col) {
@@ -568,15 +579,27 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
         } else if constexpr (EPI == kEpiPlain) {
 #pragma unroll 1
           for (int c0 = 0; c0 < kCols; c0 += 64) {
-            uint32_t u[4][16];
+            if (far) {
+              unsigned char* to = next_box();
+#pragma unroll 1
+              for (int i = 0; i < 4; ++i) {
+                uint32_t u[16];
+                tmem_ld16_issue(acc + c0 + 16 * i, u);
+                tmem_ld_wait();
+                unscale(u, col0 + c0 + 16 * i, a.w_scale + (size_t)x.e * a.N, anywhere);
+                put16(to, i, u, keep_row);
+              }
+            } else {
+              uint32_t u[4][16];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) tmem_ld16_issue(acc + c0 + 16 * i, u[i]);
-            tmem_ld_wait();
-            unsigned char* to = next_box();
+              for (int i = 0; i < 4; ++i) tmem_ld16_issue(acc + c0 + 16 * i, u[i]);
+              tmem_ld_wait();
+              unsigned char* to = next_box();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if constexpr (Form == kInt8) unscale(u[i], col0 + c0 + 16 * i, a.w_scale + (size_t)x.e * a.N);
-              put16(to, i, u[i], keep_row);
+              for (int i = 0; i < 4; ++i) {
+                if constexpr (Form == kInt8) unscale(u[i], col0 + c0 + 16 * i, a.w_scale + (size_t)x.e * a.N, near_1);
+                put16(to, i, u[i], keep_row);
+              }
             }
             box_store(&tO0, col0 + c0, y0, x.e, rows > 0 && col0 + c0 < a.N);
           }
@@ -593,7 +616,8 @@ expert_tc_kernel(const __grid_constant__ CUtensorMap tA, const __grid_constant__
               tmem_ld_wait();
               if constexpr (Form == kInt8) {
                 const float* of = a.w_scale + (size_t)x.e * 2 * a.N;
-                unscale(g, col0 + 16 * i, of); unscale(u, col0 + 16 * i, of + a.N);
+                if (far) { unscale(g, col0 + 16 * i, of, anywhere); unscale(u, col0 + 16 * i, of + a.N, anywhere); }
+                else { unscale(g, col0 + 16 * i, of, near_1); unscale(u, col0 + 16 * i, of + a.N, near_1); }
               }
               if (what == 0) {
 #pragma unroll

@@ -20,6 +20,22 @@ __device__ __forceinline__ Step8 step8(uint32_t amax_bits) {
   else if (amax >= 0x1p-118f) { s.inv = 127.f / amax; s.scale = amax / 127.f; }
   return s;
 }
+// What an integer sum stands for: sum * (row's scale * column's).  Scales of quantised bf16 lie anywhere from 2^-125 to 2^121, so the product of two
+// can leave fp32's normal range where the result does not; the sum is then multiplied by the smaller scale first, which neither loses bits (a sum is a
+// whole number below 2^31: where the product is subnormal, it is exact) nor overflows unless the result does.  NaN stays NaN.
+__device__ __forceinline__ float value8(int sum, float row, float col) {
+  const float both = row * col;
+  if (fabsf(both) >= 0x1p-126f && fabsf(both) <= 3.402823466e38f) return (float)sum * both;
+  const bool first = fabsf(row) < fabsf(col);
+  return (float)sum * (first ? row : col) * (first ? col : row);
+}
+// Whether a scale needs that care: products of two others (2^-63 to 2^63, and 0) stay in range, and then value8 is sum * (row * col), bit for bit.
+// Tiles without such a scale are multiplied that way (a vote a tile; value8 for every value took 2 227 us where this takes 2 050: E 128, C 4096, 1024 -> 4096).
+__device__ __forceinline__ bool far8(float scale) {
+  const uint32_t u = __float_as_uint(scale) & 0x7fffffffu;
+  return u != 0 && u - 0x20000000u > 0x5f000000u - 0x20000000u;
+}
+__device__ __forceinline__ bool far8(float4 s) { return far8(s.x) || far8(s.y) || far8(s.z) || far8(s.w); }
 __device__ __forceinline__ uint32_t round8(float x, float inv) { return __float_as_uint(fmaf(x, inv, 12582912.f)); }      // the low byte
 __device__ __forceinline__ uint32_t pack8(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
