@@ -272,7 +272,9 @@ maxscore_status maxscore_gate_bwd(maxscore_ctx* ctx, const void* hidden, const v
  * Equal values go to the lowest index.  Values are compared as if computed in 64 bits: bias NULL means the order of the
  * logits, which is that of s.  A logit of -inf or a bias of -inf makes an expert the last choice.  Tokens are not limited by
  * the experts' capacity here: index build, dispatch and combine leave out what does not fit.  A row with a NaN (or, with
- * softmax, +inf or nothing but -inf) gets k distinct experts all the same, and NaN where its scores are. */
+ * softmax, +inf or nothing but -inf) gets k distinct experts all the same, and NaN where its scores are: a NaN counts as nothing in
+ * its group's value, and among the experts of the groups that stay it is chosen ahead of every number.  Scores and weights are computed in fp32,
+ * each off by at most 28 + max |l - max l| steps of 2^-24 of itself (twice that with renorm); scores below 2^-126 may be 0. */
 typedef struct {
   int32_t score;         /* 0: softmax, 1: sigmoid                                                 */
   int32_t n_group;       /* divides E, at most 32; 0 or 1: no groups                               */

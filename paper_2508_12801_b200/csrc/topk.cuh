@@ -30,12 +30,23 @@ struct TopkArgs {
   float scale;
 };
 
-// Integers in the order of floats, -0 equal to 0, none of them 0, which stands for "cannot be chosen".  (NaN: first or last by its sign.)
+// Integers in the order of floats, -0 equal to 0, none of them 0, which stands for "cannot be chosen".  NaN, whatever its sign, is above infinity: a sum
+// that is not a number has the one pattern 0x7fffffff.
 __device__ __forceinline__ uint32_t order_key(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);
   return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float order_value(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
+
+// m1, m2: the two largest so far, -inf at first; x may be NaN, which counts as nothing (min.NaN hands it to a maximum that drops it)
+__device__ __forceinline__ void two_largest(float x, float& m1, float& m2) {
+  float low;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(low) : "f"(m1), "f"(x));
+  m2 = fmaxf(m2, low);
+  m1 = fmaxf(m1, x);
+}
+// value of a group; inf - inf makes it the last
+__device__ __forceinline__ float group_value(float m1, float m2, bool pairs) { return pairs ? fmaxf(m1 + m2, -INFINITY) : m1; }
 
 // e^x for x <= 0: 2^t with t = x log2(e) rounded, then what the rounding left of the exponent as a factor 1 + r ln 2.  Off by 2^-22
 // (the approximation of 2^t) and some 2^-24 (the products) of itself; below 2^-126 it is 0.  NaN stays NaN.
@@ -141,17 +152,17 @@ __device__ __noinline__ uint32_t topk_choose_64(const float* __restrict__ row, c
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] /= sum;
   }
-  auto order = [](double x) { return x == x ? x : -INFINITY; };      // NaN comes last
-  __syncwarp();
+  if (bias) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (in[j]) {
-      v[j] = order(bias ? v[j] + (double)__ldg(bias + e0 + j) : v[j]);
-      d[e0 + j] = v[j];
-    }
-  __syncwarp();
+    for (int j = 0; j < 4; ++j) if (in[j]) v[j] += (double)__ldg(bias + e0 + j);
+  }
   uint32_t kept = 1u;
   if (a.n_group > 1) {
+    auto counts = [](double x) { return x == x ? x : -INFINITY; };    // NaN is nothing in a group's value, and a value of inf - inf the last
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) if (in[j]) d[e0 + j] = counts(v[j]);
+    __syncwarp();
     double m1 = -INFINITY, m2 = -INFINITY;
     if (lane < a.n_group) {
 #pragma unroll 4
@@ -160,7 +171,7 @@ __device__ __noinline__ uint32_t topk_choose_64(const float* __restrict__ row, c
         m2 = fmax(m2, fmin(m1, x)); m1 = fmax(m1, x);
       }
     }
-    const double value = order(a.pairs && a.group_size > 1 ? m1 + m2 : m1);
+    const double value = counts(a.pairs && a.group_size > 1 ? m1 + m2 : m1);
     int before = 0;
 #pragma unroll 4
     for (int g = 0; g < a.n_group; ++g) {
@@ -169,12 +180,12 @@ __device__ __noinline__ uint32_t topk_choose_64(const float* __restrict__ row, c
     }
     kept = __ballot_sync(0xffffffffu, lane < a.n_group && before < a.topk_group);
   }
-  if (!bias) {                                          // the experts themselves by their logits, as in fp32
-    __syncwarp();
+  // the experts themselves: without a bias by their logits, as in fp32; NaN ahead of infinity, which no finite value reaches as the largest double
+  auto order = [](double x) { return x == x ? fmin(x, 1.7976931348623157e308) : INFINITY; };
+  __syncwarp();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) if (in[j]) { v[j] = order(l[j]); d[e0 + j] = v[j]; }
-    __syncwarp();
-  }
+  for (int j = 0; j < 4; ++j) if (in[j]) { v[j] = order(bias ? v[j] : l[j]); d[e0 + j] = v[j]; }
+  __syncwarp();
   int before[4] = {};
   for (uint32_t rest = kept; rest; rest &= rest - 1) {
     const int first = (__ffs(rest) - 1) * a.group_size;
@@ -262,7 +273,7 @@ topk_fwd_scan_kernel(const float* __restrict__ logits, const float* __restrict__
     }
     bool near = false;                                                 // the same in all lanes
     if (a.n_group > 1) {
-      // the two largest of each group (NaN counts as nothing)
+      // the two largest of each group
       if (!bias && a.pairs) {
 #pragma unroll
         for (int j = 0; j < VPT; ++j) c[j] = s[j];
@@ -272,12 +283,9 @@ topk_fwd_scan_kernel(const float* __restrict__ logits, const float* __restrict__
       for (int j = 0; j < VPT; ++j) if (Full || e0 + j < a.E) grouped[e0 + j + group[j]] = c[j];
       __syncwarp();
       if (speaks)
-        for (int i = 0; i < a.group_size; ++i) {
-          const float x = grouped[lane * (a.group_size + 1) + i];
-          m2 = fmaxf(m2, fminf(m1, x)); m1 = fmaxf(m1, x);
-        }
+        for (int i = 0; i < a.group_size; ++i) two_largest(grouped[lane * (a.group_size + 1) + i], m1, m2);
       __syncwarp();
-      const uint32_t mine = speaks ? order_key(a.pairs && a.group_size > 1 ? m1 + m2 : m1) : 0u;
+      const uint32_t mine = speaks ? order_key(group_value(m1, m2, a.pairs && a.group_size > 1)) : 0u;
       int before = 0;
       for (int g = 0; g < a.n_group; ++g) before += __shfl_sync(0xffffffffu, mine, g) >= mine + (g >= lane);
       const bool in = speaks && before < a.topk_group;
@@ -482,20 +490,17 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
     for (int j = 0; j < V; ++j) key[j] = there(j) ? order_key(l[j]) : 0u;
     bool near = false;                                                 // the same in a token's lanes
     if constexpr (Groups) {
-      // the two largest of each group (NaN counts as nothing)
+      // the two largest of each group
       float m1 = -INFINITY, m2 = -INFINITY;
 #pragma unroll
       for (int j = 0; j < V; ++j)
-        if (there(j)) {
-          const float x = !bias && a.pairs ? s[j] : l[j];
-          m2 = fmaxf(m2, fminf(m1, x)); m1 = fmaxf(m1, x);
-        }
+        if (there(j)) two_largest(!bias && a.pairs ? s[j] : l[j], m1, m2);
       for (int o = 1; o < 1 << a.group_shift; o <<= 1) {
         const float o1 = __shfl_xor_sync(0xffffffffu, m1, o), o2 = __shfl_xor_sync(0xffffffffu, m2, o);
         m2 = fmaxf(fminf(m1, o1), fmaxf(m2, o2));
         m1 = fmaxf(m1, o1);
       }
-      const uint32_t mine = speaks ? order_key(a.pairs && a.group_size > 1 ? m1 + m2 : m1) : 0u;
+      const uint32_t mine = speaks ? order_key(group_value(m1, m2, a.pairs && a.group_size > 1)) : 0u;
       int before = 0;                                                  // lanes of better groups: of equal ones the lower
 #pragma unroll
       for (int o = 1; o < 8; ++o) before += __shfl_xor_sync(0xffffffffu, mine, o) >= mine + ((lane8 ^ o) >> a.group_shift >= my_group);
