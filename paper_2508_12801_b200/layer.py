@@ -35,6 +35,11 @@ class MoELayer:
             raise ValueError("keep8 is a form of training")
         if int8 and training:
             raise ValueError("int8 is a form of serving: training=False")
+        # what the products take (a backward pass contracts over 2 d_ff columns)
+        unit, most = (16, (1 << 17) - 16) if int8 else (8, 1 << 18) if params.io_dtype == ms.BF16 else (4, 1 << 24)
+        for name, width, top in (("d_model", params.d_model, most), ("d_ff", d_ff, most // 2 if training else most)):
+            if width <= 0 or width % unit or width > top:
+                raise ValueError(f"{name} = {width}: a multiple of {unit} up to {top} is needed")
         self.ctx = ms.create(params, device)
         self.d_ff, self.w_layout, self.training, self.topk, self.keep8, self.int8 = d_ff, w_layout, training, topk, keep8, int8
         p, C, io, dev = params, self.ctx.capacity, self.ctx.io_torch, self.ctx.device
