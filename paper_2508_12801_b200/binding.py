@@ -86,6 +86,13 @@ _lib = _load()
 _vp, _i32 = C.c_void_p, C.c_int32
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+for _name, _n in (("route_fwd", 13), ("dispatch", 7), ("route_bwd", 16), ("gate", 6), ("softtopk_fwd", 4), ("softtopk_bwd", 6), ("softtopk_bwd_aux", 7), ("assign", 6),
+                  ("assign_iterative", 6), ("index_build", 6), ("combine_bwd", 10), ("gate_bwd", 7), ("check_internal", 3), ("test_raise_internal", 2),
+                  ("route_dispatch_host", 10)):
+    getattr(_lib, "maxscore_" + _name).argtypes = [_vp] * _n
+_lib.maxscore_combine.argtypes = [_vp] * 6 + [C.c_int, _vp]
+_lib.maxscore_aux_loss.argtypes = [_vp] * 3 + [C.c_float] + [_vp] * 3
+_lib.maxscore_assign_top2_sinkhorn.argtypes = [_vp] * 2 + [C.c_float, _i32] + [_vp] * 5
 _lib.maxscore_expert_gemm.argtypes = [_vp] * 5 + [_i32] * 3 + [_vp]
 _lib.maxscore_expert_gemm_dw.argtypes = [_vp] * 5 + [_i32] * 4 + [_vp]
 _lib.maxscore_expert_glu.argtypes = [_vp] * 6 + [_i32] * 3 + [_vp]
@@ -188,87 +195,76 @@ def destroy(ctx: Context):
 
 def route_fwd(ctx, hidden, w_gate, expert_bias, logits, scores, expert_idx, slot_idx, gate_w, slot_token,
               expert_load, stats, stream=None):
-    _check(_lib.maxscore_route_fwd(ctx.handle, _ptr(hidden), _ptr(w_gate), _ptr(expert_bias), _ptr(logits),
-                                   _ptr(scores), _ptr(expert_idx), _ptr(slot_idx), _ptr(gate_w), _ptr(slot_token),
-                                   _ptr(expert_load), _ptr(stats), _stream(stream)), "maxscore_route_fwd")
+    _call(ctx, "maxscore_route_fwd", _lib.maxscore_route_fwd, _ptr(hidden), _ptr(w_gate), _ptr(expert_bias), _ptr(logits), _ptr(scores),
+          _ptr(expert_idx), _ptr(slot_idx), _ptr(gate_w), _ptr(slot_token), _ptr(expert_load), _ptr(stats), stream=stream)
 
 
 def dispatch(ctx, src, expert_idx, slot_idx, slot_token, dst, stream=None):
-    _check(_lib.maxscore_dispatch(ctx.handle, _ptr(src), _ptr(expert_idx), _ptr(slot_idx), _ptr(slot_token),
-                                  _ptr(dst), _stream(stream)), "maxscore_dispatch")
+    _call(ctx, "maxscore_dispatch", _lib.maxscore_dispatch, _ptr(src), _ptr(expert_idx), _ptr(slot_idx), _ptr(slot_token), _ptr(dst), stream=stream)
 
 
 def combine(ctx, src, expert_idx, slot_idx, gate_w, dst, accumulate=0, stream=None):
-    _check(_lib.maxscore_combine(ctx.handle, _ptr(src), _ptr(expert_idx), _ptr(slot_idx), _ptr(gate_w), _ptr(dst),
-                                 C.c_int(accumulate), _stream(stream)), "maxscore_combine")
+    _call(ctx, "maxscore_combine", _lib.maxscore_combine, _ptr(src), _ptr(expert_idx), _ptr(slot_idx), _ptr(gate_w), _ptr(dst), C.c_int(accumulate),
+          stream=stream)
 
 
 def route_bwd(ctx, dY, yexp, hidden, w_gate, logits, expert_idx, slot_idx, gate_w, slot_token, dyexp, dgate_w,
               dlogits, dw_gate, dH, stream=None):
-    _check(_lib.maxscore_route_bwd(ctx.handle, _ptr(dY), _ptr(yexp), _ptr(hidden), _ptr(w_gate), _ptr(logits),
-                                   _ptr(expert_idx), _ptr(slot_idx), _ptr(gate_w), _ptr(slot_token), _ptr(dyexp),
-                                   _ptr(dgate_w), _ptr(dlogits), _ptr(dw_gate), _ptr(dH), _stream(stream)),
-           "maxscore_route_bwd")
+    _call(ctx, "maxscore_route_bwd", _lib.maxscore_route_bwd, _ptr(dY), _ptr(yexp), _ptr(hidden), _ptr(w_gate), _ptr(logits), _ptr(expert_idx),
+          _ptr(slot_idx), _ptr(gate_w), _ptr(slot_token), _ptr(dyexp), _ptr(dgate_w), _ptr(dlogits), _ptr(dw_gate), _ptr(dH), stream=stream)
 
 
 def gate(ctx, hidden, w_gate, expert_bias, logits, stream=None):
-    _check(_lib.maxscore_gate(ctx.handle, _ptr(hidden), _ptr(w_gate), _ptr(expert_bias), _ptr(logits),
-                              _stream(stream)), "maxscore_gate")
+    _call(ctx, "maxscore_gate", _lib.maxscore_gate, _ptr(hidden), _ptr(w_gate), _ptr(expert_bias), _ptr(logits), stream=stream)
 
 
 def softtopk_fwd(ctx, logits, scores, stream=None):
-    _check(_lib.maxscore_softtopk_fwd(ctx.handle, _ptr(logits), _ptr(scores), _stream(stream)),
-           "maxscore_softtopk_fwd")
+    _call(ctx, "maxscore_softtopk_fwd", _lib.maxscore_softtopk_fwd, _ptr(logits), _ptr(scores), stream=stream)
 
 
 def softtopk_bwd(ctx, logits, expert_idx, dgate_w, dlogits, stream=None):
-    _check(_lib.maxscore_softtopk_bwd(ctx.handle, _ptr(logits), _ptr(expert_idx), _ptr(dgate_w), _ptr(dlogits),
-                                      _stream(stream)), "maxscore_softtopk_bwd")
+    _call(ctx, "maxscore_softtopk_bwd", _lib.maxscore_softtopk_bwd, _ptr(logits), _ptr(expert_idx), _ptr(dgate_w), _ptr(dlogits), stream=stream)
 
 
 def softtopk_bwd_aux(ctx, logits, expert_idx, dgate_w, dscores_col, dlogits, stream=None):
-    _check(_lib.maxscore_softtopk_bwd_aux(ctx.handle, _ptr(logits), _ptr(expert_idx), _ptr(dgate_w), _ptr(dscores_col),
-                                          _ptr(dlogits), _stream(stream)), "maxscore_softtopk_bwd_aux")
+    _call(ctx, "maxscore_softtopk_bwd_aux", _lib.maxscore_softtopk_bwd_aux, _ptr(logits), _ptr(expert_idx), _ptr(dgate_w), _ptr(dscores_col),
+          _ptr(dlogits), stream=stream)
 
 
 def aux_loss(ctx, scores, expert_load, lam, loss, dscores_col, stream=None):
     """Eq. 9 and its gradient: loss is a 1-element float64 device tensor, dscores_col an [E] float32 one."""
-    _check(_lib.maxscore_aux_loss(ctx.handle, _ptr(scores), _ptr(expert_load), C.c_float(lam), _ptr(loss),
-                                  _ptr(dscores_col), _stream(stream)), "maxscore_aux_loss")
+    _call(ctx, "maxscore_aux_loss", _lib.maxscore_aux_loss, _ptr(scores), _ptr(expert_load), C.c_float(lam), _ptr(loss), _ptr(dscores_col),
+          stream=stream)
 
 
 def assign(ctx, matrix, expert_idx, expert_load, stats, stream=None):
-    _check(_lib.maxscore_assign(ctx.handle, _ptr(matrix), _ptr(expert_idx), _ptr(expert_load), _ptr(stats),
-                                _stream(stream)), "maxscore_assign")
+    _call(ctx, "maxscore_assign", _lib.maxscore_assign, _ptr(matrix), _ptr(expert_idx), _ptr(expert_load), _ptr(stats), stream=stream)
 
 
 def assign_top2_sinkhorn(ctx, scores, sinkhorn_eps, sinkhorn_iters, expert_idx, expert_load, plan, counts, stream=None):
     """Algorithm 1 (k = 2): top-1, then capped Sinkhorn on the residual problem; plan may be None."""
-    _check(_lib.maxscore_assign_top2_sinkhorn(ctx.handle, _ptr(scores), C.c_float(sinkhorn_eps), C.c_int32(sinkhorn_iters),
-                                              _ptr(expert_idx), _ptr(expert_load), _ptr(plan), _ptr(counts),
-                                              _stream(stream)), "maxscore_assign_top2_sinkhorn")
+    _call(ctx, "maxscore_assign_top2_sinkhorn", _lib.maxscore_assign_top2_sinkhorn, _ptr(scores), C.c_float(sinkhorn_eps), C.c_int32(sinkhorn_iters),
+          _ptr(expert_idx), _ptr(expert_load), _ptr(plan), _ptr(counts), stream=stream)
 
 
 def assign_iterative(ctx, scores, expert_idx, expert_load, counts, stream=None):
     """Top-k with capacity, then greedy rerouting of the dropped pairs; counts is an int32[2] device tensor."""
-    _check(_lib.maxscore_assign_iterative(ctx.handle, _ptr(scores), _ptr(expert_idx), _ptr(expert_load), _ptr(counts),
-                                          _stream(stream)), "maxscore_assign_iterative")
+    _call(ctx, "maxscore_assign_iterative", _lib.maxscore_assign_iterative, _ptr(scores), _ptr(expert_idx), _ptr(expert_load), _ptr(counts),
+          stream=stream)
 
 
 def index_build(ctx, expert_idx, slot_idx, slot_token, expert_load, stream=None):
-    _check(_lib.maxscore_index_build(ctx.handle, _ptr(expert_idx), _ptr(slot_idx), _ptr(slot_token),
-                                     _ptr(expert_load), _stream(stream)), "maxscore_index_build")
+    _call(ctx, "maxscore_index_build", _lib.maxscore_index_build, _ptr(expert_idx), _ptr(slot_idx), _ptr(slot_token), _ptr(expert_load),
+          stream=stream)
 
 
 def combine_bwd(ctx, dY, yexp, expert_idx, slot_idx, gate_w, slot_token, dyexp, dgate_w, stream=None):
-    _check(_lib.maxscore_combine_bwd(ctx.handle, _ptr(dY), _ptr(yexp), _ptr(expert_idx), _ptr(slot_idx),
-                                     _ptr(gate_w), _ptr(slot_token), _ptr(dyexp), _ptr(dgate_w), _stream(stream)),
-           "maxscore_combine_bwd")
+    _call(ctx, "maxscore_combine_bwd", _lib.maxscore_combine_bwd, _ptr(dY), _ptr(yexp), _ptr(expert_idx), _ptr(slot_idx), _ptr(gate_w),
+          _ptr(slot_token), _ptr(dyexp), _ptr(dgate_w), stream=stream)
 
 
 def gate_bwd(ctx, hidden, w_gate, dlogits, dw_gate, dH, stream=None):
-    _check(_lib.maxscore_gate_bwd(ctx.handle, _ptr(hidden), _ptr(w_gate), _ptr(dlogits), _ptr(dw_gate), _ptr(dH),
-                                  _stream(stream)), "maxscore_gate_bwd")
+    _call(ctx, "maxscore_gate_bwd", _lib.maxscore_gate_bwd, _ptr(hidden), _ptr(w_gate), _ptr(dlogits), _ptr(dw_gate), _ptr(dH), stream=stream)
 
 
 # ---- the experts between dispatch and combine, and the norms around them --------------------------------
@@ -483,7 +479,7 @@ def topk_bwd(ctx, logits, expert_idx, dgate_w, dscores_col, how, dlogits, stream
 def check_internal(ctx, stream=None) -> int:
     """Reads and clears the context's internal-error flag (synchronises the stream); non-zero = a bounded wait gave up."""
     flag = C.c_uint32(0)
-    _check(_lib.maxscore_check_internal(ctx.handle, C.byref(flag), _stream(stream)), "maxscore_check_internal")
+    _call(ctx, "maxscore_check_internal", _lib.maxscore_check_internal, C.byref(flag), stream=stream)
     return int(flag.value)
 
 
@@ -492,15 +488,13 @@ def launch_count(ctx) -> int:
 
 
 def test_raise_internal(ctx, stream=None):
-    _check(_lib.maxscore_test_raise_internal(ctx.handle, _stream(stream)), "maxscore_test_raise_internal")
+    _call(ctx, "maxscore_test_raise_internal", _lib.maxscore_test_raise_internal, stream=stream)
 
 
 def route_dispatch_host(ctx, hidden_host, w_gate_host, expert_bias_host, dev: DeviceBuffers, expert_idx_host,
                         slot_idx_host, gate_w_host, stats_host, stream=None):
-    _check(_lib.maxscore_route_dispatch_host(ctx.handle, _ptr(hidden_host), _ptr(w_gate_host),
-                                             _ptr(expert_bias_host), C.byref(dev), _ptr(expert_idx_host),
-                                             _ptr(slot_idx_host), _ptr(gate_w_host), _ptr(stats_host),
-                                             _stream(stream)), "maxscore_route_dispatch_host")
+    _call(ctx, "maxscore_route_dispatch_host", _lib.maxscore_route_dispatch_host, _ptr(hidden_host), _ptr(w_gate_host), _ptr(expert_bias_host),
+          C.byref(dev), _ptr(expert_idx_host), _ptr(slot_idx_host), _ptr(gate_w_host), _ptr(stats_host), stream=stream)
 
 
 def index_build_noalloc(T, E, k, C, expert_idx, slot_idx, slot_token, expert_load, stream=None):
