@@ -1,7 +1,7 @@
 // What the C entry points share on the host: the context, the workspace's layout, error texts.
 //
-// The entry points are two translation units, and so two modules on the device: the first kernel that a process uses loads its module
-// whole, and the experts' and norms' kernels are many (first context of a process 41 ms with them, 7 without).
+// The entry points are four translation units (router; experts and norms; top-k; 8-bit experts), and so four modules on the device: the first
+// kernel that a process uses loads its module whole, and the experts' and norms' kernels are many (first context of a process 41 ms with them, 7 without).
 #pragma once
 #include "../../include/maxscore.h"
 

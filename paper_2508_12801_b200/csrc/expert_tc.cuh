@@ -4,7 +4,7 @@
 // columns of B, the pair's MMA reads both halves, and each CTA's tensor memory ends up with its 128 rows of all 256 columns.
 // That takes a third off the operand traffic per flop of a single CTA's 128 x 256 tile (64 bytes per clock and SM at full rate
 // instead of 96; TMA loads that hit the L2 reach 67).  Two accumulators alternate, so the epilogue of a tile runs under the MMAs of the next.
-//   warp 0: TMA loads, five or six stages of 64-deep slices (three or four of the 256 x 512 tiles);  warp 1: TMEM, and in the leading CTA the MMAs;
+//   warp 0: TMA loads, four to six stages of 128-byte slices (three or four of the 256 x 512 tiles; a slice is 64 deep in bf16, 128 in bytes);  warp 1: TMEM, and in the leading CTA the MMAs;
 //   the other eight (sixteen): epilogue, a TMEM lane quarter and a part of the columns each, out through staging boxes.
 // Both operand majors are read in place through the descriptors: no weight is ever transposed.
 //
@@ -18,8 +18,9 @@
 // top of the loads); long runs at E 128 2 700 to 2 800 and 2 050 to 2 150.  What a sum stands for is worked out in the epilogue.
 // Form kKeep8: h as ever, then g and u block by block from the accumulator into 8 bits (E 128, C 4096, 4096 -> 1024: 7.0 to 7.9 ms, as when they are
 // kept in bf16; 6.3 without).  The backward pass takes them into registers, a sector a lane, one step ahead of its use, and forms h again: E 64, C 2560,
-// 2048 -> 1000 640 to 680 us, 810 TFLOP/s, where the bf16 form without h takes 580 to 630.  Its epilogue is 18 000 clocks a tile of the 27 000 that a tile takes
-// in long runs at 1.2 GHz, under the power cap.
+// 2048 -> 1000 640 to 680 us, 810 TFLOP/s, where the bf16 form without h takes 580 to 630.  A tile takes 27 000 clocks there, its MMAs 16 400 of them at the
+// full rate: for the rest they wait for operands (the tensor pipe is active in 58 % of the clocks), though the epilogue, 18 000 clocks, is hidden.  The ring is
+// a stage shorter than in bf16, and kept values pass the L2 as 32 sectors in 32 lines a load.
 #pragma once
 #include "expert.cuh"
 #include "int8.cuh"

@@ -118,7 +118,8 @@ rows8_kernel(const uint4* __restrict__ src, const int32_t* __restrict__ load, ui
 
 // ---- weights [E][d_in][d_out] -> integers [E][d_out][d_in] --------------------------------------------------------------------
 // A CTA owns 64 columns of one expert: their largest magnitudes first, then tiles of 64 columns x 128 rows turned round in shared
-// memory.  Once per weight, so it only has to be reasonable: the second reading comes from the L2 where a block of columns fits.
+// memory.  Once per weight, so it only has to be reasonable: the second reading comes from the L2 where a block of columns fits.  E 64, 2048 x 2048
+// 413 us, 1.9 TB/s (weights that lie the other way round take rows8_kernel: 129 us, 6.2 TB/s).
 constexpr int kTurnCols = 64, kTurnRows = 128;
 __global__ void __launch_bounds__(256)
 turn8_kernel(const __nv_bfloat16* __restrict__ w, int8_t* __restrict__ q, float* __restrict__ scale, int d_in, int d_out) {

@@ -12,7 +12,8 @@ it: a caller who wants it takes the calls below with combine_bwd, softtopk_bwd_a
 Forms of the layer:
     topk   routing by top-k (binding.make_topk) in place of SoftTopk and the flow; the balance loss enters the backward pass by dscores_col
     keep8  training with the experts' activations kept in 8 bits: [g | u] as integers, h formed again and the rows dispatched again in
-           the backward pass, so that between the passes a layer holds yexp and `keep` alone; the other buffers may be another layer's
+           the backward pass, so that between the passes a layer holds yexp, `keep`, y [T, d_model] and the router's rows (logits, scores, indices,
+           weights), beside its context's workspace; the other buffers may be another layer's
     int8   serving with rows and weights in 8-bit integers (weights from MoELayer.quantise)
 """
 from __future__ import annotations
