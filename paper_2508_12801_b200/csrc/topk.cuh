@@ -48,6 +48,13 @@ __device__ __forceinline__ void two_largest(float x, float& m1, float& m2) {
 // value of a group; inf - inf makes it the last
 __device__ __forceinline__ float group_value(float m1, float m2, bool pairs) { return pairs ? fmaxf(m1 + m2, -INFINITY) : m1; }
 
+// How far from v in fp32 the value may lie that 64 bits give: the least it can be for a group that stays, the most for one that goes.  Scores are off by
+// 2^-21 and each c by 2^-24 of itself, their sum by 2^-24 more; the terms count and not the sum, in which biases of both signs cancel.  Twice that.
+__device__ __forceinline__ float group_bound(float m1, float m2, bool pairs, float v, bool stays) {
+  const float err = fmaf(0x1p-22f, fabsf(m1) + (pairs ? fabsf(m2) : 0.f), 0x1p-19f);
+  return fabsf(v) == INFINITY ? v : stays ? v - err : v + err;
+}
+
 // e^x for x <= 0: 2^t with t = x log2(e) rounded, then what the rounding left of the exponent as a factor 1 + r ln 2.  Off by 2^-22
 // (the approximation of 2^t) and some 2^-24 (the products) of itself; below 2^-126 it is 0.  NaN stays NaN.
 __device__ __forceinline__ float exp_down(float x) {
@@ -285,14 +292,17 @@ topk_fwd_scan_kernel(const float* __restrict__ logits, const float* __restrict__
       if (speaks)
         for (int i = 0; i < a.group_size; ++i) two_largest(grouped[lane * (a.group_size + 1) + i], m1, m2);
       __syncwarp();
-      const uint32_t mine = speaks ? order_key(group_value(m1, m2, a.pairs && a.group_size > 1)) : 0u;
+      const bool two = a.pairs && a.group_size > 1;
+      const float value = group_value(m1, m2, two);
+      const uint32_t mine = speaks ? order_key(value) : 0u;
       int before = 0;
       for (int g = 0; g < a.n_group; ++g) before += __shfl_sync(0xffffffffu, mine, g) >= mine + (g >= lane);
       const bool in = speaks && before < a.topk_group;
       if (bias || a.pairs) {
-        const float low = order_value(__reduce_min_sync(0xffffffffu, in ? mine : 0xffffffffu));
-        const float high = order_value(__reduce_max_sync(0xffffffffu, in ? 0u : mine));
-        near = !(low - high > 0x1p-18f + 0x1p-21f * fabsf(low));       // two terms, hence twice the bound below
+        const uint32_t edge = order_key(group_bound(m1, m2, two, value, in));
+        const float low = order_value(__reduce_min_sync(0xffffffffu, in ? edge : 0xffffffffu));
+        const float high = order_value(__reduce_max_sync(0xffffffffu, speaks && !in ? edge : 0u));
+        near = !(low > high);
       }
       const uint32_t kept = __ballot_sync(0xffffffffu, in);
 #pragma unroll
@@ -500,14 +510,17 @@ topk_fwd_kernel(const float* __restrict__ logits, const float* __restrict__ bias
         m2 = fmaxf(fminf(m1, o1), fmaxf(m2, o2));
         m1 = fmaxf(m1, o1);
       }
-      const uint32_t mine = speaks ? order_key(group_value(m1, m2, a.pairs && a.group_size > 1)) : 0u;
+      const bool two = a.pairs && a.group_size > 1;
+      const float value = group_value(m1, m2, two);
+      const uint32_t mine = speaks ? order_key(value) : 0u;
       int before = 0;                                                  // lanes of better groups: of equal ones the lower
 #pragma unroll
       for (int o = 1; o < 8; ++o) before += __shfl_xor_sync(0xffffffffu, mine, o) >= mine + ((lane8 ^ o) >> a.group_shift >= my_group);
       const bool in = speaks && before < a.topk_group << a.group_shift;
       if (bias || a.pairs) {
-        const float low = order_value(~seg_max(in ? ~mine : 0u)), high = order_value(seg_max(in ? 0u : mine));
-        near = !(low - high > 0x1p-18f + 0x1p-21f * fabsf(low));       // two terms, hence twice the bound below
+        const uint32_t edge = order_key(group_bound(m1, m2, two, value, in));
+        const float low = order_value(~seg_max(in ? ~edge : 0u)), high = order_value(seg_max(speaks && !in ? edge : 0u));
+        near = !(low > high);
       }
 #pragma unroll
       for (int j = 0; j < V; ++j) key[j] = in ? key[j] : 0u;
