@@ -71,11 +71,16 @@ class MoELayer:
             self.dlogits = work("dlogits", lambda: new(p.T, p.E, dtype=torch.float32))
 
     def quantise(self, w_up, w_down, stream=None):
-        """The experts' weights as an int8 layer takes them: ((integers, scales) of w_up, the same of w_down), once per weight."""
+        """The experts' weights as an int8 layer takes them: ((integers, scales) of w_up, the same of w_down), once per weight.  They belong to
+        `stream`, the current one if there is none."""
         d, f, E, dev = self.ctx.params.d_model, self.d_ff, self.ctx.params.E, self.ctx.device
         out = []
+        if stream is not None and not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(getattr(stream, "cuda_stream", stream), device=dev)
         for w, d_in, d_out in ((w_up, d, 2 * f), (w_down, f, d)):
-            q, s = torch.empty(E, d_out, d_in, dtype=torch.int8, device=dev), torch.empty(E, d_out, dtype=torch.float32, device=dev)
+            # memory of the stream that writes it: the current one's may still be read by what it has queued
+            with torch.cuda.stream(stream):
+                q, s = torch.empty(E, d_out, d_in, dtype=torch.int8, device=dev), torch.empty(E, d_out, dtype=torch.float32, device=dev)
             ms.expert_quant_weight(self.ctx, w, q, s, d_in, d_out, self.w_layout, stream=stream)
             out.append((q, s))
         return tuple(out)
